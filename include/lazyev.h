@@ -281,6 +281,111 @@ int lazyev_score_pairs(const int32_t *delta_t /*device*/, const int32_t *mri /*d
                        double *score /*device*/, int64_t n, int32_t score_flags,
                        void *stream);
 
+/* ---- Rows around a decode step: norms and rotation, a cache in pages, attention over pages.  The calls of this
+ * section keep no state: they need no context (but lazyev_decode_step_shared), enqueue on the stream they are given (which
+ * belongs to the current device) and return without waiting.  Two calls may run at once, on any streams, if neither writes what
+ * the other reads or writes (the workspace of lazyev_pages_attend included).  They can be captured into a HIP graph; a replay
+ * works on what the pointers hold then, with the lengths of the captured call.  No alignment beyond the element's
+ * is asked for (multiples of 16 bytes are faster) but for the workspace. */
+
+/* Heads of the tokens of a batch, head_dim elements each: element e of head h of token i of sequence s lies at
+ * rows[s * seq_stride + i * token_stride + h * head_stride + e] (strides in elements, of any sign, so that a head
+ * may be a view into a joint projection), its result at `to` by the to_ strides: any places, the entries of
+ * a cache for instance, of which no two heads share one.  `to` may be `rows` with the same strides; an
+ * overlap of any other kind gives unspecified rows.
+ * weight (nullable): [head_dim] of the rows' type: the head is normed, x / sqrt(mean(x^2) + eps) * weight. */
+typedef struct {
+  const void *rows;             /* (device)                                                             */
+  void       *to;               /* (device)                                                             */
+  int64_t     seq_stride, token_stride, head_stride;
+  int64_t     to_seq_stride, to_token_stride, to_head_stride;
+  const void *weight;           /* (device, nullable)                                                   */
+  int32_t     n_heads;
+} lazyev_heads;
+
+#define LAZYEV_ROPE_NONE   0    /* no rotation                                                          */
+#define LAZYEV_ROPE_HALVES 1    /* elements j and j + dims / 2 are turned together, j < dims / 2        */
+#define LAZYEV_ROPE_PAIRS  2    /* elements 2 j and 2 j + 1                                             */
+/* The pair j of a token at position p is turned by the angle p * inv_freq[j]: (x, y) becomes (x cos - y sin, y cos + x sin).
+ * The angle is worked out in binary64, so positions may be as far as they like.  Elements from dims on stay. */
+typedef struct {
+  int32_t      layout;          /* LAZYEV_ROPE_*                                                        */
+  int32_t      dims;            /* a multiple of 16, at most head_dim (layout NONE: ignored)            */
+  const float *inv_freq;        /* (device) [dims / 2] fp32 (layout NONE: ignored)                      */
+  float        eps;             /* of the norms, >= 0                                                   */
+} lazyev_rotation;
+
+/* Norms of the query and key heads and the rotation by the token's position, in one pass: what lazyev_decode_step and
+ * lazyev_prefill_track take their rows after.  Arithmetic in fp32, rounded once to the rows' type.
+ * Token i of sequence s is at position start + positions[s * n_tokens + i], or start + i without `positions`.
+ * q or k may be null (not both).  head_dim 64 or 128, dtype LAZYEV_DTYPE_*.  n_seqs or n_tokens 0: nothing to do.
+ * Errors: EINVAL, EHIP. */
+int lazyev_norm_rope(int32_t n_seqs, int32_t n_tokens, int32_t head_dim, int32_t dtype,
+                     const lazyev_heads *q /*host, nullable*/, const lazyev_heads *k /*host, nullable*/,
+                     const lazyev_rotation *rotation /*host*/, const int32_t *positions /*device, nullable*/,
+                     int32_t start, void *stream);
+
+/* A cache in pages: entry i of table row s is place i % page_size of page table[s * table_stride + i / page_size],
+ * for every KV head.  Rows of the table may share pages.  A page number outside 0 .. n_pages - 1 stands for no page: its
+ * entries are not written and no token sees them.
+ * The caches of a context are such a pool too, per layer: n_pages = batch pages of page_size = capacity entries, so the same
+ * calls fill a sequence's prompt (table row {sequence}) and attend over it. */
+typedef struct {
+  int32_t n_kv_heads, head_dim, dtype;             /* head_dim 64 or 128                                */
+  int32_t n_pages, page_size;                      /* page_size up to 2^20                              */
+  int32_t n_seqs, table_stride;                    /* rows of the table, entries from one to the next   */
+  void    *k_pages, *v_pages;                      /* (device) [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
+  const int32_t *table;                            /* (device) [n_seqs][table_stride]                   */
+} lazyev_pages;
+
+/* Writes the keys and values of n_tokens tokens of every table row to the row's entries start .. start + n_tokens - 1: the keys
+ * normed (k->weight) and rotated on the way, by the position position0 + i of the i-th token, the values as they are
+ * (v->weight null).  k and v describe the source only: their `to` members are ignored.
+ * A page that several of the written entries lead to (one number twice in the table) holds unspecified ones of their rows.
+ * start + n_tokens <= table_stride * page_size.  Errors: EINVAL, EHIP. */
+int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32_t n_tokens,
+                        const lazyev_heads *k /*host*/, const lazyev_heads *v /*host*/,
+                        const lazyev_rotation *rotation /*host*/, int32_t position0, void *stream);
+
+/* Attention of n_tokens tokens of every table row over the row's first `length` entries (Eq. 4 for many queries at once: the
+ * entries are read once for the tokens that share them):
+ *   out[s][i][h] = softmax(scale * q[s][i][h] K^T) V,  lse[s][i][h] = ln(sum of exp(scale * q[s][i][h] k))
+ * over the entries below visible[s * n_tokens + i] (null: all; values beyond 0 .. length count as the nearest of the two).
+ * A batch's decode step over its common prefix: one table row, every sequence's query a token of it.  A prompt after the
+ * prefix: likewise.  A prompt over itself: visible = i + 1.
+ * A token that sees nothing gets zeros, and lse = -inf.  What a token does not see has no influence on it, whatever it holds.
+ * joined_out, joined_lse (nullable, together): the output and lse of the same queries over other entries, for instance the
+ *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  `out` is not q.
+ * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; bf16 weights
+ * are rounded to bf16 for the product with V.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times.
+ * Workspace: lazyev_pages_attend_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).
+ * Errors: EINVAL (length 0 .. table_stride * page_size among them), EWORKSPACE, EHIP. */
+int lazyev_pages_attend(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,
+                        const int32_t *visible /*device, nullable*/,
+                        const void *q /*device, [n_seqs][n_tokens][n_q_heads][head_dim]*/,
+                        const void *joined_out /*device, nullable, like q*/,
+                        const float *joined_lse /*device, nullable, [n_seqs][n_tokens][n_q_heads]*/,
+                        void *out /*device, like q*/, float *lse /*device, nullable*/, float scale,
+                        void *workspace /*device*/, size_t workspace_bytes, void *stream);
+/* Bytes for such a call; 0 also for arguments that the call refuses. */
+size_t lazyev_pages_attend_workspace(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens,
+                                     int32_t n_q_heads);
+
+/* lazyev_decode_step of a batch whose sequences share a prefix: the same append and the same tracking, with attention over
+ * the first prefix_len entries of the pages' one table row AND the sequences' own caches.  The softmax is over both: p of the
+ * activation test (and p_out) is the weight that an own entry has beside the prefix.  The prefix takes no part in tracking and is
+ * never evicted.  `out` is not q.  prefix_len 0 is lazyev_decode_step.  With per-sequence timing, sequences that take no part are left alone.
+ * The pages' head_dim, dtype and n_kv_heads are the context's and n_seqs is 1; scale is the context's.  Own and prefix parts
+ * are rounded to the rows' type once each.
+ * workspace: lazyev_pages_attend_workspace(prefix, prefix_len, batch, n_q_heads) bytes, on the context's stream.
+ * Errors: those of lazyev_decode_step, EWORKSPACE, EINVAL (a prefix that does not fit the context; the two-kernel attention
+ * of lazyev_set_variant 0).  Nothing is enqueued on an error but EHIP. */
+int lazyev_decode_step_shared(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q /*device*/,
+                              const void *k_new /*device*/, const void *v_new /*device*/, void *out /*device*/,
+                              const lazyev_pages *prefix /*host*/, int32_t prefix_len,
+                              void *workspace /*device*/, size_t workspace_bytes,
+                              float *p_out /*device, nullable*/, const float *p_override /*device, nullable*/);
+
 void lazyev_destroy(lazyev_ctx *ctx);              /* frees host memory only; NULL is allowed */
 const char *lazyev_strerror(int code);
 int lazyev_last_hip_error(const lazyev_ctx *ctx);  /* hipError_t of the last EHIP, else 0 */

@@ -27,6 +27,7 @@ SCORE_H2_DECREASING = 16
 SCORE_CURRENT_ATTENTION = 32
 MAX_HIST_BINS = 8192
 LDS_CANDIDATES = 8192
+ROPE_NONE, ROPE_HALVES, ROPE_PAIRS = 0, 1, 2
 
 
 class Config(C.Structure):
@@ -46,12 +47,31 @@ class Stats(C.Structure):
                 ("n_rows_moved", C.POINTER(C.c_int64))]
 
 
+class Heads(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("to", C.c_void_p), ("seq_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("to_seq_stride", C.c_int64),
+                ("to_token_stride", C.c_int64), ("to_head_stride", C.c_int64),
+                ("weight", C.c_void_p), ("n_heads", C.c_int32)]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("dims", C.c_int32), ("inv_freq", C.c_void_p), ("eps", C.c_float)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_seqs", C.c_int32),
+                ("table_stride", C.c_int32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p),
+                ("table", C.c_void_p)]
+
+
 # what include/lazyev.h declares (the contract) ...
 EXPORTS = ["lazyev_capacity", "lazyev_workspace_size", "lazyev_init", "lazyev_decode_step",
            "lazyev_prefill_track", "lazyev_prefill_track_seq", "lazyev_evict", "lazyev_evict_all",
            "lazyev_evict_static", "lazyev_stats", "lazyev_admit", "lazyev_retire",
            "lazyev_cached_before_step", "lazyev_mri_histogram", "lazyev_window_from_histogram",
-           "lazyev_score_pairs", "lazyev_destroy", "lazyev_strerror", "lazyev_last_hip_error"]
+           "lazyev_score_pairs", "lazyev_norm_rope", "lazyev_pages_append", "lazyev_pages_attend",
+           "lazyev_pages_attend_workspace", "lazyev_decode_step_shared", "lazyev_destroy", "lazyev_strerror", "lazyev_last_hip_error"]
 # ... and include/lazyev_bench.h (knobs and the per-kernel timer in the same library; the plain
 # streaming probes in liblazyev_bench.so, loaded by bench_lib() when somebody measures)
 BENCH_EXPORTS = ["lazyev_set_chunk", "lazyev_set_target_blocks", "lazyev_set_variant", "lazyev_set_spin_ticks",
@@ -112,6 +132,22 @@ lib.lazyev_mri_histogram.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER
 lib.lazyev_score_pairs.restype = C.c_int
 lib.lazyev_score_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32,
                                    C.c_void_p]
+lib.lazyev_norm_rope.restype = C.c_int
+lib.lazyev_norm_rope.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(Heads), C.POINTER(Heads),
+                                 C.POINTER(Rotation), C.c_void_p, C.c_int32, C.c_void_p]
+lib.lazyev_pages_append.restype = C.c_int
+lib.lazyev_pages_append.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.POINTER(Heads), C.POINTER(Heads),
+                                    C.POINTER(Rotation), C.c_int32, C.c_void_p]
+lib.lazyev_pages_attend_workspace.restype = C.c_size_t
+lib.lazyev_pages_attend_workspace.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32]
+lib.lazyev_pages_attend.restype = C.c_int
+lib.lazyev_pages_attend.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
+                                    C.c_size_t, C.c_void_p]
+lib.lazyev_decode_step_shared.restype = C.c_int
+lib.lazyev_decode_step_shared.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p, C.POINTER(Pages), C.c_int32, C.c_void_p, C.c_size_t,
+                                          C.c_void_p, C.c_void_p]
 lib.lazyev_set_chunk.restype = C.c_int
 lib.lazyev_set_chunk.argtypes = [C.c_void_p, C.c_int32]
 lib.lazyev_set_target_blocks.restype = C.c_int
@@ -169,6 +205,173 @@ def window_from_histogram(hist, quantile: float = 0.8) -> int:
     w = C.c_int32(0)
     _check(lib.lazyev_window_from_histogram(arr, n, quantile, C.byref(w)), "lazyev_window_from_histogram")
     return w.value
+
+
+_DTYPES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+
+
+def _need(ok, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _stream_of(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _on(device):
+    """The device as the current one: launches and their stream belong to it."""
+    return torch.cuda.device(device)
+
+
+class NormRope:
+    """Norms of the query and key heads of a layer and the rotation by the token's position (lazyev_norm_rope).
+
+    q_weight, k_weight [head_dim] of the rows' type, or None: not normed.  inv_freq [dims / 2] fp32, or None: not
+    rotated; layout ROPE_HALVES (elements j and j + dims / 2 form a pair) or ROPE_PAIRS (2 j and 2 j + 1).
+    """
+
+    def __init__(self, head_dim, dtype=torch.bfloat16, q_weight=None, k_weight=None, eps=1e-6, inv_freq=None,
+                 layout=ROPE_HALVES):
+        _need(dtype in _DTYPES and head_dim in (64, 128), "rows of 64 or 128 elements, fp32 or bf16")
+        self.device = None
+        for w in (q_weight, k_weight):
+            _need(w is None or (w.dtype == dtype and w.shape == (head_dim,) and w.is_contiguous()),
+                  "a norm's weight is [head_dim], contiguous, of the rows' type")
+        _need(inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()),
+              "inv_freq is [dims / 2], contiguous, fp32")
+        for x in (q_weight, k_weight, inv_freq):
+            if x is None:
+                continue
+            _need(x.is_cuda and self.device in (None, x.device), "weights and frequencies are on one GPU")
+            self.device = x.device
+        dims = 0 if inv_freq is None else 2 * inv_freq.numel()
+        _need(inv_freq is None or (dims >= 16 and dims % 16 == 0 and dims <= head_dim and layout in (ROPE_HALVES, ROPE_PAIRS)),
+              "rotated elements: a multiple of 16, at most head_dim")
+        self.head_dim, self.dtype = head_dim, dtype
+        self.q_weight, self.k_weight, self.inv_freq = q_weight, k_weight, inv_freq
+        self.rotation = Rotation(ROPE_NONE if inv_freq is None else layout, dims, 0 if inv_freq is None else inv_freq.data_ptr(), eps)
+
+    def heads(self, x, to, weight):
+        """lazyev_heads of x [S,n,H,d] or [n,H,d] (any strides, the last one 1) with its result at `to` (the same shape)."""
+        for y in (x, to):
+            _need(y.is_cuda and y.dtype == self.dtype and y.dim() in (3, 4) and y.shape == x.shape and y.shape[-1] == self.head_dim and
+                  (y.stride(-1) == 1 or y.numel() == 0), "heads are [S, n, H, head_dim] or [n, H, head_dim] of the rows' type on a GPU, "
+                  "their elements side by side")
+            _need(y.device == x.device and self.device in (None, y.device), "one GPU for everything in a call")
+        a, b = x.stride(), to.stride()
+        if len(a) == 3:
+            a, b = (0,) + a, (0,) + b
+        return Heads(x.data_ptr(), to.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2],
+                     None if weight is None else weight.data_ptr(), x.shape[-2])
+
+    def __call__(self, q=None, k=None, positions=None, start=0, q_out=None, k_out=None):
+        """q, k [S,n,H,d] or [n,H,d] (either may be None) -> (q_out, k_out), new tensors where none are given (in place:
+        the same tensor).  positions int32 [S,n] or [n]: token i is at start + positions[i]; None: at start + i."""
+        _need(q is not None or k is not None, "queries, keys or both")
+        first = q if q is not None else k
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        hq = None if q is None else self.heads(q, q_out, self.q_weight)
+        hk = None if k is None else self.heads(k, k_out, self.k_weight)
+        if q is not None and k is not None:
+            _need(q.shape[:-2] == k.shape[:-2] and q.device == k.device, "queries and keys of the same tokens")
+        if positions is not None:
+            _need(positions.dtype == torch.int32 and positions.shape == first.shape[:-2] and positions.is_contiguous() and
+                  positions.device == first.device, "positions are int32, one for each token, contiguous, on the rows' GPU")
+        n_seqs, n_tokens = (1, first.shape[0]) if first.dim() == 3 else first.shape[:2]
+        _need(-1 << 31 <= start < 1 << 31, "start is a 32-bit number")
+        with _on(first.device):
+            code = lib.lazyev_norm_rope(n_seqs, n_tokens, self.head_dim, _DTYPES[self.dtype], hq, hk, self.rotation, _ptr(positions),
+                                        start, _stream_of(first.device))
+        _check(code, "lazyev_norm_rope")
+        return q_out, k_out
+
+
+class PagedCache:
+    """Keys and values of one layer in pages: k_pages, v_pages [n_pages,Hkv,page_size,d] and table [S,m] int32 (entry i of row s is
+    place i % page_size of page table[s, i // page_size]), all the caller's tensors.  A layer's caches of a LazyEviction are such
+    pages too: PagedCache(eng.k_cache[l], eng.v_cache[l], table) with one page per sequence, a page number = a sequence."""
+
+    def __init__(self, k_pages, v_pages, table, n_q_heads=None):
+        for x in (k_pages, v_pages):
+            _need(x.is_cuda and x.dtype in _DTYPES and x.dim() == 4 and x.is_contiguous() and x.shape == k_pages.shape and
+                  x.dtype == k_pages.dtype and x.device == k_pages.device and x.numel() > 0,
+                  "pages are [n_pages, Hkv, page_size, head_dim], contiguous, fp32 or bf16, on a GPU")
+        _need(table.dtype == torch.int32 and table.dim() == 2 and table.numel() > 0 and table.device == k_pages.device and
+              table.stride(1) == 1 and (table.shape[0] == 1 or table.stride(0) >= table.shape[1]),
+              "the table is [S, pages of a row], int32, rows side by side, on the pages' GPU")
+        n_pages, heads, page_size, d = k_pages.shape
+        _need(d in (64, 128), "rows of 64 or 128 elements")
+        self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
+        self.n_q_heads, self.device, self.dtype = n_q_heads, k_pages.device, k_pages.dtype
+        self.entries = table.shape[1] * page_size      # of a row
+        self.pages = Pages(heads, d, _DTYPES[self.dtype], n_pages, page_size, table.shape[0],
+                           table.stride(0) if table.shape[0] > 1 else table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr())
+
+    def append(self, start, k, v, rope=None, position0=None):
+        """lazyev_pages_append: k, v [S,n,Hkv,d] (or [n,Hkv,d] of a single row; any strides, the last one 1) become the entries
+        start .. start + n - 1, the keys normed and rotated by `rope` (a NormRope, None: as they are) on the way, token i by
+        the position position0 + i (None: its entry's number)."""
+        pg = self.pages
+        rope = rope if rope is not None else NormRope(pg.head_dim, self.dtype)
+        _need(rope.dtype == self.dtype and rope.head_dim == pg.head_dim, "the rotation's rows are the pages'")
+        for x in (k, v):
+            _need((x.dim() == 4 and x.shape[0] == pg.n_seqs or x.dim() == 3 and pg.n_seqs == 1) and x.shape[-2] == pg.n_kv_heads and
+                  x.device == self.device and x.shape == k.shape, "keys and values are [S, n, Hkv, head_dim] of the table's rows")
+        n = k.shape[-3]
+        _need(0 <= start and start + n <= self.entries, "entries beyond the table's row")
+        hk, hv = rope.heads(k, k, rope.k_weight), rope.heads(v, v, None)
+        with _on(self.device):
+            code = lib.lazyev_pages_append(pg, start, n, hk, hv, rope.rotation, start if position0 is None else position0,
+                                           _stream_of(self.device))
+        _check(code, "lazyev_pages_append")
+
+    def workspace_bytes(self, length, n_tokens, n_q_heads=None) -> int:
+        return lib.lazyev_pages_attend_workspace(self.pages, length, n_tokens, n_q_heads or self.n_q_heads or self.pages.n_kv_heads)
+
+    def attend(self, length, q, visible=None, joined=None, out=None, lse=None, scale=0.0, workspace=None):
+        """lazyev_pages_attend: q [S,n,Hq,d] (or [n,Hq,d] of a single row) over the first `length` entries -> (out like q,
+        lse [S,n,Hq] fp32).  visible int32 [S,n]: entries that a token sees (None: all).  joined: (out, lse) of the same queries
+        over other entries, to be joined.  workspace: uint8, at least workspace_bytes(length, n) (None: allocated)."""
+        pg = self.pages
+        _need(q.is_cuda and q.device == self.device and q.dtype == self.dtype and q.is_contiguous() and
+              (q.dim() == 4 and q.shape[0] == pg.n_seqs or q.dim() == 3 and pg.n_seqs == 1) and q.shape[-1] == pg.head_dim,
+              "queries are [S, n, Hq, head_dim] of the table's rows, contiguous, of the pages' type, on their GPU")
+        n, n_q_heads = q.shape[-3], q.shape[-2]
+        _need(self.n_q_heads in (None, n_q_heads), "another number of query heads")
+        _need(0 <= length <= self.entries, "entries beyond the table's row")
+        out = torch.empty_like(q) if out is None else out
+        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device) if lse is None else lse
+        outs, lses = [out], [lse]
+        if joined is not None:
+            outs.append(joined[0])
+            lses.append(joined[1])
+        for x in outs:
+            _need(x.shape == q.shape and x.dtype == q.dtype and x.is_contiguous() and x.device == q.device, "outputs are like q")
+        for x in lses:
+            _need(x.shape == q.shape[:-1] and x.dtype == torch.float32 and x.is_contiguous() and x.device == q.device,
+                  "log-sum-exps are fp32, one for each row of q")
+        if visible is not None:
+            _need(visible.dtype == torch.int32 and visible.shape == q.shape[:-2] and visible.is_contiguous() and visible.device == q.device,
+                  "visible is int32, one for each token, contiguous, on the pages' GPU")
+        with _on(self.device):
+            workspace, n_bytes = self._workspace(length, n, n_q_heads, workspace)
+            code = lib.lazyev_pages_attend(pg, length, n, n_q_heads, _ptr(visible), q.data_ptr(), _ptr(outs[1] if joined is not None else None),
+                                           _ptr(lses[1] if joined is not None else None), out.data_ptr(), lse.data_ptr(), scale,
+                                           _ptr(workspace), n_bytes, _stream_of(self.device))
+        _check(code, "lazyev_pages_attend")
+        return out, lse
+
+    def _workspace(self, length, n_tokens, n_q_heads, given):
+        """(workspace, its bytes) for a call: the given one, or one from torch's allocator for the current stream."""
+        if given is not None:
+            _need(given.dtype == torch.uint8 and given.is_contiguous() and given.device == self.device, "a workspace is bytes on the pages' GPU")
+            return given, given.numel()
+        n = lib.lazyev_pages_attend_workspace(self.pages, length, n_tokens, n_q_heads)
+        return (torch.empty(n, dtype=torch.uint8, device=self.device), n) if n else (None, 0)
 
 
 class LazyEviction:
@@ -232,6 +435,19 @@ class LazyEviction:
                                       _ptr(p_override))
         if code != OK:
             raise LazyevError(code, "lazyev_decode_step")
+
+    def decode_step_shared(self, layer, t, q, k_new, v_new, out, prefix, prefix_len, p_out=None, p_override=None,
+                           workspace=None):
+        """lazyev_decode_step_shared: decode_step over the first prefix_len entries of `prefix` (a PagedCache of one
+        table row) and the sequences' own caches."""
+        cfg = self.cfg
+        with torch.cuda.stream(self.stream):
+            workspace, n_bytes = prefix._workspace(prefix_len, cfg.batch, cfg.n_q_heads, workspace)
+            code = lib.lazyev_decode_step_shared(self._ctx, layer, t, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                                 out.data_ptr(), prefix.pages, prefix_len, _ptr(workspace), n_bytes,
+                                                 _ptr(p_out), _ptr(p_override))
+        if code != OK:
+            raise LazyevError(code, "lazyev_decode_step_shared")
 
     def prefill_track(self, layer, q_prompt, p_out=None, p_override=None):
         """lazyev_prefill_track.  q_prompt [S,P,Hq,d]; p_out / p_override [S,Hq,P,P] fp32."""

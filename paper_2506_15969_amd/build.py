@@ -30,6 +30,10 @@ SOURCES = {"decode_kernels": ("decode_kernels.hip", []),
            # the eviction file holds the bit-reproducible binary64 score: no fused multiply-add there
            "evict_kernels": ("evict_kernels.hip", ["-ffp-contract=off"]),
            "lazyev_api": ("lazyev_api.hip", []),
+           # rows around a decode step, a cache in pages and the attention over it
+           "rope_kernels": ("rope_kernels.hip", []),
+           "pages_kernels": ("pages_kernels.hip", []),
+           "pages_api": ("pages_api.hip", []),
            "prefill_kernels": ("prefill_kernels.hip", ["-fno-honor-nans"])}
 # measuring aids (plain streaming probes): a library of their own, not part of the path
 BENCH_LIB = os.path.join(LIBDIR, "liblazyev_bench.so")

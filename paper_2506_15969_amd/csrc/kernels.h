@@ -199,6 +199,63 @@ struct PrefillArgs {
 };
 hipError_t launch_prefill_track(const PrefillArgs &a, hipStream_t stream);
 
+// Rows of heads on their way through norm and rotation (see lazyev_heads).
+struct RopeRows {
+  const void *in, *weight;
+  void *out;                        // with pages: the pool
+  int64_t in_seq, in_token, in_head, out_seq, out_token, out_head;   // elements
+  int32_t heads, turn;              // turn 0: not rotated
+};
+// A table of pages and the division of an entry's number by the page size.
+struct PageTable {
+  const int32_t *table;             // null: rows go by their strides
+  int32_t stride, n_pages, page_size;
+  uint32_t magic, shift;            // see page_div
+};
+// Numbers for page_of: n / d = (n + floor(n magic / 2^32)) >> shift for n < 2^31, 2^(shift - 1) < d <= 2^shift.
+inline void page_div(PageTable &t) {
+  t.shift = 0;
+  while ((1u << t.shift) < static_cast<uint32_t>(t.page_size)) ++t.shift;
+  t.magic = static_cast<uint32_t>(((((1ull << t.shift) - t.page_size) << 32) / t.page_size) + 1);
+}
+__device__ inline int page_of(const PageTable &t, int entry) {
+  return static_cast<int>((__umulhi(static_cast<unsigned>(entry), t.magic) + static_cast<unsigned>(entry)) >> t.shift);
+}
+struct RopeArgs {
+  RopeRows rows[2];                 // rows[1].heads may be 0
+  int32_t n_seqs, n_tokens;
+  int32_t layout, half;             // pairs of a head that are turned (0: none)
+  float eps;
+  const float *inv_freq;
+  const int32_t *positions;         // [n_seqs][n_tokens] or null
+  int64_t start;                    // position of token 0, or what is added to `positions`
+  PageTable pages;                  // of the results, ...
+  int32_t first_entry;              // ... from this entry on
+};
+hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
+
+// Attention over pages (see lazyev_pages_attend).
+struct AttendArgs {
+  int32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
+  int32_t head_dim, dtype;
+  int32_t length;
+  const int32_t *visible;
+  float scale;
+  const void *q, *k_pages, *v_pages;
+  PageTable pages;
+  const void *joined_out;
+  const float *joined_lse;
+  // the same part from a decode call: [n_tokens * n_kv_heads][8][2] largest logit and 1 / sum, made those over both
+  float *joined_stat;
+  Slots slots;                      // with joined_stat: sequences (tokens) that take no part at step t are left alone
+  int32_t t;
+  void *out;
+  float *lse;
+  void *workspace;
+};
+size_t attend_workspace(const AttendArgs &a);
+hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);
+
 // `ev`, when not null, points at three events recorded before the first kernel, between the two
 // kernels and after the second (per-kernel timing for the profiling aid).
 hipError_t launch_decode(const DecodeArgs &a, hipStream_t stream, hipEvent_t *ev);

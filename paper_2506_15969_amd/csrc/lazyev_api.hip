@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "pages_api.h"
 
 namespace lazyev {
 int decode_chunk_max();
@@ -489,8 +490,11 @@ int lazyev_set_variant(lazyev_ctx *ctx, int32_t variant) {
   return LAZYEV_OK;
 }
 
-int lazyev_decode_step(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q, const void *k_new,
-                       const void *v_new, void *out, float *p_out, const float *p_override) {
+}  // extern "C"
+
+// shared: the attention over a prefix that the call is joined with (null: none).
+static int decode_step(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q, const void *k_new, const void *v_new, void *out,
+                       lazyev::AttendArgs *shared, float *p_out, const float *p_override) {
   if (!ctx || !q || !k_new || !v_new || !out) return LAZYEV_EINVAL;
   const lazyev_config &c = ctx->cfg;
   if (layer < 0 || layer >= c.n_layers) return LAZYEV_EINVAL;
@@ -647,12 +651,43 @@ int lazyev_decode_step(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q,
     k.activation_counter = a.activation_counter;
     k.slots = a.slots;
     ctx->cur_buf ^= 1;
+    if (shared) {                                  // `out` and the statistics that the tracking reads become those over both
+      shared->joined_out = out; shared->joined_stat = a.stat_out;
+      shared->q = q; shared->out = out;
+      shared->scale = ctx->scale;
+      shared->slots = a.slots; shared->t = t;
+      const hipError_t es = lazyev::launch_attend(*shared, ctx->stream);
+      if (es != hipSuccess) return fail_hip(ctx, es);
+    }
     if (p_out || p_override) {                     // the caller looks at the weights now
       const hipError_t ef = flush_tracking(ctx);
       if (ef != hipSuccess) return fail_hip(ctx, ef);
     }
   }
   return LAZYEV_OK;
+}
+
+extern "C" {
+
+int lazyev_decode_step(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q, const void *k_new, const void *v_new, void *out,
+                       float *p_out, const float *p_override) {
+  return decode_step(ctx, layer, t, q, k_new, v_new, out, nullptr, p_out, p_override);
+}
+
+int lazyev_decode_step_shared(lazyev_ctx *ctx, int32_t layer, int32_t t, const void *q, const void *k_new, const void *v_new, void *out,
+                              const lazyev_pages *prefix, int32_t prefix_len, void *workspace, size_t workspace_bytes,
+                              float *p_out, const float *p_override) {
+  if (!ctx || !prefix || (q && q == out)) return LAZYEV_EINVAL;
+  const lazyev_config &c = ctx->cfg;
+  lazyev::AttendArgs a;
+  if (prefix->n_seqs != 1 || prefix->n_kv_heads != c.n_kv_heads || prefix->head_dim != c.head_dim || prefix->dtype != c.dtype ||
+      ctx->variant == 0 || !lazyev::attend_args(prefix, prefix_len, c.batch, c.n_q_heads, &a))
+    return LAZYEV_EINVAL;
+  if (prefix_len == 0) return decode_step(ctx, layer, t, q, k_new, v_new, out, nullptr, p_out, p_override);
+  const size_t need = lazyev::attend_workspace(a);
+  if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)) return LAZYEV_EWORKSPACE;
+  a.workspace = workspace;
+  return decode_step(ctx, layer, t, q, k_new, v_new, out, &a, p_out, p_override);
 }
 
 }  // extern "C"

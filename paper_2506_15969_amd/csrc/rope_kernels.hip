@@ -1,0 +1,212 @@
+// Norms of heads and their rotation by the token's position, in one pass over the rows, from any places to any
+// places or into the pages of a cache (where the values go along as they are).
+//
+//   n = x / sqrt(mean(x^2) + eps) * w;   (n_a, n_b) -> (n_a cos - n_b sin, n_b cos + n_a sin), angle = position * inv_freq
+//
+// A head is L lanes of 16 bytes; the sum of squares is joined over the L lanes and the partner of an element that is
+// turned with the other half's comes from its lane by a permutation, all on fp32 values that never leave the registers.
+// A block takes kTokens tokens (one, where that gives too few blocks) and a share of their heads.  The angle's sine and
+// cosine are the same for all heads of a token: each is worked out once in the block, one pair per thread, and kept in LDS.  The
+// angle is needed modulo a turn only: the product position * inv_freq / 2 pi in binary64 has 2^-52 of itself as its error,
+// so that its fraction is good to 1e-9 at positions of millions, where an fp32 angle is off by a tenth of a turn.
+#include "kernels.h"
+#include "lazyev.h"
+
+#include <type_traits>
+
+namespace lazyev {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / 64;
+typedef unsigned short bf16_t;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+
+// 16 bytes of a row and its elements as fp32.
+template <typename T>
+struct Chunk {
+  static constexpr int kElems = 16 / static_cast<int>(sizeof(T));
+  __device__ static void open(const u32x4_t &w, float (&x)[kElems]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4) {
+        x[e] = __uint_as_float(w[e]);
+      } else {
+        x[2 * e] = __uint_as_float(w[e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+      }
+    }
+  }
+  __device__ static u32x4_t close(const float (&x)[kElems]) {
+    u32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(x[e]);
+      else w[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2_t{x[2 * e], x[2 * e + 1]}, bf16x2_t));
+    }
+    return w;
+  }
+};
+
+// kVec: every row starts at a multiple of 16 bytes.
+template <typename T, bool kVec>
+__device__ __forceinline__ u32x4_t load_chunk(const T *p) {
+  if constexpr (kVec) return *reinterpret_cast<const u32x4_t *>(p);
+  T e[16 / sizeof(T)];
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(16 / sizeof(T)); ++i) e[i] = p[i];
+  u32x4_t w;
+  __builtin_memcpy(&w, e, 16);
+  return w;
+}
+template <typename T, bool kVec>
+__device__ __forceinline__ void store_chunk(T *p, const u32x4_t &w) {
+  if constexpr (kVec) {
+    *reinterpret_cast<u32x4_t *>(p) = w;
+    return;
+  }
+  T e[16 / sizeof(T)];
+  __builtin_memcpy(e, &w, 16);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(16 / sizeof(T)); ++i) p[i] = e[i];
+}
+
+// grid: x = spans of kTokens tokens (of all sequences in a row), y = shares of their heads
+template <typename T, int D, int kTokens, bool kVec>
+__global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
+  constexpr int E = Chunk<T>::kElems, L = D / E, kRows = 64 / L;   // elements and lanes of a chunk / a head, heads of a wave
+  constexpr int kWavesPerToken = kWaves / kTokens;
+  __shared__ float2 turn[kTokens][D / 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
+  const long long token0 = static_cast<long long>(blockIdx.x) * kTokens;
+  if (a.half > 0) {
+    for (int x = threadIdx.x; x < kTokens * a.half; x += kBlock) {
+      const int j = x % a.half, k = x / a.half;
+      const long long tk = token0 + k;
+      if (tk >= tokens) break;
+      const long long p = a.start + (a.positions ? a.positions[tk] : static_cast<int>(tk % a.n_tokens));
+      constexpr double kPerTurn = 0.15915494309189533576888;
+      const double turns = static_cast<double>(p) * static_cast<double>(a.inv_freq[j]) * kPerTurn;
+      float s, c;
+      sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
+      turn[k][j] = make_float2(c, s);
+    }
+    __syncthreads();
+  }
+  const int my_k = kTokens == 1 ? 0 : wave / kWavesPerToken;
+  const long long tk = token0 + my_k;
+  if (tk >= tokens) return;
+  const int seq = static_cast<int>(tk / a.n_tokens), token = static_cast<int>(tk % a.n_tokens);
+  // where the token's rows go in the pages
+  long long page_row = 0;
+  if (a.pages.table) {
+    const int entry = a.first_entry + token, pg = page_of(a.pages, entry);
+    const int page = a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg];
+    if (page < 0 || page >= a.pages.n_pages) return;
+    page_row = static_cast<long long>(page) * a.rows[0].heads * a.pages.page_size + (entry - pg * a.pages.page_size);
+  }
+  const int li = lane % L, e0 = li * E;            // this lane's elements of a head: e0 .. e0 + E - 1
+  const bool halves = a.layout == LAZYEV_ROPE_HALVES;
+  const bool turned = e0 < 2 * a.half;
+  float cs[E], sn[E];                              // (pairs: of the first E / 2 places)
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int j = halves ? e0 % (a.half > 0 ? a.half : 1) + e : e0 / 2 + e / 2;
+    const float2 cv = turned ? turn[my_k][j] : make_float2(1.f, 0.f);
+    cs[e] = cv.x;
+    sn[e] = (halves ? e0 < a.half : e % 2 == 0) ? -cv.y : cv.y;
+  }
+  const int partner = halves && turned ? (e0 < a.half ? lane + a.half / E : lane - a.half / E) : lane;
+  float w[2][E];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (a.rows[s].weight) Chunk<T>::open(load_chunk<T, kVec>(static_cast<const T *>(a.rows[s].weight) + e0), w[s]);
+    else
+#pragma unroll
+      for (int e = 0; e < E; ++e) w[s][e] = 1.f;
+  }
+  const int n0 = a.rows[0].heads, n = n0 + a.rows[1].heads;
+  const int step = kRows * kWavesPerToken * static_cast<int>(gridDim.y);
+  for (int h0 = (static_cast<int>(blockIdx.y) * kWavesPerToken + wave % kWavesPerToken) * kRows; h0 < n; h0 += step) {
+    const int at = h0 + lane / L;
+    const bool have = at < n;                      // (lanes without a head work on the last one and leave nothing)
+    const int which = min(at, n - 1) >= n0 ? 1 : 0, h = min(at, n - 1) - (which ? n0 : 0);
+    const RopeRows &r = a.rows[which];
+    const u32x4_t raw = load_chunk<T, kVec>(static_cast<const T *>(r.in) + seq * r.in_seq + token * r.in_token + h * r.in_head + e0);
+    float x[E];
+    Chunk<T>::open(raw, x);
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
+    const float inv = r.weight ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = x[e] * inv * (which ? w[1][e] : w[0][e]);
+    float y[E];
+    if (halves) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = __shfl(x[e], partner);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = x[e ^ 1];
+    }
+    const bool turns = turned && r.turn;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = turns ? fmaf(y[e], sn[e], x[e] * cs[e]) : x[e];
+    if (!have) continue;
+    T *to = static_cast<T *>(r.out);
+    to += a.pages.table ? (page_row + static_cast<long long>(h) * a.pages.page_size) * D : seq * r.out_seq + token * r.out_token + h * r.out_head;
+    store_chunk<T, kVec>(to + e0, r.turn || r.weight ? Chunk<T>::close(x) : raw);
+  }
+}
+
+template <typename T, int D, bool kVec>
+hipError_t launch(const RopeArgs &a, hipStream_t stream) {
+  constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
+  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
+  const int heads = a.rows[0].heads + a.rows[1].heads;
+  // Four tokens a block share nothing but the block; a single one with its heads dealt to more blocks where
+  // that would leave the chip's 256 compute units without eight blocks each
+  if (tokens >= 4 * 2048) {
+    hipLaunchKernelGGL((rope_kernel<T, D, 4, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
+  } else {
+    const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
+    const int want = static_cast<int>((2048 + tokens - 1) / tokens);
+    hipLaunchKernelGGL((rope_kernel<T, D, 1, kVec>), dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(shares < want ? shares : want)),
+                       dim3(kBlock), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_any(const RopeArgs &a, hipStream_t stream) {
+  // 16 bytes at a time where every row starts at a multiple of 16 bytes
+  uintptr_t low = 0;
+  for (const RopeRows &r : a.rows) {
+    if (r.heads == 0) continue;
+    low |= reinterpret_cast<uintptr_t>(r.in) | reinterpret_cast<uintptr_t>(r.out) | reinterpret_cast<uintptr_t>(r.weight);
+    low |= static_cast<uintptr_t>(r.in_seq | r.in_token | r.in_head) * sizeof(T);
+    if (!a.pages.table) low |= static_cast<uintptr_t>(r.out_seq | r.out_token | r.out_head) * sizeof(T);
+  }
+  return low % 16 == 0 ? launch<T, D, true>(a, stream) : launch<T, D, false>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream) {
+  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
+  if (tokens < 1 || tokens > 0x7FFFFFFFLL || a.rows[0].heads < 1 || a.rows[1].heads < 0 || a.half < 0 || a.half > head_dim / 2 || a.half % 8 != 0 ||
+      (a.half > 0 && !a.inv_freq) || (a.pages.table && a.rows[1].heads != 0 && a.rows[1].heads != a.rows[0].heads))
+    return hipErrorInvalidValue;
+  if (dtype == LAZYEV_DTYPE_FP32 && head_dim == 64) return launch_any<float, 64>(a, stream);
+  if (dtype == LAZYEV_DTYPE_FP32 && head_dim == 128) return launch_any<float, 128>(a, stream);
+  if (dtype == LAZYEV_DTYPE_BF16 && head_dim == 64) return launch_any<bf16_t, 64>(a, stream);
+  if (dtype == LAZYEV_DTYPE_BF16 && head_dim == 128) return launch_any<bf16_t, 128>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace lazyev
