@@ -252,6 +252,9 @@ struct AttendArgs {
   void *out;
   float *lse;
   void *workspace;
+  // filled in by the launch: splits of the entries and what they leave in the workspace; all rows at multiples of 16 bytes
+  int32_t n_split, split_keys, wide;
+  float *part_o, *part_ml, *part_lse;
 };
 size_t attend_workspace(const AttendArgs &a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);

@@ -1,34 +1,92 @@
-// Attention of tokens that share a context over its pages (lazyev_pages_attend).  One wave per row (token and query
-// head): every group of L lanes takes every 64 / L-th entry with a running maximum and sum; the groups are joined at the end.
+// Attention of tokens that share a context over its pages (lazyev_pages_attend): the rows of a unit (table row and KV
+// head) are its tokens' query heads, token by token, and every row goes over the same entries.
+//
+// A wave keeps 32 rows: their queries, their output O^T (fp32) and, per row, a reference m and the sum l of the weights
+// relative to it, exp2(s log2 e - m).  Entries come in stages of kKeys, fetched straight into LDS by the whole block while the
+// stage before is worked on, a page number one stage further ahead.  Of a stage each of the kWK waves that share 32
+// rows takes its own kKeys / kWK entries, 32 at a time:
+//   S^T = K Q^T    v_mfma_f32_32x32x16_bf16 (fp32 rows: 32x32x2_f32): lane (c, h) = (l % 32, l / 32) holds, of row c, the
+//                  logits of the entries 8 i + 4 h + j (i, j < 4)
+//   P = exp2(S)    in place; rounded to bf16 for the product with bf16 values (half a step, 2^-8, of each weight, in place of
+//                  two products; the sum l is that of the weights before, as it also is a result of its own)
+//   O^T += V^T P^T lane (c, h) already holds 8 entries of row c, in an order that the products take from V as well: V
+//                  is read transposed (ds_read_b64_tr_b16), 4 entries of 16 columns to 16 lanes
+// The reference is raised only when a sum of 16 weights relative to it exceeds 2^12 (never rescaled otherwise): a sum
+// is as exact relative to any reference in the range of fp32.  Every decision that changes a row's arithmetic
+// is taken for that row alone: what other rows see has no influence on it.
+// Entries that some row of the wave does not see (or that lead to no page) are masked to weight zero, and V is then
+// multiplied with its infinities and NaN taken out; these are brought in by products of their own, with 1 in their places, whose
+// sums are positive where a row sees one.
+//
+// Few rows: the entries are also cut into splits, which leave (m, l, O) in the workspace for a second kernel.
 #include "kernels.h"
 #include "lazyev.h"
+
+#include <cfloat>
+#include <type_traits>
 
 namespace lazyev {
 namespace {
 
-constexpr int kBlock = 256;
 typedef unsigned short bf16_t;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(bf16_t x) { return __uint_as_float(static_cast<unsigned>(x) << 16); }
-__device__ __forceinline__ void put(float *p, float x) { *p = x; }
-__device__ __forceinline__ void put(bf16_t *p, float x) { *p = __builtin_bit_cast(bf16_t, static_cast<__bf16>(x)); }
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFar = 0x1p12f;         // a sum of weights beyond this raises the reference
+constexpr float kHuge = 0x1p24f;        // of references beyond this the rounding exceeds 1 (see exponent_of)
+constexpr int kSplitMax = 256;
 
-// What a row found in the pages (largest logit m, sum l relative to it; l = 0: nothing) and elsewhere: the shares of
-// both in the output, the pages' one already divided by l, and the log-sum-exp over both.
+template <typename T, int D>
+struct Rows {
+  static constexpr bool kF32 = sizeof(T) == 4;
+  static constexpr int kChunks = D * static_cast<int>(sizeof(T)) / 16;   // 16-byte chunks of a row
+  static constexpr int kOps = kChunks / 2;         // chunks of a row that a lane holds as an operand
+  static constexpr int kTiles = D / 32;            // output tiles of 32 columns
+  // Where chunk x of entry r of a stage lies among the entry's chunks: keys are read by 16 entries at a time, one chunk of
+  // each; values by 4 (bf16) entries, 64 bytes of each, or (fp32) an entry and the one four further, 128 bytes of each.
+  __device__ static int k_slot(int r, int x) { return x ^ (kChunks == 8 ? (r >> 1) & 7 : r & 15); }
+  __device__ static int v_slot(int r, int x) { return x ^ (kF32 ? ((r >> 2) & 1) * 8 : kChunks == 8 ? ((r >> 1) & 1) * 4 : (r & 3) * 4); }
+};
+
+__device__ __forceinline__ unsigned pair_to_bf16(float lo, float hi) {
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
+}
+__device__ __forceinline__ float bf16_low(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// x of lane ^ 32 joined with x
+__device__ __forceinline__ float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// What a row found in the pages (reference m in units of log 2, sum l relative to it; l = 0: nothing) and elsewhere:
+// the factors of the pages' unnormalised output and of the other one, and the log-sum-exp over both.
 struct Joined { float pages, other, lse; };
-__device__ __forceinline__ Joined join(float m, float l, bool other, float lse_other) {
-  const float lse = l > 0.f || l != l ? m + logf(l) : -INFINITY;
+__device__ __forceinline__ Joined join(float m, float l, float lse_other) {
+  const bool some = !(l <= 0.f);                   // (a NaN is something)
+  const float lse = some ? fmaf(m, kLn2, logf(l)) : -INFINITY;
   Joined j;
-  if (!other || lse_other == -INFINITY) {
-    j.pages = l > 0.f || l != l ? 1.f / l : 0.f;
+  if (lse_other == -INFINITY) {
+    j.pages = some ? 1.f / l : 0.f;
     j.other = 0.f;
     j.lse = lse;
     return j;
   }
   const float top = fmaxf(lse, lse_other);
   const float a = expf(lse - top), b = expf(lse_other - top);
-  j.pages = l > 0.f || l != l ? a / ((a + b) * l) : 0.f;
+  j.pages = some ? a / ((a + b) * l) : 0.f;
   j.other = b / (a + b);
   j.lse = top + logf(a + b);
   return j;
@@ -39,78 +97,616 @@ __device__ __forceinline__ bool takes_part(const AttendArgs &a, int token) {
   return a.slots.prompt_len[token] >= 0 && a.t - a.slots.t0[token] >= 1;
 }
 
+// A row as the caller sees it.
+struct RowPlace {
+  int token;                        // of all sequences
+  int head, kvh;                    // head: within the KV head's group
+  long long row;                    // token * n_q_heads + query head
+};
+__device__ __forceinline__ RowPlace row_place(const AttendArgs &a, int unit, int r) {
+  RowPlace p;
+  const int seq = unit / a.n_kv_heads, i = r / a.group;
+  p.kvh = unit % a.n_kv_heads;
+  p.head = r - i * a.group;
+  p.token = seq * a.n_tokens + i;
+  p.row = static_cast<long long>(p.token) * a.n_q_heads + p.kvh * a.group + p.head;
+  return p;
+}
+
+// Four output elements of a row (columns e0 .. e0 + 3) joined with the other part and stored.
 template <typename T, int D>
-__global__ __launch_bounds__(kBlock) void attend_kernel(const AttendArgs a) {
-  constexpr int E = 16 / static_cast<int>(sizeof(T)), L = D / E, kGroups = 64 / L;
-  const int lane = threadIdx.x & 63;
-  const long long row = static_cast<long long>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-  if (row >= static_cast<long long>(a.n_seqs) * a.n_tokens * a.n_q_heads) return;
-  const long long tk = row / a.n_q_heads;
-  const int head = static_cast<int>(row % a.n_q_heads), kvh = head / a.group, seq = static_cast<int>(tk / a.n_tokens);
-  if (!takes_part(a, static_cast<int>(tk))) return;
-  const int seen = a.visible ? min(max(a.visible[tk], 0), a.length) : a.length;
-  const int e0 = lane % L * E;
-  float q[E], acc[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = to_float(static_cast<const T *>(a.q)[row * D + e0 + e]);
-    acc[e] = 0.f;
-  }
-  for (int i = lane / L; i < seen; i += kGroups) {
-    const int pg = page_of(a.pages, i), page = a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg];
-    if (page < 0 || page >= a.pages.n_pages) continue;
-    const long long at = ((static_cast<long long>(page) * a.n_kv_heads + kvh) * a.pages.page_size + (i - pg * a.pages.page_size)) * D + e0;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s = fmaf(q[e], to_float(static_cast<const T *>(a.k_pages)[at + e]), s);
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o);
-    s *= a.scale;
-    const float up = s > m ? s : m, keep = m == up ? 1.f : expf(m - up), p = expf(s - up);
-    m = up;
-    l = l * keep + p;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(p, to_float(static_cast<const T *>(a.v_pages)[at + e]), acc[e] * keep);
-  }
-#pragma unroll
-  for (int o = L; o < 64; o <<= 1) {
-    const float mo = __shfl_xor(m, o), lo = __shfl_xor(l, o), up = fmaxf(m, mo);
-    const float x = m == up ? 1.f : expf(m - up), y = mo == up ? 1.f : expf(mo - up);
-    m = up;
-    l = l * x + lo * y;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] * x + __shfl_xor(acc[e], o) * y;
-  }
-  const bool other = a.joined_stat || a.joined_lse;
-  float lse_other = 0.f;
-  float *stat = a.joined_stat ? a.joined_stat + (tk * a.n_kv_heads + kvh) * 16 + 2 * (head % a.group) : nullptr;
-  if (stat) lse_other = stat[0] - logf(stat[1]);
-  else if (other) lse_other = a.joined_lse[row];
-  const Joined j = join(m, l, other, lse_other);
-  if (lane < L) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float x = acc[e] * j.pages;
-      if (other && j.other != 0.f) x = fmaf(j.other, to_float(static_cast<const T *>(a.joined_out)[row * D + e0 + e]), x);
-      put(static_cast<T *>(a.out) + row * D + e0 + e, x);
+__device__ __forceinline__ void finish4(const AttendArgs &a, const RowPlace &p, int e0, f32x4_t o, const Joined &j) {
+  T *to = static_cast<T *>(a.out) + p.row * D + e0;
+  f32x4_t x = o * j.pages;
+  if (j.pages == 0.f) x = f32x4_t{0.f, 0.f, 0.f, 0.f};      // (whatever lies there when nothing was seen)
+  if (j.other != 0.f) {
+    const T *from = static_cast<const T *>(a.joined_out) + p.row * D + e0;
+    f32x4_t y;
+    if constexpr (sizeof(T) == 4) {
+      if (a.wide) y = *reinterpret_cast<const f32x4_t *>(from);
+      else y = f32x4_t{from[0], from[1], from[2], from[3]};
+    } else {
+      u32x2_t w;
+      if (a.wide) w = *reinterpret_cast<const u32x2_t *>(from);
+      else w = u32x2_t{from[0] | static_cast<unsigned>(from[1]) << 16, from[2] | static_cast<unsigned>(from[3]) << 16};
+      y = f32x4_t{bf16_low(w[0]), bf16_high(w[0]), bf16_low(w[1]), bf16_high(w[1])};
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(j.other, y[e], x[e]);
   }
-  if (lane == 0) {
-    if (a.lse) a.lse[row] = j.lse;
-    if (stat) stat[1] *= j.other;
+  if constexpr (sizeof(T) == 4) {
+    if (a.wide) *reinterpret_cast<f32x4_t *>(to) = x;
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[e] = x[e];
+  } else {
+    const u32x2_t w = {pair_to_bf16(x[0], x[1]), pair_to_bf16(x[2], x[3])};
+    if (a.wide) *reinterpret_cast<u32x2_t *>(to) = w;
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[e] = static_cast<bf16_t>(w[e / 2] >> (16 * (e % 2)));
   }
 }
 
+// Log-sum-exp of what the row is joined with (nothing: -inf).
+__device__ __forceinline__ float lse_joined(const AttendArgs &a, const RowPlace &p) {
+  if (a.joined_stat) {
+    const float *st = a.joined_stat + (static_cast<size_t>(p.token) * a.n_kv_heads + p.kvh) * 16 + 2 * p.head;
+    return st[0] - logf(st[1]);
+  }
+  return a.joined_lse ? a.joined_lse[p.row] : -INFINITY;
+}
+// Once for a row; both may be what lse_joined reads (of two kernels the first reads, the second writes).
+__device__ __forceinline__ void finish_row(const AttendArgs &a, const RowPlace &p, const Joined &j) {
+  if (a.lse) a.lse[p.row] = j.lse;
+  if (a.joined_stat) a.joined_stat[(static_cast<size_t>(p.token) * a.n_kv_heads + p.kvh) * 16 + 2 * p.head + 1] *= j.other;
+}
+
+// A weight's exponent relative to the reference m: a multiply-add is exact but for one rounding of its result; where m, which
+// is a rounded product itself, is so large that the difference of the two could leave the range, the product is rounded as well.
+__device__ __forceinline__ float exponent_of(float s, float c2, float m) {
+  float x = s * c2;
+  __asm__("" : "+v"(x));                           // (not fused)
+  return fabsf(m) > kHuge ? x - m : fmaf(s, c2, -m);
+}
+
+// The elements of an operand register of V that are finite, and 1 where they are of a kind (0 +inf, 1 -inf, 2 NaN).
+template <bool kF32>
+__device__ __forceinline__ unsigned finite_of(unsigned w) {
+  if (kF32) return (w & 0x7F800000u) == 0x7F800000u ? 0u : w;
+  const unsigned lo = (w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu, hi = (w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u;
+  return lo | hi;
+}
+__device__ __forceinline__ bool of_kind(unsigned bits32, int kind) {   // an fp32 number's bits
+  return kind == 2 ? (bits32 & 0x7FFFFFFFu) > 0x7F800000u : bits32 == (kind == 0 ? 0x7F800000u : 0xFF800000u);
+}
+template <bool kF32>
+__device__ __forceinline__ unsigned kind_of(unsigned w, int kind) {
+  if (kF32) return of_kind(w, kind) ? 0x3F800000u : 0u;
+  return (of_kind(w << 16, kind) ? 0x3F80u : 0u) | (of_kind(w & 0xFFFF0000u, kind) ? 0x3F800000u : 0u);
+}
+
+// kWR x kWK waves: kWR of 32 rows each, kWK that share the entries of a stage.
+template <typename T, int D, int kWR, int kWK, int kKeys>
+struct Shape {
+  using R = Rows<T, D>;
+  static constexpr int kWaves = kWR * kWK, kBlock = 64 * kWaves;
+  static constexpr int kSub = kKeys / kWK / 32;    // sub-tiles of 32 entries that a wave takes of a stage
+  static constexpr int kPerLoad = 64 / R::kChunks; // entries that a wave's load of 16 bytes a lane brings
+  static constexpr int kLoads = kKeys / (kPerLoad * kWaves);   // of K and of V each, per wave and stage
+  static_assert(kSub >= 1 && kLoads >= 1 && kLoads * kPerLoad * kWaves == kKeys, "whole loads");
+  static constexpr int kPerSimd = D * sizeof(T) == 512 ? 1 : 2;   // (fp32 rows of 128: queries and output take 128 registers, the products' operands more)
+  static constexpr int kStageBytes = kKeys * D * static_cast<int>(sizeof(T));   // of K; of V as many
+  static_assert((kWK - 1) * kWR * 32 * D * 4 <= 2 * kStageBytes, "the waves' outputs fit where two stages of K were");
+};
+
+template <typename T, int D, int kWR, int kWK, int kKeys>
+__global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPerSimd)) void attend_kernel(const AttendArgs a) {
+  using R = Rows<T, D>;
+  using S = Shape<T, D, kWR, kWK, kKeys>;
+  constexpr int kSub = S::kSub, kOps = R::kOps, kTiles = R::kTiles, C = R::kChunks;
+  __shared__ __align__(16) char k_even[S::kStageBytes];
+  __shared__ __align__(16) char k_odd[S::kStageBytes];
+  __shared__ __align__(16) char v_even[S::kStageBytes];
+  __shared__ __align__(16) char v_odd[S::kStageBytes];
+  __shared__ int shared_end[2];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, h = lane >> 5;
+  const int wr = wave % kWR, wk = wave / kWR;
+  const int units = a.n_seqs * a.n_kv_heads, M = a.n_tokens * a.group;
+  // late rows first: where a token sees its past only, they have the most to do
+  const int spans = (M + 32 * kWR - 1) / (32 * kWR);
+  const int b = static_cast<int>(blockIdx.x);
+  const int unit = b % units, split = b / units % a.n_split, span = spans - 1 - b / units / a.n_split;
+  const int seq = unit / a.n_kv_heads, kvh = unit % a.n_kv_heads;
+  const int r0 = (span * kWR + wr) * 32;           // this wave's rows
+  const bool have = r0 < M;
+  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+
+  // entries of this block: first .. end - 1; what its rows see of them
+  const int first = split * a.split_keys, last = min(first + a.split_keys, a.length);
+  int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
+  if (!have) seen = 0;
+  int most = seen, least = seen;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    most = max(most, __shfl_xor(most, o));
+    least = min(least, __shfl_xor(least, o));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+  if (threadIdx.x < 2) shared_end[threadIdx.x] = 0;
+  __syncthreads();
+  if (lane == 0) atomicMax(&shared_end[0], most);
+  __syncthreads();
+  const int end = __builtin_amdgcn_readfirstlane(min(last, shared_end[0]));
+  const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
+  bool holes = false;                              // pages that are none among the block's
+  if (n_stages > 0) {
+    int bad = 0;
+    for (int i = page_of(a.pages, first) + threadIdx.x; i <= page_of(a.pages, end - 1); i += S::kBlock)
+      bad |= static_cast<unsigned>(table[i]) >= static_cast<unsigned>(a.pages.n_pages) ? 1 : 0;
+    if (bad) shared_end[1] = 1;
+  }
+
+  u32x4_t qb[kOps];
+  {
+    const T *q = static_cast<const T *>(a.q) + place.row * D + h * (16 / sizeof(T));
+    if (a.wide) {
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) qb[j] = *reinterpret_cast<const u32x4_t *>(q + j * (32 / sizeof(T)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        T e[16 / sizeof(T)];
+#pragma unroll
+        for (int x = 0; x < static_cast<int>(16 / sizeof(T)); ++x) e[x] = q[j * (32 / sizeof(T)) + x];
+        __builtin_memcpy(&qb[j], e, 16);
+      }
+    }
+  }
+
+  // ---- stages on their way to LDS
+  const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
+  int page[S::kLoads];
+  unsigned within[S::kLoads];                      // the entry's row in its page
+  auto look_up = [&](int st) {
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+      const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
+      const int entry = min(first + st * kKeys + r, end - 1);
+      const int pg = page_of(a.pages, entry);
+      within[u] = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+      page[u] = table[pg];
+    }
+  };
+  auto fetch = [&](char *k_to, char *v_to) {
+    typedef const __attribute__((address_space(1))) void *from_t;
+    typedef __attribute__((address_space(3))) void *to_t;
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+      const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
+      // (no page: any row; its entries are masked)
+      const unsigned pg = static_cast<unsigned>(page[u]) < static_cast<unsigned>(a.pages.n_pages) ? page[u] : 0u;
+      const size_t row = static_cast<size_t>(pg * page_rows + within[u]) * (D * sizeof(T));
+      const int at = (u * S::kWaves + wave) * 1024;
+      __builtin_amdgcn_global_load_lds((from_t)(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16), (to_t)(k_to + at), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((from_t)(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16), (to_t)(v_to + at), 16, 0, 0);
+    }
+  };
+
+  const float c2 = a.scale * kLog2e;
+  f32x16_t o[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[t][x] = 0.f;
+  float m = -FLT_MAX, l = 0.f;                     // l: over this lane's entries
+  bool plain = true;                               // (of the wave) no reference beyond kHuge
+
+  // Where this lane's operands lie in a stage: of K chunk 2 j + h of entry c of a sub-tile, of V the first entry's part of the
+  // columns 32 t ..  All other entries lie at fixed distances (the places among an entry's chunks repeat).
+  int k_at[kOps], v_at[kTiles];
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) k_at[j] = (c * C + R::k_slot(c, 2 * j + h)) * 16;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const int r = R::kF32 ? 4 * h : 4 * h + (lane & 15) / 4, at = (R::kF32 ? 32 * t + c : 32 * t + (lane & 16) + (lane & 3) * 4) * static_cast<int>(sizeof(T));
+    v_at[t] = (r * C + R::v_slot(r, at / 16)) * 16 + at % 16;
+  }
+  constexpr int kEntry = C * 16;                   // bytes of an entry
+
+  // one sub-tile's logits
+  auto logits = [&](const char *ks, int e0, f32x16_t &s) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) {
+      const u32x4_t ka = *reinterpret_cast<const u32x4_t *>(ks + k_at[j] + e0 * kEntry);
+      if constexpr (R::kF32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[e]), __uint_as_float(qb[j][e]), s, 0, 0, 0);
+      } else {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ka), __builtin_bit_cast(bf16x8_t, qb[j]), s, 0, 0, 0);
+      }
+    }
+  };
+  // The operand of V for a product: columns 32 t .., bf16: entries 16 g .. 16 g + 15 of the sub-tile; fp32: the entries
+  // 8 i + 4 h + j with 4 i + j = g.
+  auto values = [&](const char *vs, int e0, int t, int g) {
+    if constexpr (R::kF32) {
+      return *reinterpret_cast<const unsigned *>(vs + v_at[t] + (e0 + 8 * (g / 4) + g % 4) * kEntry);
+    } else {
+      typedef __attribute__((address_space(3))) s16x4_t *at_t;
+      u32x4_t w;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_t)(vs + v_at[t] + (e0 + 16 * g + 8 * u) * kEntry));
+        const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+        w[2 * u] = y[0];
+        w[2 * u + 1] = y[1];
+      }
+      return w;
+    }
+  };
+  constexpr int kProducts = R::kF32 ? 16 : 2;      // of a sub-tile and a tile of columns
+  using Weights = std::conditional_t<R::kF32, f32x16_t, u32x4_t[2]>;
+  auto product = [&](auto v, const Weights &p, int g, f32x16_t &to) {
+    if constexpr (R::kF32) to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), p[g], to, 0, 0, 0);
+    else to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, p[g]), to, 0, 0, 0);
+  };
+  auto weights_of = [&](const f32x16_t &s, Weights &p, auto fast) {   // -> their sum
+    float w[16], sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) w[x] = __builtin_amdgcn_exp2f(decltype(fast)::value ? fmaf(s[x], c2, -m) : exponent_of(s[x], c2, m));
+#pragma unroll
+    for (int x = 0; x < 16; x += 4) sum += (w[x] + w[x + 1]) + (w[x + 2] + w[x + 3]);
+    if constexpr (R::kF32) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) p[x] = w[x];
+    } else {
+#pragma unroll
+      for (int x = 0; x < 16; x += 2) p[x / 8][x % 8 / 2] = pair_to_bf16(w[x], w[x + 1]);
+    }
+    return sum;
+  };
+  auto weights = [&](const f32x16_t (&s)[kSub], Weights (&p)[kSub]) {
+    float sum = 0.f;
+    if (plain) {                                   // (wave-uniform)
+#pragma unroll
+      for (int x = 0; x < kSub; ++x) sum += weights_of(s[x], p[x], std::true_type{});
+    } else {
+#pragma unroll
+      for (int x = 0; x < kSub; ++x) sum += weights_of(s[x], p[x], std::false_type{});
+    }
+    return sum;
+  };
+
+  auto work = [&](const char *ks, const char *vs, int st) {
+    const int key0 = first + st * kKeys + wk * (32 * kSub);   // this wave's entries
+    ks += wk * (32 * kSub * kEntry);
+    vs += wk * (32 * kSub * kEntry);
+    if (key0 >= most) return;                      // (wave-uniform) nobody sees them
+    f32x16_t s[kSub];
+    Weights p[kSub];
+#pragma unroll
+    for (int x = 0; x < kSub; ++x) logits(ks, 32 * x, s[x]);
+    const bool mask = holes || key0 + 32 * kSub > min(least, last);
+    if (mask) {
+      const int limit = min(seen, last) - key0 - 4 * h;
+      unsigned there[kSub];                        // bit i: the entry is on a page
+#pragma unroll
+      for (int x = 0; x < kSub; ++x) there[x] = 0xFFFFu;
+      if (holes) {
+#pragma unroll
+        for (int x = 0; x < kSub; ++x)
+#pragma unroll 1
+          for (int i = 0; i < 16; ++i) {
+            const int key = min(key0 + 32 * x + 8 * (i / 4) + 4 * h + i % 4, end - 1);
+            if (static_cast<unsigned>(table[page_of(a.pages, key)]) >= static_cast<unsigned>(a.pages.n_pages)) there[x] &= ~(1u << i);
+          }
+      }
+#pragma unroll
+      for (int x = 0; x < kSub; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[x][i] = 32 * x + 8 * (i / 4) + i % 4 < limit && (there[x] >> i & 1u) != 0 ? s[x][i] : -INFINITY;
+    }
+    float sum = weights(s, p);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > kFar) != 0, 0)) {
+      float top = s[0][0];
+#pragma unroll
+      for (int x = 0; x < kSub; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
+      const bool far = max_of_halves(sum) > kFar;  // (of this row)
+      const float up = far ? fmaxf(m, max_of_halves(top) * c2) : m;
+      const float keep = __builtin_amdgcn_exp2f(m - up);
+      m = up;
+      l = far ? l * keep : l;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[t][x] = far ? o[t][x] * keep : o[t][x];
+      plain = __builtin_amdgcn_ballot_w64(fabsf(m) > kHuge && m != -FLT_MAX) == 0;
+      sum = weights(s, p);
+    }
+    l += sum;
+    if (!mask) {
+#pragma unroll
+      for (int x = 0; x < kSub; ++x)
+#pragma unroll
+        for (int g = 0; g < kProducts; ++g)
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) product(values(vs, 32 * x, t, g), p[x], g, o[t]);
+      return;
+    }
+    bool odd = false;                              // infinities or NaN among the values
+#pragma unroll
+    for (int x = 0; x < kSub; ++x)
+#pragma unroll
+      for (int g = 0; g < kProducts; ++g)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          auto v = values(vs, 32 * x, t, g);
+          if constexpr (R::kF32) {
+            const unsigned f = finite_of<true>(v);
+            odd = odd || f != v;
+            v = f;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned f = finite_of<false>(v[e]);
+              odd = odd || f != v[e];
+              v[e] = f;
+            }
+          }
+          product(v, p[x], g, o[t]);
+        }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          f32x16_t n;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) n[x] = 0.f;
+#pragma unroll
+          for (int x = 0; x < kSub; ++x)
+#pragma unroll
+            for (int g = 0; g < kProducts; ++g) {
+              auto v = values(vs, 32 * x, t, g);
+              if constexpr (R::kF32) v = kind_of<true>(v, kind);
+              else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = kind_of<false>(v[e], kind);
+              product(v, p[x], g, n);
+            }
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[t][x] = n[x] > 0.f ? o[t][x] + what : o[t][x];
+        }
+      }
+    }
+  };
+
+  if (n_stages > 0) {
+    look_up(0);
+    fetch(k_even, v_even);
+    look_up(min(1, n_stages - 1));
+    __syncthreads();                               // stage 0 is complete
+    holes = __builtin_amdgcn_readfirstlane(shared_end[1]) != 0;
+    int st = 0;
+    while (true) {
+      if (st + 1 < n_stages) {
+        fetch(k_odd, v_odd);
+        look_up(min(st + 2, n_stages - 1));
+      }
+      work(k_even, v_even, st);
+      __syncthreads();                             // the next stage is complete, this one no longer read
+      if (++st >= n_stages) break;
+      if (st + 1 < n_stages) {
+        fetch(k_even, v_even);
+        look_up(min(st + 2, n_stages - 1));
+      }
+      work(k_odd, v_odd, st);
+      __syncthreads();
+      if (++st >= n_stages) break;
+    }
+  }
+  l = sum_of_halves(l);
+
+  // ---- the waves that share rows -> the first of them
+  if constexpr (kWK > 1) {
+    // (where the stages were; every wave is past its last one)
+    auto at = [&](int which, int x) -> float & {   // register x of the wave's partial
+      const int i = ((which * kWR + wr) * (16 * kTiles) + x) * 64 + lane;
+      return (i < S::kStageBytes / 4) ? reinterpret_cast<float *>(k_even)[i] : reinterpret_cast<float *>(k_odd)[i - S::kStageBytes / 4];
+    };
+    float *ml = reinterpret_cast<float *>(v_even);
+    if (wk > 0) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) at(wk - 1, 16 * t + x) = o[t][x];
+      ml[(((wk - 1) * kWR + wr) * 2) * 64 + lane] = m;
+      ml[(((wk - 1) * kWR + wr) * 2 + 1) * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int w = 0; w < kWK - 1; ++w) {
+      const float mo = ml[((w * kWR + wr) * 2) * 64 + lane], lo = ml[((w * kWR + wr) * 2 + 1) * 64 + lane];
+      const float up = fmaxf(m, mo);
+      const float x0 = __builtin_amdgcn_exp2f(m - up), x1 = __builtin_amdgcn_exp2f(mo - up);
+      m = up;
+      l = l * x0 + lo * x1;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[t][x] = o[t][x] * x0 + at(w, 16 * t + x) * x1;
+    }
+  }
+  if (!have) return;
+
+  if (a.n_split > 1) {
+    // for the second kernel: [unit][32 rows][split][register / 4][lane] float4, and (m, l) of the rows
+    const int tiles = (M + 31) / 32;
+    const size_t p = (static_cast<size_t>(unit) * tiles + r0 / 32) * a.n_split + split;
+    f32x4_t *to = reinterpret_cast<f32x4_t *>(a.part_o) + p * (4 * kTiles * 64) + lane;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[(4 * t + i) * 64] = f32x4_t{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+    a.part_ml[p * 64 + lane] = h == 0 ? m : l;
+    if (split == 0 && h == 0) a.part_lse[static_cast<size_t>(unit) * (tiles * 32) + r0 + c] = lse_joined(a, place);
+    return;
+  }
+  if (r0 + c >= M || !takes_part(a, place.token)) return;
+  const Joined j = join(m, l, lse_joined(a, place));
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      finish4<T, D>(a, place, 32 * t + 8 * i + 4 * h, f32x4_t{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]}, j);
+  if (h == 0) finish_row(a, place, j);
+}
+
+// The splits of 32 rows joined: blocks = unit, 32 rows and 32 columns; four groups of 256 threads take every fourth split.
+constexpr int kMergeBlock = 1024;
 template <typename T, int D>
-hipError_t launch(const AttendArgs &a, hipStream_t stream) {
-  const long long rows = static_cast<long long>(a.n_seqs) * a.n_tokens * a.n_q_heads;
-  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(static_cast<unsigned>((rows + kBlock / 64 - 1) / (kBlock / 64))), dim3(kBlock), 0, stream, a);
+__global__ __launch_bounds__(kMergeBlock) void attend_merge_kernel(const AttendArgs a) {
+  constexpr int kTiles = D / 32, kGroups = 4, kBatch = 8;
+  __shared__ float ml[kSplitMax * 64];
+  __shared__ f32x4_t sums[kGroups - 1][256];
+  __shared__ float lsums[kGroups][32];
+  const int lane = threadIdx.x & 63, i = threadIdx.x >> 6 & 3, g = threadIdx.x >> 8;
+  const int c = lane & 31, h = lane >> 5;
+  const int M = a.n_tokens * a.group, tiles = (M + 31) / 32, n = a.n_split;
+  const int t = static_cast<int>(blockIdx.x) % kTiles, ut = static_cast<int>(blockIdx.x) / kTiles;
+  const int unit = ut / tiles, r0 = ut % tiles * 32;
+  const size_t p0 = static_cast<size_t>(ut) * n;
+  const f32x4_t *from = reinterpret_cast<const f32x4_t *>(a.part_o) + p0 * (4 * kTiles * 64) + (4 * t + i) * 64 + lane;
+  f32x4_t x[kBatch];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) x[k] = from[static_cast<size_t>(min(s0 + k * kGroups, n - 1)) * (4 * kTiles * 64)];
+  };
+  load(g);
+  const float lse_other = a.part_lse[static_cast<size_t>(ut) * 32 + c];
+  for (int k = threadIdx.x; k < n * 64; k += kMergeBlock) ml[k] = a.part_ml[p0 * 64 + k];
+  __syncthreads();
+  float m = -FLT_MAX;
+  for (int s = 0; s < n; ++s) m = fmaxf(m, ml[s * 64 + c]);
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int s0 = g; s0 < n; s0 += kBatch * kGroups) {
+    f32x4_t y[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) y[k] = x[k];
+    if (s0 + kBatch * kGroups < n) load(s0 + kBatch * kGroups);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int s = s0 + k * kGroups;
+      if (s >= n) break;
+      const float w = __builtin_amdgcn_exp2f(ml[s * 64 + c] - m);
+      l = fmaf(ml[s * 64 + 32 + c], w, l);
+      sum += y[k] * w;
+    }
+  }
+  if (i == 0 && h == 0) lsums[g][c] = l;
+  if (g > 0) sums[g - 1][threadIdx.x & 255] = sum;
+  __syncthreads();
+  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  if (g > 0 || r0 + c >= M || !takes_part(a, place.token)) return;
+#pragma unroll
+  for (int k = 0; k < kGroups - 1; ++k) sum += sums[k][threadIdx.x];
+  l = (lsums[0][c] + lsums[1][c]) + (lsums[2][c] + lsums[3][c]);
+  const Joined j = join(m, l, lse_other);
+  finish4<T, D>(a, place, 32 * t + 8 * i + 4 * h, sum, j);
+  if (t == 0 && i == 0 && h == 0) finish_row(a, place, j);
+}
+
+// How a call is cut: rows of a block, waves that share rows, entries of a stage, splits of the entries.
+struct Plan { int wr, wk, keys, n_split, split_keys; };
+
+template <typename T, int D>
+Plan plan_of(const AttendArgs &a) {
+  constexpr bool kLong = D * sizeof(T) == 512;     // (fewer entries a stage, and waves, than LDS and registers hold of other rows)
+  const long long M = static_cast<long long>(a.n_tokens) * a.group, units = static_cast<long long>(a.n_seqs) * a.n_kv_heads;
+  Plan p;
+  if (M <= 32) p = {1, kLong ? 2 : 4, kLong ? 64 : 128, 1, 0};
+  else if (M <= 64) p = {2, 2, 64, 1, 0};
+  else if (M <= 128 || kLong) p = {4, 1, 64, 1, 0};
+  else p = {8, 1, 64, 1, 0};
+  const long long blocks = units * ((M + 32 * p.wr - 1) / (32 * p.wr));
+  long long n = 512 / blocks;
+  const long long most = (a.length + p.keys - 1) / p.keys;
+  n = n > most ? most : n;
+  n = n > kSplitMax ? kSplitMax : n < 1 ? 1 : n;
+  const long long stages = (most + n - 1) / n;
+  p.split_keys = static_cast<int>((stages < 1 ? 1 : stages) * p.keys);
+  p.n_split = a.length > 0 ? (a.length + p.split_keys - 1) / p.split_keys : 1;
+  return p;
+}
+
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+size_t tiles_of(const AttendArgs &a) {
+  return static_cast<size_t>(a.n_seqs) * a.n_kv_heads * ((static_cast<size_t>(a.n_tokens) * a.group + 31) / 32);
+}
+size_t bytes_of(const AttendArgs &a, const Plan &p) {
+  if (p.n_split <= 1) return 0;
+  const size_t parts = tiles_of(a) * p.n_split;
+  return align_up(parts * 32 * a.head_dim * sizeof(float)) + align_up(parts * 64 * sizeof(float)) + align_up(tiles_of(a) * 32 * sizeof(float));
+}
+
+template <typename T, int D, int kWR, int kWK, int kKeys>
+hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
+  const long long M = static_cast<long long>(a.n_tokens) * a.group;
+  const long long grid = static_cast<long long>(a.n_seqs) * a.n_kv_heads * a.n_split * ((M + 32 * kWR - 1) / (32 * kWR));
+  if (grid > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWR * kWK), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch(AttendArgs a, hipStream_t stream) {
+  constexpr bool kLong = D * sizeof(T) == 512;
+  const Plan p = plan_of<T, D>(a);
+  a.n_split = p.n_split;
+  a.split_keys = p.split_keys;
+  a.wide = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.joined_out)) % 16 == 0;
+  if (bytes_of(a, p) > 0) {
+    if (!a.workspace) return hipErrorInvalidValue;
+    const size_t parts = tiles_of(a) * p.n_split;
+    char *w = static_cast<char *>(a.workspace);
+    a.part_o = reinterpret_cast<float *>(w);
+    w += align_up(parts * 32 * D * sizeof(float));
+    a.part_ml = reinterpret_cast<float *>(w);
+    w += align_up(parts * 64 * sizeof(float));
+    a.part_lse = reinterpret_cast<float *>(w);
+  }
+  hipError_t e;
+  if (p.wr == 1) e = launch_shape<T, D, 1, kLong ? 2 : 4, kLong ? 64 : 128>(a, stream);
+  else if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64>(a, stream);
+  else if (kLong || p.wr == 4) e = launch_shape<T, D, 4, 1, 64>(a, stream);
+  else e = launch_shape<T, D, kLong ? 4 : 8, 1, 64>(a, stream);
+  if (e != hipSuccess || p.n_split <= 1) return e;
+  const size_t blocks = tiles_of(a) * (D / 32);
+  if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((attend_merge_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kMergeBlock), 0, stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attend_workspace(const AttendArgs &) { return 0; }
+size_t attend_workspace(const AttendArgs &a) {
+  if (a.dtype == LAZYEV_DTYPE_FP32) return a.head_dim == 64 ? bytes_of(a, plan_of<float, 64>(a)) : bytes_of(a, plan_of<float, 128>(a));
+  return a.head_dim == 64 ? bytes_of(a, plan_of<bf16_t, 64>(a)) : bytes_of(a, plan_of<bf16_t, 128>(a));
+}
 
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream) {
   const long long rows = static_cast<long long>(a.n_seqs) * a.n_tokens * a.n_q_heads;
