@@ -14,9 +14,8 @@
 // The reference is raised only when a sum of 16 weights relative to it exceeds 2^12 (never rescaled otherwise): a sum
 // is as exact relative to any reference in the range of fp32.  Every decision that changes a row's arithmetic
 // is taken for that row alone: what other rows see has no influence on it.
-// Entries that some row of the wave does not see (or that lead to no page) are masked to weight zero, and V is then
-// multiplied with its infinities and NaN taken out; these are brought in by products of their own, with 1 in their places, whose
-// sums are positive where a row sees one.
+// Entries that a row does not see (or that lead to no page) are masked to weight zero.  In stages where that happens V has its
+// infinities and NaN taken out before it is multiplied; the rows that do see one get it at the end.
 //
 // Few rows: the entries are also cut into splits, which leave (m, l, O) in the workspace for a second kernel.
 #include "kernels.h"
@@ -170,20 +169,35 @@ __device__ __forceinline__ float exponent_of(float s, float c2, float m) {
   return fabsf(m) > kHuge ? x - m : fmaf(s, c2, -m);
 }
 
-// The elements of an operand register of V that are finite, and 1 where they are of a kind (0 +inf, 1 -inf, 2 NaN).
+// Elements whose exponents are all ones taken out of a chunk of V.
 template <bool kF32>
-__device__ __forceinline__ unsigned finite_of(unsigned w) {
-  if (kF32) return (w & 0x7F800000u) == 0x7F800000u ? 0u : w;
-  const unsigned lo = (w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu, hi = (w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u;
-  return lo | hi;
-}
-__device__ __forceinline__ bool of_kind(unsigned bits32, int kind) {   // an fp32 number's bits
-  return kind == 2 ? (bits32 & 0x7FFFFFFFu) > 0x7F800000u : bits32 == (kind == 0 ? 0x7F800000u : 0xFF800000u);
+__device__ __forceinline__ unsigned odd_bits(unsigned w) {             // the sign bits of those elements
+  return kF32 ? ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u : ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
 }
 template <bool kF32>
-__device__ __forceinline__ unsigned kind_of(unsigned w, int kind) {
-  if (kF32) return of_kind(w, kind) ? 0x3F800000u : 0u;
-  return (of_kind(w << 16, kind) ? 0x3F80u : 0u) | (of_kind(w & 0xFFFF0000u, kind) ? 0x3F800000u : 0u);
+__device__ __forceinline__ bool take_out_odd(u32x4_t &w) {
+  unsigned any = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned odd = odd_bits<kF32>(w[e]);
+    any |= odd;
+    w[e] &= ~(kF32 ? 0u - (odd >> 31) : (odd >> 15) * 0xFFFFu);
+  }
+  return any != 0;
+}
+
+// The order of the products of a basic block (kMfma for each of kN operands) and the reads of their operands from LDS (kReads each):
+// kDepth operands are on their way while one is multiplied.
+template <int kN, int kMfma, int kReads, int kDepth>
+__device__ __forceinline__ void ahead() {
+  constexpr int kFirst = kDepth < kN ? kDepth : kN;
+  __builtin_amdgcn_sched_group_barrier(0x100, kFirst * kReads, 0);
+#pragma unroll
+  for (int i = 0; i < kN - kFirst; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, kMfma, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kFirst * kMfma, 0);
 }
 
 // kWR x kWK waves: kWR of 32 rows each, kWK that share the entries of a stage.
@@ -209,7 +223,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   __shared__ __align__(16) char k_odd[S::kStageBytes];
   __shared__ __align__(16) char v_even[S::kStageBytes];
   __shared__ __align__(16) char v_odd[S::kStageBytes];
-  __shared__ int shared_end[2];
+  __shared__ int shared_most, shared_least, shared_holes, shared_odd;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
@@ -237,18 +251,25 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
   const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
-  if (threadIdx.x < 2) shared_end[threadIdx.x] = 0;
+  if (threadIdx.x == 0) {
+    shared_most = shared_holes = shared_odd = 0;
+    shared_least = a.length;
+  }
   __syncthreads();
-  if (lane == 0) atomicMax(&shared_end[0], most);
+  if (lane == 0 && have) {
+    atomicMax(&shared_most, most);
+    atomicMin(&shared_least, least);
+  }
   __syncthreads();
-  const int end = __builtin_amdgcn_readfirstlane(min(last, shared_end[0]));
+  const int end = __builtin_amdgcn_readfirstlane(min(last, shared_most));
   const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
   bool holes = false;                              // pages that are none among the block's
+  int clean_from = 0;
   if (n_stages > 0) {
     int bad = 0;
     for (int i = page_of(a.pages, first) + threadIdx.x; i <= page_of(a.pages, end - 1); i += S::kBlock)
       bad |= static_cast<unsigned>(table[i]) >= static_cast<unsigned>(a.pages.n_pages) ? 1 : 0;
-    if (bad) shared_end[1] = 1;
+    if (bad) shared_holes = 1;
   }
 
   u32x4_t qb[kOps];
@@ -394,6 +415,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     Weights p[kSub];
 #pragma unroll
     for (int x = 0; x < kSub; ++x) logits(ks, 32 * x, s[x]);
+    ahead<kSub * kOps, R::kF32 ? 4 : 1, 1, 4>();
     const bool mask = holes || key0 + 32 * kSub > min(least, last);
     if (mask) {
       const int limit = min(seen, last) - key0 - 4 * h;
@@ -435,62 +457,29 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       sum = weights(s, p);
     }
     l += sum;
-    if (!mask) {
-#pragma unroll
-      for (int x = 0; x < kSub; ++x)
-#pragma unroll
-        for (int g = 0; g < kProducts; ++g)
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t) product(values(vs, 32 * x, t, g), p[x], g, o[t]);
-      return;
-    }
-    bool odd = false;                              // infinities or NaN among the values
 #pragma unroll
     for (int x = 0; x < kSub; ++x)
 #pragma unroll
       for (int g = 0; g < kProducts; ++g)
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          auto v = values(vs, 32 * x, t, g);
-          if constexpr (R::kF32) {
-            const unsigned f = finite_of<true>(v);
-            odd = odd || f != v;
-            v = f;
-          } else {
+        for (int t = 0; t < kTiles; ++t) product(values(vs, 32 * x, t, g), p[x], g, o[t]);
+    ahead<kSub * kProducts * kTiles, 1, R::kF32 ? 1 : 2, 4>();
+  };
+  // A stage of which some row of the block does not see all: weight zero times an infinity or NaN would be NaN, so these are
+  // taken out of its values; what rows see of them is added when the loop is done.
+  auto clean = [&](char *vs) {
+    bool odd = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned f = finite_of<false>(v[e]);
-              odd = odd || f != v[e];
-              v[e] = f;
-            }
-          }
-          product(v, p[x], g, o[t]);
-        }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
-#pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind) {
-        const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          f32x16_t n;
-#pragma unroll
-          for (int x = 0; x < 16; ++x) n[x] = 0.f;
-#pragma unroll
-          for (int x = 0; x < kSub; ++x)
-#pragma unroll
-            for (int g = 0; g < kProducts; ++g) {
-              auto v = values(vs, 32 * x, t, g);
-              if constexpr (R::kF32) v = kind_of<true>(v, kind);
-              else
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = kind_of<false>(v[e], kind);
-              product(v, p[x], g, n);
-            }
-#pragma unroll
-          for (int x = 0; x < 16; ++x) o[t][x] = n[x] > 0.f ? o[t][x] + what : o[t][x];
-        }
+    for (int u = 0; u < S::kLoads; ++u) {
+      u32x4_t *at = reinterpret_cast<u32x4_t *>(vs) + u * S::kBlock + threadIdx.x;
+      u32x4_t w = *at;
+      if (take_out_odd<R::kF32>(w)) {
+        odd = true;
+        *at = w;
       }
     }
+    if (odd) shared_odd = 1;
+    __syncthreads();
   };
 
   if (n_stages > 0) {
@@ -498,13 +487,16 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     fetch(k_even, v_even);
     look_up(min(1, n_stages - 1));
     __syncthreads();                               // stage 0 is complete
-    holes = __builtin_amdgcn_readfirstlane(shared_end[1]) != 0;
+    holes = __builtin_amdgcn_readfirstlane(shared_holes) != 0;
+    // the first stage that somebody does not see all of
+    clean_from = holes ? 0 : max(min(__builtin_amdgcn_readfirstlane(shared_least), last) - first, 0) / kKeys;
     int st = 0;
     while (true) {
       if (st + 1 < n_stages) {
         fetch(k_odd, v_odd);
         look_up(min(st + 2, n_stages - 1));
       }
+      if (st >= clean_from) clean(v_even);
       work(k_even, v_even, st);
       __syncthreads();                             // the next stage is complete, this one no longer read
       if (++st >= n_stages) break;
@@ -512,6 +504,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
         fetch(k_even, v_even);
         look_up(min(st + 2, n_stages - 1));
       }
+      if (st >= clean_from) clean(v_odd);
       work(k_odd, v_odd, st);
       __syncthreads();
       if (++st >= n_stages) break;
@@ -551,6 +544,26 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
   }
   if (!have) return;
+
+  if (__builtin_expect(n_stages > 0 && __builtin_amdgcn_readfirstlane(shared_odd) != 0, 0)) {
+    // the infinities and NaN that were taken out and that a row sees (with a weight above zero, however small)
+    for (int key = first + clean_from * kKeys; key < min(last, most); ++key) {
+      const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
+      if (static_cast<unsigned>(no) >= static_cast<unsigned>(a.pages.n_pages)) continue;
+      const T *v = static_cast<const T *>(a.v_pages) +
+                   static_cast<size_t>(no * page_rows + kvh * head_rows + static_cast<unsigned>(key - pg * a.pages.page_size)) * D + 4 * h;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const T e = v[32 * t + 8 * (x / 4) + x % 4];
+          float f;
+          if constexpr (R::kF32) f = e;
+          else f = __uint_as_float(static_cast<unsigned>(e) << 16);
+          o[t][x] += key < seen && !(fabsf(f) <= FLT_MAX) ? f : 0.f;
+        }
+    }
+  }
 
   if (a.n_split > 1) {
     // for the second kernel: [unit][32 rows][split][register / 4][lane] float4, and (m, l) of the rows
