@@ -22,6 +22,7 @@
 #include "lazyev.h"
 
 #include <cfloat>
+#include <climits>
 #include <type_traits>
 
 namespace lazyev {
@@ -201,7 +202,7 @@ __device__ __forceinline__ void ahead() {
 }
 
 // kWR x kWK waves: kWR of 32 rows each, kWK that share the entries of a stage.
-template <typename T, int D, int kWR, int kWK, int kKeys>
+template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
 struct Shape {
   using R = Rows<T, D>;
   static constexpr int kWaves = kWR * kWK, kBlock = 64 * kWaves;
@@ -210,20 +211,19 @@ struct Shape {
   static constexpr int kLoads = kKeys / (kPerLoad * kWaves);   // of K and of V each, per wave and stage
   static_assert(kSub >= 1 && kLoads >= 1 && kLoads * kPerLoad * kWaves == kKeys, "whole loads");
   static constexpr int kPerSimd = D * sizeof(T) == 512 ? 1 : 2;   // (fp32 rows of 128: queries and output take 128 registers, the products' operands more)
-  static constexpr int kStageBytes = kKeys * D * static_cast<int>(sizeof(T));   // of K; of V as many
-  static_assert((kWK - 1) * kWR * 32 * D * 4 <= 2 * kStageBytes, "the waves' outputs fit where two stages of K were");
+  static constexpr int kHalf = kKeys * D * static_cast<int>(sizeof(T)), kStage = 2 * kHalf;   // bytes of a stage: of K, then of V
 };
+constexpr int kWindow = 1024;           // page numbers that a block keeps in LDS
 
-template <typename T, int D, int kWR, int kWK, int kKeys>
-__global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPerSimd)) void attend_kernel(const AttendArgs a) {
+template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
+__global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs>::kPerSimd)) void attend_kernel(const AttendArgs a) {
   using R = Rows<T, D>;
-  using S = Shape<T, D, kWR, kWK, kKeys>;
+  using S = Shape<T, D, kWR, kWK, kKeys, kBufs>;
   constexpr int kSub = S::kSub, kOps = R::kOps, kTiles = R::kTiles, C = R::kChunks;
-  __shared__ __align__(16) char k_even[S::kStageBytes];
-  __shared__ __align__(16) char k_odd[S::kStageBytes];
-  __shared__ __align__(16) char v_even[S::kStageBytes];
-  __shared__ __align__(16) char v_odd[S::kStageBytes];
-  __shared__ int shared_most, shared_least, shared_holes, shared_odd;
+  __shared__ __align__(16) char stages[kBufs * S::kStage];
+  __shared__ int window[kWindow];
+  __shared__ float shared_ml[kWK][kWR][64];
+  __shared__ int shared_most[S::kWaves], shared_least[S::kWaves], shared_hole[kBufs], shared_odd;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
@@ -238,6 +238,8 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   const bool have = r0 < M;
   const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
 
+  const float lse_other = lse_joined(a, place);
+
   // entries of this block: first .. end - 1; what its rows see of them
   const int first = split * a.split_keys, last = min(first + a.split_keys, a.length);
   int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
@@ -251,26 +253,13 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
   const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
-  if (threadIdx.x == 0) {
-    shared_most = shared_holes = shared_odd = 0;
-    shared_least = a.length;
-  }
-  __syncthreads();
-  if (lane == 0 && have) {
-    atomicMax(&shared_most, most);
-    atomicMin(&shared_least, least);
-  }
-  __syncthreads();
-  const int end = __builtin_amdgcn_readfirstlane(min(last, shared_most));
-  const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
-  bool holes = false;                              // pages that are none among the block's
-  int clean_from = 0;
-  if (n_stages > 0) {
-    int bad = 0;
-    for (int i = page_of(a.pages, first) + threadIdx.x; i <= page_of(a.pages, end - 1); i += S::kBlock)
-      bad |= static_cast<unsigned>(table[i]) >= static_cast<unsigned>(a.pages.n_pages) ? 1 : 0;
-    if (bad) shared_holes = 1;
-  }
+  // the first window of page numbers
+  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
+  int window_at = page_of(a.pages, first);
+  auto fill_window = [&]() __attribute__((always_inline)) {
+    for (int i = threadIdx.x; i < kWindow && window_at + i <= page_last; i += S::kBlock) window[i] = table[window_at + i];
+  };
+  if (last > first) fill_window();
 
   u32x4_t qb[kOps];
   {
@@ -291,31 +280,71 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
 
   // ---- stages on their way to LDS
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
-  int page[S::kLoads];
-  unsigned within[S::kLoads];                      // the entry's row in its page
-  auto look_up = [&](int st) {
+  if (lane == 0) {
+    shared_most[wave] = most;
+    shared_least[wave] = have ? least : a.length;
+  }
+  if (threadIdx.x < kBufs) shared_hole[threadIdx.x] = 0;
+  if (threadIdx.x == 0) shared_odd = 0;
+  __syncthreads();
+  int end = 0, block_least = a.length;
 #pragma unroll
-    for (int u = 0; u < S::kLoads; ++u) {
-      const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
-      const int entry = min(first + st * kKeys + r, end - 1);
-      const int pg = page_of(a.pages, entry);
-      within[u] = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
-      page[u] = table[pg];
-    }
+  for (int w = 0; w < S::kWaves; ++w) {
+    end = max(end, shared_most[w]);
+    block_least = min(block_least, shared_least[w]);
+  }
+  end = __builtin_amdgcn_readfirstlane(min(end, last));
+  const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
+  // the first stage that some row does not see all of
+  const int clean_from = max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
+  int cleaned = INT_MAX;                           // ... and the first one that was cleaned
+
+  // Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as the compiler has every read of
+  // LDS wait for all loads into it: they leave nothing in registers, and the waits for them are in `arrived`.)
+  const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
+  auto load_1k = [&](const char *from, unsigned to) __attribute__((always_inline)) {
+    __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
   };
-  auto fetch = [&](char *k_to, char *v_to) {
-    typedef const __attribute__((address_space(1))) void *from_t;
-    typedef __attribute__((address_space(3))) void *to_t;
+  auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
+    const int e0 = first + st * kKeys;
+    if (page_of(a.pages, min(e0 + kKeys, end) - 1) >= window_at + kWindow) {   // (uniform)
+      window_at = page_of(a.pages, e0);
+      __syncthreads();
+      fill_window();
+      __syncthreads();
+    }
+    bool hole = false;
 #pragma unroll
     for (int u = 0; u < S::kLoads; ++u) {
       const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
-      // (no page: any row; its entries are masked)
-      const unsigned pg = static_cast<unsigned>(page[u]) < static_cast<unsigned>(a.pages.n_pages) ? page[u] : 0u;
-      const size_t row = static_cast<size_t>(pg * page_rows + within[u]) * (D * sizeof(T));
-      const int at = (u * S::kWaves + wave) * 1024;
-      __builtin_amdgcn_global_load_lds((from_t)(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16), (to_t)(k_to + at), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((from_t)(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16), (to_t)(v_to + at), 16, 0, 0);
+      const int entry = min(e0 + r, end - 1), pg = page_of(a.pages, entry);
+      unsigned no = static_cast<unsigned>(window[pg - window_at]);
+      if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
+        hole = true;
+        no = 0;
+      }
+      const unsigned in_page = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+      const size_t row = static_cast<size_t>(no * page_rows + in_page) * (D * sizeof(T));
+      const unsigned to = stages_at + buf * S::kStage + (u * S::kWaves + wave) * 1024;
+      load_1k(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16, to);
+      load_1k(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16, to + S::kHalf);
     }
+    if (hole) shared_hole[buf] = st + 1;           // (by the barrier before the stage is worked on)
+  };
+  // Waits for this wave's loads of a stage, of which `younger` more stages are on their way behind it, and for the other waves.
+  auto arrived = [&](int younger) __attribute__((always_inline)) {
+    constexpr int kOps2 = 2 * S::kLoads;
+    auto wait = [&](auto n) __attribute__((always_inline)) {   // vmcnt(n), lgkmcnt(0)
+      constexpr int x = decltype(n)::value;
+      __asm__ volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt((x & 15) | 7 << 4 | (x >> 4) << 14);
+    };
+    static_assert((kBufs - 2) * kOps2 < 64, "the counter has six bits");
+    if (kBufs > 3 && younger >= 2) wait(std::integral_constant<int, (kBufs > 3 ? 2 : 0) * kOps2>{});
+    else if (kBufs > 2 && younger >= 1) wait(std::integral_constant<int, (kBufs > 2 ? 1 : 0) * kOps2>{});
+    else wait(std::integral_constant<int, 0>{});
+    __builtin_amdgcn_s_barrier();
+    __asm__ volatile("" ::: "memory");
   };
 
   const float c2 = a.scale * kLog2e;
@@ -340,7 +369,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   constexpr int kEntry = C * 16;                   // bytes of an entry
 
   // one sub-tile's logits
-  auto logits = [&](const char *ks, int e0, f32x16_t &s) {
+  auto logits = [&](const char *ks, int e0, f32x16_t &s) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) s[x] = 0.f;
 #pragma unroll
@@ -357,7 +386,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   };
   // The operand of V for a product: columns 32 t .., bf16: entries 16 g .. 16 g + 15 of the sub-tile; fp32: the entries
   // 8 i + 4 h + j with 4 i + j = g.
-  auto values = [&](const char *vs, int e0, int t, int g) {
+  auto values = [&](const char *vs, int e0, int t, int g) __attribute__((always_inline)) {
     if constexpr (R::kF32) {
       return *reinterpret_cast<const unsigned *>(vs + v_at[t] + (e0 + 8 * (g / 4) + g % 4) * kEntry);
     } else {
@@ -375,11 +404,11 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   };
   constexpr int kProducts = R::kF32 ? 16 : 2;      // of a sub-tile and a tile of columns
   using Weights = std::conditional_t<R::kF32, f32x16_t, u32x4_t[2]>;
-  auto product = [&](auto v, const Weights &p, int g, f32x16_t &to) {
+  auto product = [&](auto v, const Weights &p, int g, f32x16_t &to) __attribute__((always_inline)) {
     if constexpr (R::kF32) to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), p[g], to, 0, 0, 0);
     else to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, p[g]), to, 0, 0, 0);
   };
-  auto weights_of = [&](const f32x16_t &s, Weights &p, auto fast) {   // -> their sum
+  auto weights_of = [&](const f32x16_t &s, Weights &p, auto fast) __attribute__((always_inline)) {   // -> their sum
     float w[16], sum = 0.f;
 #pragma unroll
     for (int x = 0; x < 16; ++x) w[x] = __builtin_amdgcn_exp2f(decltype(fast)::value ? fmaf(s[x], c2, -m) : exponent_of(s[x], c2, m));
@@ -394,7 +423,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
     return sum;
   };
-  auto weights = [&](const f32x16_t (&s)[kSub], Weights (&p)[kSub]) {
+  auto weights = [&](const f32x16_t (&s)[kSub], Weights (&p)[kSub]) __attribute__((always_inline)) {
     float sum = 0.f;
     if (plain) {                                   // (wave-uniform)
 #pragma unroll
@@ -406,7 +435,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     return sum;
   };
 
-  auto work = [&](const char *ks, const char *vs, int st) {
+  auto work = [&](const char *ks, const char *vs, int st, bool holes) __attribute__((always_inline)) {
     const int key0 = first + st * kKeys + wk * (32 * kSub);   // this wave's entries
     ks += wk * (32 * kSub * kEntry);
     vs += wk * (32 * kSub * kEntry);
@@ -467,7 +496,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   };
   // A stage of which some row of the block does not see all: weight zero times an infinity or NaN would be NaN, so these are
   // taken out of its values; what rows see of them is added when the loop is done.
-  auto clean = [&](char *vs) {
+  auto clean = [&](char *vs) __attribute__((always_inline)) {
     bool odd = false;
 #pragma unroll
     for (int u = 0; u < S::kLoads; ++u) {
@@ -482,110 +511,116 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     __syncthreads();
   };
 
-  if (n_stages > 0) {
-    look_up(0);
-    fetch(k_even, v_even);
-    look_up(min(1, n_stages - 1));
-    __syncthreads();                               // stage 0 is complete
-    holes = __builtin_amdgcn_readfirstlane(shared_holes) != 0;
-    // the first stage that somebody does not see all of
-    clean_from = holes ? 0 : max(min(__builtin_amdgcn_readfirstlane(shared_least), last) - first, 0) / kKeys;
-    int st = 0;
-    while (true) {
-      if (st + 1 < n_stages) {
-        fetch(k_odd, v_odd);
-        look_up(min(st + 2, n_stages - 1));
-      }
-      if (st >= clean_from) clean(v_even);
-      work(k_even, v_even, st);
-      __syncthreads();                             // the next stage is complete, this one no longer read
-      if (++st >= n_stages) break;
-      if (st + 1 < n_stages) {
-        fetch(k_even, v_even);
-        look_up(min(st + 2, n_stages - 1));
-      }
-      if (st >= clean_from) clean(v_odd);
-      work(k_odd, v_odd, st);
-      __syncthreads();
-      if (++st >= n_stages) break;
+  // Stages 0 .. kBufs - 2 are on their way before the first one is worked on; one barrier a stage: behind it the stage is
+  // complete and the one before it, whose place the next load takes, no longer read.
+#pragma unroll
+  for (int st = 0; st < kBufs - 1; ++st)
+    if (st < n_stages) fetch(st, st);
+  int buf = 0;
+#pragma unroll 1
+  for (int st = 0; st < n_stages; ++st) {
+    arrived(n_stages - 1 - st);
+    if (st + kBufs - 1 < n_stages) fetch(st + kBufs - 1, buf == 0 ? kBufs - 1 : buf - 1);
+    char *at = stages + buf * S::kStage;
+    const bool holes = __builtin_amdgcn_readfirstlane(shared_hole[buf]) == st + 1;
+    if (holes || st >= clean_from) {
+      cleaned = min(cleaned, st);
+      clean(at + S::kHalf);
     }
+    work(at, at + S::kHalf, st, holes);
+    buf = buf + 1 == kBufs ? 0 : buf + 1;
   }
   l = sum_of_halves(l);
 
-  // ---- the waves that share rows -> the first of them
-  if constexpr (kWK > 1) {
-    // (where the stages were; every wave is past its last one)
-    auto at = [&](int which, int x) -> float & {   // register x of the wave's partial
-      const int i = ((which * kWR + wr) * (16 * kTiles) + x) * 64 + lane;
-      return (i < S::kStageBytes / 4) ? reinterpret_cast<float *>(k_even)[i] : reinterpret_cast<float *>(k_odd)[i - S::kStageBytes / 4];
-    };
-    float *ml = reinterpret_cast<float *>(v_even);
-    if (wk > 0) {
+  // ---- the waves that share rows: their outputs go through LDS, and each of them ends up with a part of the columns, groups
+  // of four per lane: group k of this wave is columns 32 t + 8 i + 4 h .. with 4 t + i = first_group + k
+  constexpr int kOwn = 4 * kTiles / kWK;
+  const int first_group = wk * kOwn;
+  f32x4_t part[kOwn];
+  if constexpr (kWK == 1) {
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+    for (int k = 0; k < kOwn; ++k) part[k] = f32x4_t{o[k / 4][k % 4 * 4], o[k / 4][k % 4 * 4 + 1], o[k / 4][k % 4 * 4 + 2], o[k / 4][k % 4 * 4 + 3]};
+  } else {
+    // (where the stages were, in rounds of what these hold)
+    constexpr int kAll = S::kWaves * 32 * D * 4, kRounds = (kAll + kBufs * S::kStage - 1) / (kBufs * S::kStage), kPer = kOwn / kRounds;
+    static_assert(kPer * kRounds == kOwn, "whole rounds");
+    static_assert(S::kWaves * kWK * kPer * 64 * 16 <= kBufs * S::kStage, "every wave has a place");
+    auto place_of_wave = [&](int w) __attribute__((always_inline)) { return reinterpret_cast<f32x4_t *>(stages) + w * (kWK * kPer * 64) + lane; };
+    __syncthreads();                               // (every wave is past its last stage)
+    shared_ml[wk][wr][lane] = h == 0 ? m : l;
+    f32x4_t *mine = place_of_wave(wave);
+    float x[kWK];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) at(wk - 1, 16 * t + x) = o[t][x];
-      ml[(((wk - 1) * kWR + wr) * 2) * 64 + lane] = m;
-      ml[(((wk - 1) * kWR + wr) * 2 + 1) * 64 + lane] = l;
-    }
-    __syncthreads();
-    if (wk > 0) return;
+    for (int rnd = 0; rnd < kRounds; ++rnd) {
 #pragma unroll
-    for (int w = 0; w < kWK - 1; ++w) {
-      const float mo = ml[((w * kWR + wr) * 2) * 64 + lane], lo = ml[((w * kWR + wr) * 2 + 1) * 64 + lane];
-      const float up = fmaxf(m, mo);
-      const float x0 = __builtin_amdgcn_exp2f(m - up), x1 = __builtin_amdgcn_exp2f(mo - up);
-      m = up;
-      l = l * x0 + lo * x1;
+      for (int w = 0; w < kWK; ++w)                // for wave w: its groups of this round
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+        for (int k = 0; k < kPer; ++k) {
+          const int g = w * kOwn + rnd * kPer + k;
+          mine[(w * kPer + k) * 64] = f32x4_t{o[g / 4][g % 4 * 4], o[g / 4][g % 4 * 4 + 1], o[g / 4][g % 4 * 4 + 2], o[g / 4][g % 4 * 4 + 3]};
+        }
+      __asm__ volatile("" ::"v"(lse_other));       // (read by all before one of them replaces it)
+      __syncthreads();
+      if (rnd == 0) {
+        m = -FLT_MAX;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) o[t][x] = o[t][x] * x0 + at(w, 16 * t + x) * x1;
+        for (int w = 0; w < kWK; ++w) m = fmaxf(m, shared_ml[w][wr][c]);
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWK; ++w) {
+          x[w] = __builtin_amdgcn_exp2f(shared_ml[w][wr][c] - m);
+          l = fmaf(shared_ml[w][wr][32 + c], x[w], l);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWK; ++w) sum += place_of_wave(w * kWR + wr)[(wk * kPer + k) * 64] * x[w];
+        part[rnd * kPer + k] = sum;
+      }
+      if (rnd + 1 < kRounds) __syncthreads();
     }
   }
   if (!have) return;
 
-  if (__builtin_expect(n_stages > 0 && __builtin_amdgcn_readfirstlane(shared_odd) != 0, 0)) {
+  if (__builtin_expect(cleaned != INT_MAX && __builtin_amdgcn_readfirstlane(shared_odd) != 0, 0)) {
     // the infinities and NaN that were taken out and that a row sees (with a weight above zero, however small)
-    for (int key = first + clean_from * kKeys; key < min(last, most); ++key) {
+    for (int key = first + cleaned * kKeys; key < min(last, most); ++key) {
       const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
       if (static_cast<unsigned>(no) >= static_cast<unsigned>(a.pages.n_pages)) continue;
       const T *v = static_cast<const T *>(a.v_pages) +
                    static_cast<size_t>(no * page_rows + kvh * head_rows + static_cast<unsigned>(key - pg * a.pages.page_size)) * D + 4 * h;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+      for (int k = 0; k < kOwn; ++k)
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const T e = v[32 * t + 8 * (x / 4) + x % 4];
+        for (int e = 0; e < 4; ++e) {
+          const T y = v[8 * (first_group + k) + e];
           float f;
-          if constexpr (R::kF32) f = e;
-          else f = __uint_as_float(static_cast<unsigned>(e) << 16);
-          o[t][x] += key < seen && !(fabsf(f) <= FLT_MAX) ? f : 0.f;
+          if constexpr (R::kF32) f = y;
+          else f = __uint_as_float(static_cast<unsigned>(y) << 16);
+          part[k][e] += key < seen && !(fabsf(f) <= FLT_MAX) ? f : 0.f;
         }
     }
   }
 
   if (a.n_split > 1) {
-    // for the second kernel: [unit][32 rows][split][register / 4][lane] float4, and (m, l) of the rows
+    // for the second kernel: [unit][32 rows][split][group][lane] float4, and (m, l) of the rows
     const int tiles = (M + 31) / 32;
     const size_t p = (static_cast<size_t>(unit) * tiles + r0 / 32) * a.n_split + split;
     f32x4_t *to = reinterpret_cast<f32x4_t *>(a.part_o) + p * (4 * kTiles * 64) + lane;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) to[(4 * t + i) * 64] = f32x4_t{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+    for (int k = 0; k < kOwn; ++k) to[(first_group + k) * 64] = part[k];
+    if (wk > 0) return;
     a.part_ml[p * 64 + lane] = h == 0 ? m : l;
-    if (split == 0 && h == 0) a.part_lse[static_cast<size_t>(unit) * (tiles * 32) + r0 + c] = lse_joined(a, place);
+    if (split == 0 && h == 0) a.part_lse[static_cast<size_t>(unit) * (tiles * 32) + r0 + c] = lse_other;
     return;
   }
   if (r0 + c >= M || !takes_part(a, place.token)) return;
-  const Joined j = join(m, l, lse_joined(a, place));
+  const Joined j = join(m, l, lse_other);
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      finish4<T, D>(a, place, 32 * t + 8 * i + 4 * h, f32x4_t{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]}, j);
-  if (h == 0) finish_row(a, place, j);
+  for (int k = 0; k < kOwn; ++k) finish4<T, D>(a, place, 8 * (first_group + k) + 4 * h, part[k], j);
+  if (wk == 0 && h == 0) finish_row(a, place, j);
 }
 
 // The splits of 32 rows joined: blocks = unit, 32 rows and 32 columns; four groups of 256 threads take every fourth split.
@@ -676,12 +711,12 @@ size_t bytes_of(const AttendArgs &a, const Plan &p) {
   return align_up(parts * 32 * a.head_dim * sizeof(float)) + align_up(parts * 64 * sizeof(float)) + align_up(tiles_of(a) * 32 * sizeof(float));
 }
 
-template <typename T, int D, int kWR, int kWK, int kKeys>
+template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
 hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
   const long long M = static_cast<long long>(a.n_tokens) * a.group;
   const long long grid = static_cast<long long>(a.n_seqs) * a.n_kv_heads * a.n_split * ((M + 32 * kWR - 1) / (32 * kWR));
   if (grid > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWR * kWK), 0, stream, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kBufs>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWR * kWK), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -703,10 +738,10 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
     a.part_lse = reinterpret_cast<float *>(w);
   }
   hipError_t e;
-  if (p.wr == 1) e = launch_shape<T, D, 1, kLong ? 2 : 4, kLong ? 64 : 128>(a, stream);
-  else if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64>(a, stream);
-  else if (kLong || p.wr == 4) e = launch_shape<T, D, 4, 1, 64>(a, stream);
-  else e = launch_shape<T, D, kLong ? 4 : 8, 1, 64>(a, stream);
+  if (p.wr == 1) e = launch_shape<T, D, 1, kLong ? 2 : 4, kLong ? 64 : 128, 2>(a, stream);
+  else if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64, 2>(a, stream);
+  else if (kLong || p.wr == 4) e = launch_shape<T, D, 4, 1, 64, 2>(a, stream);
+  else e = launch_shape<T, D, kLong ? 4 : 8, 1, 64, kLong ? 2 : 3>(a, stream);
   if (e != hipSuccess || p.n_split <= 1) return e;
   const size_t blocks = tiles_of(a) * (D / 32);
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
