@@ -73,53 +73,41 @@ __device__ __forceinline__ void store_chunk(T *p, const u32x4_t &w) {
   for (int i = 0; i < static_cast<int>(16 / sizeof(T)); ++i) p[i] = e[i];
 }
 
-// grid: x = spans of kTokens tokens (of all sequences in a row), y = shares of their heads
-template <typename T, int D, int kTokens, bool kVec>
+// grid: x = spans of kTokens tokens (of all sequences in a row), y = shares of their heads.  A wave takes kBatch times its
+// heads at once: their loads are on their way together, the first ones while the sines and cosines are worked out.
+template <typename T, int D, int kTokens, int kBatch, bool kVec>
 __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
   constexpr int E = Chunk<T>::kElems, L = D / E, kRows = 64 / L;   // elements and lanes of a chunk / a head, heads of a wave
   constexpr int kWavesPerToken = kWaves / kTokens;
   __shared__ float2 turn[kTokens][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
-  const long long token0 = static_cast<long long>(blockIdx.x) * kTokens;
-  if (a.half > 0) {
-    for (int x = threadIdx.x; x < kTokens * a.half; x += kBlock) {
-      const int j = x % a.half, k = x / a.half;
-      const long long tk = token0 + k;
-      if (tk >= tokens) break;
-      const long long p = a.start + (a.positions ? a.positions[tk] : static_cast<int>(tk % a.n_tokens));
-      constexpr double kPerTurn = 0.15915494309189533576888;
-      const double turns = static_cast<double>(p) * static_cast<double>(a.inv_freq[j]) * kPerTurn;
-      float s, c;
-      sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
-      turn[k][j] = make_float2(c, s);
-    }
-    __syncthreads();
-  }
+  const int tokens = a.n_seqs * a.n_tokens;
+  const int token0 = static_cast<int>(blockIdx.x) * kTokens;
   const int my_k = kTokens == 1 ? 0 : wave / kWavesPerToken;
-  const long long tk = token0 + my_k;
-  if (tk >= tokens) return;
-  const int seq = static_cast<int>(tk / a.n_tokens), token = static_cast<int>(tk % a.n_tokens);
-  // where the token's rows go in the pages
-  long long page_row = 0;
-  if (a.pages.table) {
-    const int entry = a.first_entry + token, pg = page_of(a.pages, entry);
-    const int page = a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg];
-    if (page < 0 || page >= a.pages.n_pages) return;
-    page_row = static_cast<long long>(page) * a.rows[0].heads * a.pages.page_size + (entry - pg * a.pages.page_size);
-  }
+  const int tk = min(token0 + my_k, tokens - 1);   // (a wave without a token works on the last one and leaves nothing)
+  const int seq = a.n_seqs == 1 ? 0 : tk / a.n_tokens, token = tk - seq * a.n_tokens;
   const int li = lane % L, e0 = li * E;            // this lane's elements of a head: e0 .. e0 + E - 1
-  const bool halves = a.layout == LAZYEV_ROPE_HALVES;
-  const bool turned = e0 < 2 * a.half;
-  float cs[E], sn[E];                              // (pairs: of the first E / 2 places)
+  const int n0 = a.rows[0].heads, n = n0 + a.rows[1].heads;
+  const T *in[2];
+  T *out[2];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int j = halves ? e0 % (a.half > 0 ? a.half : 1) + e : e0 / 2 + e / 2;
-    const float2 cv = turned ? turn[my_k][j] : make_float2(1.f, 0.f);
-    cs[e] = cv.x;
-    sn[e] = (halves ? e0 < a.half : e % 2 == 0) ? -cv.y : cv.y;
+  for (int s = 0; s < 2; ++s) {
+    in[s] = static_cast<const T *>(a.rows[s].in) + (seq * a.rows[s].in_seq + token * a.rows[s].in_token) + e0;
+    out[s] = static_cast<T *>(a.rows[s].out) + (a.pages.table ? 0 : seq * a.rows[s].out_seq + token * a.rows[s].out_token) + e0;
   }
-  const int partner = halves && turned ? (e0 < a.half ? lane + a.half / E : lane - a.half / E) : lane;
+  constexpr int kStep = kRows * kWavesPerToken;
+  const int step = kStep * static_cast<int>(gridDim.y);
+  int h0 = (static_cast<int>(blockIdx.y) * kWavesPerToken + wave % kWavesPerToken) * kRows + lane / L;   // this lane's head
+  u32x4_t raw[kBatch];
+  auto load = [&](int first) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int at = min(first + u * step, n - 1);
+      const bool second = at >= n0;
+      raw[u] = load_chunk<T, kVec>((second ? in[1] : in[0]) + (second ? at - n0 : at) * (second ? a.rows[1].in_head : a.rows[0].in_head));
+    }
+  };
+  load(h0);
   float w[2][E];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
@@ -128,39 +116,79 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) w[s][e] = 1.f;
   }
-  const int n0 = a.rows[0].heads, n = n0 + a.rows[1].heads;
-  const int step = kRows * kWavesPerToken * static_cast<int>(gridDim.y);
-  for (int h0 = (static_cast<int>(blockIdx.y) * kWavesPerToken + wave % kWavesPerToken) * kRows; h0 < n; h0 += step) {
-    const int at = h0 + lane / L;
-    const bool have = at < n;                      // (lanes without a head work on the last one and leave nothing)
-    const int which = min(at, n - 1) >= n0 ? 1 : 0, h = min(at, n - 1) - (which ? n0 : 0);
-    const RopeRows &r = a.rows[which];
-    const u32x4_t raw = load_chunk<T, kVec>(static_cast<const T *>(r.in) + seq * r.in_seq + token * r.in_token + h * r.in_head + e0);
-    float x[E];
-    Chunk<T>::open(raw, x);
-    float ss = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
-    const float inv = r.weight ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = x[e] * inv * (which ? w[1][e] : w[0][e]);
-    float y[E];
-    if (halves) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = __shfl(x[e], partner);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = x[e ^ 1];
+  if (a.half > 0) {
+    for (int x = threadIdx.x; x < kTokens * a.half; x += kBlock) {
+      const int k = x / a.half, j = x - k * a.half, at = min(token0 + k, tokens - 1);
+      const long long p = a.start + (a.positions ? a.positions[at] : a.n_seqs == 1 ? at : at % a.n_tokens);
+      constexpr double kPerTurn = 0.15915494309189533576888;
+      const double turns = static_cast<double>(p) * static_cast<double>(a.inv_freq[j]) * kPerTurn;
+      float s, c;
+      sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
+      turn[k][j] = make_float2(c, s);
     }
-    const bool turns = turned && r.turn;
+    __syncthreads();
+  }
+  if (token0 + my_k >= tokens) return;
+  // where the token's rows go in the pages
+  if (a.pages.table) {
+    const int entry = a.first_entry + token, pg = page_of(a.pages, entry);
+    const int page = a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg];
+    if (page < 0 || page >= a.pages.n_pages) return;
+    const long long row = static_cast<long long>(page) * n0 * a.pages.page_size + (entry - pg * a.pages.page_size);
+    out[0] += row * D;
+    out[1] += row * D;
+  }
+  const long long out_head[2] = {a.pages.table ? static_cast<long long>(a.pages.page_size) * D : a.rows[0].out_head,
+                                 a.pages.table ? static_cast<long long>(a.pages.page_size) * D : a.rows[1].out_head};
+  const bool halves = a.layout == LAZYEV_ROPE_HALVES;
+  const bool turned = e0 < 2 * a.half;
+  float cs[E], sn[E];                              // (pairs: of the first E / 2 places)
+  {
+    const int j0 = halves ? (e0 < a.half ? e0 : e0 - a.half) : e0 / 2;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = turns ? fmaf(y[e], sn[e], x[e] * cs[e]) : x[e];
-    if (!have) continue;
-    T *to = static_cast<T *>(r.out);
-    to += a.pages.table ? (page_row + static_cast<long long>(h) * a.pages.page_size) * D : seq * r.out_seq + token * r.out_token + h * r.out_head;
-    store_chunk<T, kVec>(to + e0, r.turn || r.weight ? Chunk<T>::close(x) : raw);
+    for (int e = 0; e < E; ++e) {
+      const float2 cv = turned ? turn[my_k][j0 + (halves ? e : e / 2)] : make_float2(1.f, 0.f);
+      cs[e] = cv.x;
+      sn[e] = (halves ? e0 < a.half : e % 2 == 0) ? -cv.y : cv.y;
+    }
+  }
+  const int partner = halves && turned ? (e0 < a.half ? lane + a.half / E : lane - a.half / E) : lane;
+  for (; h0 - lane / L < n; h0 += kBatch * step) {   // (the same in all lanes)
+    u32x4_t done[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int at = h0 + u * step;
+      const bool second = min(at, n - 1) >= n0;
+      const bool normed = second ? a.rows[1].weight != nullptr : a.rows[0].weight != nullptr, turns = second ? a.rows[1].turn : a.rows[0].turn;
+      float x[E], y[E];
+      Chunk<T>::open(raw[u], x);
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
+      const float inv = normed ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = x[e] * inv * (second ? w[1][e] : w[0][e]);
+      if (halves) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = __shfl(x[e], partner);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = x[e ^ 1];
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = turned && turns ? fmaf(y[e], sn[e], x[e] * cs[e]) : x[e];
+      done[u] = turns || normed ? Chunk<T>::close(x) : raw[u];
+    }
+    const int next = h0 + kBatch * step;
+    if (next - lane / L < n) load(next);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int at = h0 + u * step;
+      const bool second = at >= n0;
+      if (at < n) store_chunk<T, kVec>((second ? out[1] : out[0]) + (second ? at - n0 : at) * (second ? out_head[1] : out_head[0]), done[u]);
+    }
   }
 }
 
@@ -169,14 +197,14 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
   const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
   const int heads = a.rows[0].heads + a.rows[1].heads;
-  // Four tokens a block share nothing but the block; a single one with its heads dealt to more blocks where
+  // Four tokens a block, a wave each, with four times its heads at once, or a single one with its heads dealt to more blocks and waves where
   // that would leave the chip's 256 compute units without eight blocks each
   if (tokens >= 4 * 2048) {
-    hipLaunchKernelGGL((rope_kernel<T, D, 4, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((rope_kernel<T, D, 4, 4, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
   } else {
     const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
     const int want = static_cast<int>((2048 + tokens - 1) / tokens);
-    hipLaunchKernelGGL((rope_kernel<T, D, 1, kVec>), dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(shares < want ? shares : want)),
+    hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec>), dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(shares < want ? shares : want)),
                        dim3(kBlock), 0, stream, a);
   }
   return hipGetLastError();
@@ -199,7 +227,7 @@ hipError_t launch_any(const RopeArgs &a, hipStream_t stream) {
 
 hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream) {
   const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
-  if (tokens < 1 || tokens > 0x7FFFFFFFLL || a.rows[0].heads < 1 || a.rows[1].heads < 0 || a.half < 0 || a.half > head_dim / 2 || a.half % 8 != 0 ||
+  if (tokens < 1 || tokens > (1ll << 30) || a.rows[0].heads < 1 || a.rows[1].heads < 0 || a.half < 0 || a.half > head_dim / 2 || a.half % 8 != 0 ||
       (a.half > 0 && !a.inv_freq) || (a.pages.table && a.rows[1].heads != 0 && a.rows[1].heads != a.rows[0].heads))
     return hipErrorInvalidValue;
   if (dtype == LAZYEV_DTYPE_FP32 && head_dim == 64) return launch_any<float, 64>(a, stream);
