@@ -357,7 +357,8 @@ int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32
  * joined_out, joined_lse (nullable, together): the output and lse of the same queries over other entries, for instance the
  *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  `out` is not q.
  * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; bf16 weights
- * are rounded to bf16 for the product with V.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times.
+ * are rounded to bf16 for the product with V.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times;
+ * n_tokens * n_q_heads / n_kv_heads is at most 65535 * 32.
  * Workspace: lazyev_pages_attend_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).
  * Errors: EINVAL (length 0 .. table_stride * page_size among them), EWORKSPACE, EHIP. */
 int lazyev_pages_attend(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,

@@ -77,7 +77,8 @@ namespace lazyev {
 bool attend_args(const lazyev_pages *p, int32_t length, int32_t n_tokens, int32_t n_q_heads, AttendArgs *out) {
   if (!pages_ok(p) || length < 0 || n_tokens < 0 || n_q_heads < 1 || n_q_heads % p->n_kv_heads != 0) return false;
   if (n_q_heads / p->n_kv_heads > 64 || static_cast<long long>(length) > static_cast<long long>(p->table_stride) * p->page_size) return false;
-  // (rows, and rows of one table row and KV head, have 32-bit numbers; a table row's entries too)
+  // (rows and a table row's entries have 32-bit numbers; those of a table row and KV head are cut into at most 65535 blocks)
+  if (static_cast<long long>(n_tokens) * (n_q_heads / p->n_kv_heads) > 65535 * 32) return false;
   if (length > (1 << 30) || static_cast<long long>(p->n_seqs) * p->n_kv_heads > kIntMax / 64) return false;
   if (n_tokens > 0 && static_cast<long long>(p->n_seqs) * n_tokens > (1ll << 30) / n_q_heads) return false;
   AttendArgs a;

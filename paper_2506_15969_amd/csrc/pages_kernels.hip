@@ -41,7 +41,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = 0x1p12f;         // a sum of weights beyond this raises the reference
 constexpr float kHuge = 0x1p24f;        // of references beyond this the rounding exceeds 1 (see exponent_of)
-constexpr int kSplitMax = 256;
+constexpr int kSplitMax = 128;
 
 template <typename T, int D>
 struct Rows {
@@ -103,10 +103,17 @@ struct RowPlace {
   int head, kvh;                    // head: within the KV head's group
   long long row;                    // token * n_q_heads + query head
 };
+// x / y for 0 <= x < 2^24, y > 0 (the rounded quotient is off by one at most).
+__device__ __forceinline__ int quotient(int x, int y) {
+  int q = static_cast<int>(static_cast<float>(x) * __builtin_amdgcn_rcpf(static_cast<float>(y)));
+  const int r = x - q * y;
+  q += r >= y ? 1 : 0;
+  return q - (r < 0 ? 1 : 0);
+}
 __device__ __forceinline__ RowPlace row_place(const AttendArgs &a, int unit, int r) {
   RowPlace p;
-  const int seq = unit / a.n_kv_heads, i = r / a.group;
-  p.kvh = unit % a.n_kv_heads;
+  const int seq = a.n_seqs == 1 ? 0 : unit / a.n_kv_heads, i = quotient(r, a.group);
+  p.kvh = unit - seq * a.n_kv_heads;
   p.head = r - i * a.group;
   p.token = seq * a.n_tokens + i;
   p.row = static_cast<long long>(p.token) * a.n_q_heads + p.kvh * a.group + p.head;
@@ -228,12 +235,11 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
   const int wr = wave % kWR, wk = wave / kWR;
-  const int units = a.n_seqs * a.n_kv_heads, M = a.n_tokens * a.group;
-  // late rows first: where a token sees its past only, they have the most to do
-  const int spans = (M + 32 * kWR - 1) / (32 * kWR);
-  const int b = static_cast<int>(blockIdx.x);
-  const int unit = b % units, split = b / units % a.n_split, span = spans - 1 - b / units / a.n_split;
-  const int seq = unit / a.n_kv_heads, kvh = unit % a.n_kv_heads;
+  const int M = a.n_tokens * a.group;
+  // (blocks of one unit, split and so on are as far from one another as there are units: those of eight units, or four, share
+  // an XCD and its L2.)  Late rows first: where a token sees its past only, they have the most to do
+  const int unit = static_cast<int>(blockIdx.x), split = static_cast<int>(blockIdx.y), span = static_cast<int>(gridDim.z - 1 - blockIdx.z);
+  const int seq = a.n_seqs == 1 ? 0 : unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
   const int r0 = (span * kWR + wr) * 32;           // this wave's rows
   const bool have = r0 < M;
   const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
@@ -245,10 +251,12 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
   if (!have) seen = 0;
   int most = seen, least = seen;
+  if (a.visible) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    most = max(most, __shfl_xor(most, o));
-    least = min(least, __shfl_xor(least, o));
+    for (int o = 1; o < 32; o <<= 1) {
+      most = max(most, __shfl_xor(most, o));
+      least = min(least, __shfl_xor(least, o));
+    }
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
@@ -301,9 +309,11 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
 
   // Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as the compiler has every read of
   // LDS wait for all loads into it: they leave nothing in registers, and the waits for them are in `arrived`.)
+  const bool once = gridDim.z == 1;                // nobody else reads these entries (uniform): they need not stay in the caches
   const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
   auto load_1k = [&](const char *from, unsigned to) __attribute__((always_inline)) {
-    __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+    if (once) __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
+    else __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
   };
   auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
     const int e0 = first + st * kKeys;
@@ -444,7 +454,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     Weights p[kSub];
 #pragma unroll
     for (int x = 0; x < kSub; ++x) logits(ks, 32 * x, s[x]);
-    ahead<kSub * kOps, R::kF32 ? 4 : 1, 1, 4>();
+    ahead<kSub * kOps, R::kF32 ? 4 : 1, 1, R::kF32 ? 2 : 4>();
     const bool mask = holes || key0 + 32 * kSub > min(least, last);
     if (mask) {
       const int limit = min(seen, last) - key0 - 4 * h;
@@ -623,29 +633,28 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   if (wk == 0 && h == 0) finish_row(a, place, j);
 }
 
-// The splits of 32 rows joined: blocks = unit, 32 rows and 32 columns; four groups of 256 threads take every fourth split.
-constexpr int kMergeBlock = 1024;
-template <typename T, int D>
-__global__ __launch_bounds__(kMergeBlock) void attend_merge_kernel(const AttendArgs a) {
-  constexpr int kTiles = D / 32, kGroups = 4, kBatch = 8;
-  __shared__ float ml[kSplitMax * 64];
-  __shared__ f32x4_t sums[kGroups - 1][256];
+// The splits of 32 rows joined: blocks = unit and 32 rows (x), 32 columns (y); kGroups groups of 256 threads take every kGroups-th
+// of up to kMost splits each.
+template <typename T, int D, int kGroups, int kMost>
+__global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const AttendArgs a) {
+  constexpr int kTiles = D / 32, kBatch = 8;
+  __shared__ float ml[kMost * 64];
+  __shared__ f32x4_t sums[kGroups > 1 ? kGroups - 1 : 1][256];
   __shared__ float lsums[kGroups][32];
   const int lane = threadIdx.x & 63, i = threadIdx.x >> 6 & 3, g = threadIdx.x >> 8;
   const int c = lane & 31, h = lane >> 5;
   const int M = a.n_tokens * a.group, tiles = (M + 31) / 32, n = a.n_split;
-  const int t = static_cast<int>(blockIdx.x) % kTiles, ut = static_cast<int>(blockIdx.x) / kTiles;
-  const int unit = ut / tiles, r0 = ut % tiles * 32;
+  const int t = static_cast<int>(blockIdx.y), ut = static_cast<int>(blockIdx.x);
   const size_t p0 = static_cast<size_t>(ut) * n;
   const f32x4_t *from = reinterpret_cast<const f32x4_t *>(a.part_o) + p0 * (4 * kTiles * 64) + (4 * t + i) * 64 + lane;
   f32x4_t x[kBatch];
-  auto load = [&](int s0) {
+  auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) x[k] = from[static_cast<size_t>(min(s0 + k * kGroups, n - 1)) * (4 * kTiles * 64)];
   };
+  for (int k = threadIdx.x; k < n * 64; k += 256 * kGroups) ml[k] = a.part_ml[p0 * 64 + k];
   load(g);
   const float lse_other = a.part_lse[static_cast<size_t>(ut) * 32 + c];
-  for (int k = threadIdx.x; k < n * 64; k += kMergeBlock) ml[k] = a.part_ml[p0 * 64 + k];
   __syncthreads();
   float m = -FLT_MAX;
   for (int s = 0; s < n; ++s) m = fmaxf(m, ml[s * 64 + c]);
@@ -659,46 +668,91 @@ __global__ __launch_bounds__(kMergeBlock) void attend_merge_kernel(const AttendA
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int s = s0 + k * kGroups;
-      if (s >= n) break;
-      const float w = __builtin_amdgcn_exp2f(ml[s * 64 + c] - m);
-      l = fmaf(ml[s * 64 + 32 + c], w, l);
-      sum += y[k] * w;
+      if (s < n) {                                 // (uniform)
+        const float w = __builtin_amdgcn_exp2f(ml[s * 64 + c] - m);
+        l = fmaf(ml[s * 64 + 32 + c], w, l);
+        sum += y[k] * w;
+      }
     }
   }
-  if (i == 0 && h == 0) lsums[g][c] = l;
-  if (g > 0) sums[g - 1][threadIdx.x & 255] = sum;
-  __syncthreads();
-  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
-  if (g > 0 || r0 + c >= M || !takes_part(a, place.token)) return;
+  if constexpr (kGroups > 1) {
+    if (i == 0 && h == 0) lsums[g][c] = l;
+    if (g > 0) sums[g - 1][threadIdx.x & 255] = sum;
+    __syncthreads();
+    if (g > 0) return;
+    l = 0.f;
 #pragma unroll
-  for (int k = 0; k < kGroups - 1; ++k) sum += sums[k][threadIdx.x];
-  l = (lsums[0][c] + lsums[1][c]) + (lsums[2][c] + lsums[3][c]);
+    for (int k = 0; k < kGroups; ++k) l += lsums[k][c];
+#pragma unroll
+    for (int k = 0; k < kGroups - 1; ++k) sum += sums[k][threadIdx.x];
+  }
+  const int unit = tiles == 1 ? ut : ut / tiles, r0 = (ut - unit * tiles) * 32;
+  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  if (r0 + c >= M || !takes_part(a, place.token)) return;
   const Joined j = join(m, l, lse_other);
   finish4<T, D>(a, place, 32 * t + 8 * i + 4 * h, sum, j);
   if (t == 0 && i == 0 && h == 0) finish_row(a, place, j);
 }
 
-// How a call is cut: rows of a block, waves that share rows, entries of a stage, splits of the entries.
+// How a call is cut: rows of a block (32 wr), waves that share rows, entries of a stage, splits of the entries.
 struct Plan { int wr, wk, keys, n_split, split_keys; };
+
+// The shapes of blocks, and what a stage of theirs takes on a full chip of 256 (us; rows of 128 x bf16).  More rows in a block
+// share an entry's way to LDS, and a wave with 64 entries a stage has two chains of products; fewer rows make more blocks of few
+// tokens without splits.  The cheapest by the sum of these is taken: stages one after the other, or the bytes where they take longer, a
+// fixed part, and for splits a second launch that reads what the first left (16 KB for 32 rows and split).  Measured, us, 128 x bf16,
+// (32 wr rows, wk) and splits:
+//   4 KV heads,  224 rows,   8192 entries  (64, 4) x 16 21.5   (128, 2) x 32 22.8   (256, 1) x 32 25.2
+//   4 KV heads,  512 rows,   8192          (64, 4) x  8 25.7   (128, 2) x 16 27.8   (256, 1) x 16 33.2
+//   4 KV heads, 2048 rows,   4096          (64, 4) x  2 36.7   (128, 2) x  4 33.6   (256, 1) x  4 43.3
+//   4 KV heads, 4480 rows,   4096          (64, 4) x  1 99.8   (128, 2) x  3 64.0   (256, 1) x  3 55.7
+//   8 KV heads, 20480 rows, their past     (64, 4) x  1 299    (128, 2) x  1 214    (256, 1) x  1 193.5
+//   8 KV heads,   80 rows, 100003          (64, 4) x 16 107    (128, 2) x 32 81.7   (256, 1) x 32 89.4
+struct BlockShape { int wr, wk, keys; float stage_us; };
+template <typename T, int D>
+struct Shapes {
+  static constexpr int kBytes = D * static_cast<int>(sizeof(T));
+  static constexpr float kCost = sizeof(T) == 4 ? (D == 128 ? 8.f : 4.f) : D == 128 ? 1.f : 0.6f;   // (fp32 products run at a sixteenth of the rate)
+};
+// fp32 rows of 128 (512 bytes): fewer entries a stage, and waves, than LDS and registers hold of the others
+constexpr BlockShape kShapes[] = {{1, 4, 128, 1.2f}, {2, 4, 128, 1.65f}, {4, 2, 128, 2.1f}, {8, 1, 64, 1.9f}};
+constexpr BlockShape kShapesLong[] = {{2, 2, 64, 1.2f}, {4, 1, 64, 2.0f}};
 
 template <typename T, int D>
 Plan plan_of(const AttendArgs &a) {
-  constexpr bool kLong = D * sizeof(T) == 512;     // (fewer entries a stage, and waves, than LDS and registers hold of other rows)
-  const long long M = static_cast<long long>(a.n_tokens) * a.group, units = static_cast<long long>(a.n_seqs) * a.n_kv_heads;
-  Plan p;
-  if (M <= 32) p = {1, kLong ? 2 : 4, kLong ? 64 : 128, 1, 0};
-  else if (M <= 64) p = {2, 2, 64, 1, 0};
-  else if (M <= 128 || kLong) p = {4, 1, 64, 1, 0};
-  else p = {8, 1, 64, 1, 0};
-  const long long blocks = units * ((M + 32 * p.wr - 1) / (32 * p.wr));
-  long long n = 512 / blocks;
-  const long long most = (a.length + p.keys - 1) / p.keys;
-  n = n > most ? most : n;
-  n = n > kSplitMax ? kSplitMax : n < 1 ? 1 : n;
-  const long long stages = (most + n - 1) / n;
-  p.split_keys = static_cast<int>((stages < 1 ? 1 : stages) * p.keys);
-  p.n_split = a.length > 0 ? (a.length + p.split_keys - 1) / p.split_keys : 1;
-  return p;
+  constexpr bool kLong = Shapes<T, D>::kBytes == 512;
+  const BlockShape *shapes = kLong ? kShapesLong : kShapes;
+  const int n_shapes = kLong ? 2 : 4;
+  const int M = a.n_tokens * a.group, units = a.n_seqs * a.n_kv_heads, tiles = (M + 31) / 32;
+  const float bytes_us = 2.f * units * a.length * Shapes<T, D>::kBytes / 5.4e6f;
+  Plan best = {0, 0, 0, 1, 0};
+  float best_us = FLT_MAX;
+  for (int i = 0; i < n_shapes; ++i) {
+    const BlockShape &s = shapes[i];
+    if (i > 0 && 32 * shapes[i - 1].wr >= M) break;            // (rows enough for the shape before)
+    if (i + 1 < n_shapes && M > 32 * s.wr * 64) continue;      // (far more rows than blocks of few are for)
+    const long long blocks = static_cast<long long>(units) * ((M + 32 * s.wr - 1) / (32 * s.wr));
+    const int stages = a.length > 0 ? (a.length + s.keys - 1) / s.keys : 1;
+    const int fill = static_cast<int>(256 / blocks);
+    for (int k = 0; k < 4; ++k) {                              // splits: none, half a chip of blocks, one chip, two
+      int n = k == 0 ? 1 : k == 1 ? fill / 2 : k == 2 ? fill : static_cast<int>(512 / blocks);
+      n = n > stages ? stages : n;
+      n = n > kSplitMax ? kSplitMax : n;
+      if (n < (k == 0 ? 1 : 2)) continue;
+      const int each = (stages + n - 1) / n;
+      n = (stages + each - 1) / each;
+      const float full = static_cast<float>(blocks) * n / 256.f;
+      const float rounds = full > 3.f ? full : full > 2.f ? 3.f : full > 1.f ? 2.f : 1.f;
+      const float work = rounds * each * s.stage_us * Shapes<T, D>::kCost;
+      const float join = n > 1 ? 4.f + 0.04f * n + 2.f * units * tiles * n * (32.f * D * 4.f) / 5e6f : 0.f;
+      const float us = 7.f + (work > bytes_us ? work : bytes_us) + join;
+      if (us < best_us) {
+        best_us = us;
+        best = {s.wr, s.wk, s.keys, n, each * s.keys};
+      }
+    }
+  }
+  return best;
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -713,16 +767,16 @@ size_t bytes_of(const AttendArgs &a, const Plan &p) {
 
 template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
 hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
-  const long long M = static_cast<long long>(a.n_tokens) * a.group;
-  const long long grid = static_cast<long long>(a.n_seqs) * a.n_kv_heads * a.n_split * ((M + 32 * kWR - 1) / (32 * kWR));
-  if (grid > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kBufs>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWR * kWK), 0, stream, a);
+  const long long M = static_cast<long long>(a.n_tokens) * a.group, spans = (M + 32 * kWR - 1) / (32 * kWR);
+  if (spans > 65535) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(a.n_seqs * a.n_kv_heads), static_cast<unsigned>(a.n_split), static_cast<unsigned>(spans));
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kBufs>), grid, dim3(64 * kWR * kWK), 0, stream, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch(AttendArgs a, hipStream_t stream) {
-  constexpr bool kLong = D * sizeof(T) == 512;
+  constexpr bool kLong = Shapes<T, D>::kBytes == 512;
   const Plan p = plan_of<T, D>(a);
   a.n_split = p.n_split;
   a.split_keys = p.split_keys;
@@ -737,15 +791,22 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
     w += align_up(parts * 64 * sizeof(float));
     a.part_lse = reinterpret_cast<float *>(w);
   }
-  hipError_t e;
-  if (p.wr == 1) e = launch_shape<T, D, 1, kLong ? 2 : 4, kLong ? 64 : 128, 2>(a, stream);
-  else if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64, 2>(a, stream);
-  else if (kLong || p.wr == 4) e = launch_shape<T, D, 4, 1, 64, 2>(a, stream);
-  else e = launch_shape<T, D, kLong ? 4 : 8, 1, 64, kLong ? 2 : 3>(a, stream);
+  hipError_t e = hipErrorInvalidValue;
+  if constexpr (kLong) {
+    if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64, 2>(a, stream);
+    else if (p.wr == 4) e = launch_shape<T, D, 4, 1, 64, 2>(a, stream);
+  } else {
+    if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128, 2>(a, stream);
+    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128, 2>(a, stream);
+    else if (p.wr == 4) e = launch_shape<T, D, 4, 2, 128, 2>(a, stream);
+    else if (p.wr == 8) e = launch_shape<T, D, 8, 1, 64, 2>(a, stream);
+  }
   if (e != hipSuccess || p.n_split <= 1) return e;
-  const size_t blocks = tiles_of(a) * (D / 32);
+  const size_t blocks = tiles_of(a);
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((attend_merge_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kMergeBlock), 0, stream, a);
+  const dim3 grid(static_cast<unsigned>(blocks), D / 32);
+  if (p.n_split <= 16) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 16>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((attend_merge_kernel<T, D, 4, kSplitMax>), grid, dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 

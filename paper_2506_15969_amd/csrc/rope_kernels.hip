@@ -197,10 +197,12 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
   const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
   const int heads = a.rows[0].heads + a.rows[1].heads;
-  // Four tokens a block, a wave each, with four times its heads at once, or a single one with its heads dealt to more blocks and waves where
-  // that would leave the chip's 256 compute units without eight blocks each
-  if (tokens >= 4 * 2048) {
-    hipLaunchKernelGGL((rope_kernel<T, D, 4, 4, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
+  // Four tokens a block, a wave each, with twice its heads at once, or a single one with its heads dealt to more blocks and waves where
+  // that would be fewer than two blocks for each of the chip's 256 compute units.  us, one / four tokens a block: 28 / 4 heads of 128 x bf16 x
+  // 32 tokens 3.7 / 7.8, 500 5.3 / 8.4, 2000 11.4 / 11.6, 5000 21.4 / 19.6; 8192 of 40 / 8 48.4 / 45.6; 16384 appended of 8 (key and value) heads 47.2 / 30.8.
+  // (More loads of a wave at once take more registers than they hide: four instead of two 46.6 and 32.1 in the last two.)
+  if (tokens >= 2048) {
+    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
   } else {
     const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
     const int want = static_cast<int>((2048 + tokens - 1) / tokens);
