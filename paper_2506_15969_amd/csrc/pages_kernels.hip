@@ -745,7 +745,8 @@ Plan plan_of(const AttendArgs &a) {
       const float rounds = full > 3.f ? full : full > 2.f ? 3.f : full > 1.f ? 2.f : 1.f;
       const float work = rounds * each * s.stage_us * Shapes<T, D>::kCost;
       const float join = n > 1 ? 4.f + 0.04f * n + 2.f * units * tiles * n * (32.f * D * 4.f) / 5e6f : 0.f;
-      const float us = 7.f + (work > bytes_us ? work : bytes_us) + join;
+      const float read = bytes_us / (full < 1.f ? full : 1.f);
+      const float us = 7.f + (work > read ? work : read) + join;
       if (us < best_us) {
         best_us = us;
         best = {s.wr, s.wk, s.keys, n, each * s.keys};

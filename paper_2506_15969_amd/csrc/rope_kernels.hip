@@ -5,10 +5,13 @@
 //
 // A head is L lanes of 16 bytes; the sum of squares is joined over the L lanes and the partner of an element that is
 // turned with the other half's comes from its lane by a permutation, all on fp32 values that never leave the registers.
-// A block takes kTokens tokens (one, where that gives too few blocks) and a share of their heads.  The angle's sine and
-// cosine are the same for all heads of a token: each is worked out once in the block, one pair per thread, and kept in LDS.  The
+// The angle's sine and cosine are the same for all heads of a token: each is worked out once in the block, one pair per
+// thread, and kept in LDS.  The
 // angle is needed modulo a turn only: the product position * inv_freq / 2 pi in binary64 has 2^-52 of itself as its error,
 // so that its fraction is good to 1e-9 at positions of millions, where an fp32 angle is off by a tenth of a turn.
+//
+// Bound by memory: 8192 tokens of 40 + 8 heads of 128 x bf16 (201 MB read and written) 45.6 us, 4.4 TB/s; 16384 tokens appended
+// of 8 heads (134 MB) 30.8 us, 4.4 TB/s; a copy of 1 GiB reaches 5.2 on the same card.
 #include "kernels.h"
 #include "lazyev.h"
 
@@ -74,16 +77,19 @@ __device__ __forceinline__ void store_chunk(T *p, const u32x4_t &w) {
 }
 
 // grid: x = spans of kTokens tokens (of all sequences in a row), y = shares of their heads.  A wave takes kBatch times its
-// heads at once: their loads are on their way together, the first ones while the sines and cosines are worked out.
+// heads at once: their loads are on their way together, the first ones while the sines and cosines are worked out.  Up to
+// four tokens a block: a wave's L-lane groups take heads of one token.  More: each group has a token of its own.
 template <typename T, int D, int kTokens, int kBatch, bool kVec>
 __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
   constexpr int E = Chunk<T>::kElems, L = D / E, kRows = 64 / L;   // elements and lanes of a chunk / a head, heads of a wave
-  constexpr int kWavesPerToken = kWaves / kTokens;
+  constexpr bool kOwnToken = kTokens > kWaves;     // a token for every group
+  static_assert(!kOwnToken || kTokens == kWaves * kRows, "");
+  constexpr int kWavesPerToken = kOwnToken ? 1 : kWaves / kTokens;
   __shared__ float2 turn[kTokens][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tokens = a.n_seqs * a.n_tokens;
   const int token0 = static_cast<int>(blockIdx.x) * kTokens;
-  const int my_k = kTokens == 1 ? 0 : wave / kWavesPerToken;
+  const int my_k = kOwnToken ? wave * kRows + lane / L : kTokens == 1 ? 0 : wave / kWavesPerToken;
   const int tk = min(token0 + my_k, tokens - 1);   // (a wave without a token works on the last one and leaves nothing)
   const int seq = a.n_seqs == 1 ? 0 : tk / a.n_tokens, token = tk - seq * a.n_tokens;
   const int li = lane % L, e0 = li * E;            // this lane's elements of a head: e0 .. e0 + E - 1
@@ -95,9 +101,10 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
     in[s] = static_cast<const T *>(a.rows[s].in) + (seq * a.rows[s].in_seq + token * a.rows[s].in_token) + e0;
     out[s] = static_cast<T *>(a.rows[s].out) + (a.pages.table ? 0 : seq * a.rows[s].out_seq + token * a.rows[s].out_token) + e0;
   }
-  constexpr int kStep = kRows * kWavesPerToken;
+  constexpr int kStep = kOwnToken ? 1 : kRows * kWavesPerToken;
   const int step = kStep * static_cast<int>(gridDim.y);
-  int h0 = (static_cast<int>(blockIdx.y) * kWavesPerToken + wave % kWavesPerToken) * kRows + lane / L;   // this lane's head
+  const int lane_head = kOwnToken ? 0 : lane / L;
+  int h0 = kOwnToken ? static_cast<int>(blockIdx.y) : (static_cast<int>(blockIdx.y) * kWavesPerToken + wave % kWavesPerToken) * kRows + lane_head;   // this lane's head
   u32x4_t raw[kBatch];
   auto load = [&](int first) __attribute__((always_inline)) {
 #pragma unroll
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
     }
   }
   const int partner = halves && turned ? (e0 < a.half ? lane + a.half / E : lane - a.half / E) : lane;
-  for (; h0 - lane / L < n; h0 += kBatch * step) {   // (the same in all lanes)
+  for (; h0 - lane_head < n; h0 += kBatch * step) {   // (the same in all lanes)
     u32x4_t done[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -182,7 +189,7 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
       done[u] = turns || normed ? Chunk<T>::close(x) : raw[u];
     }
     const int next = h0 + kBatch * step;
-    if (next - lane / L < n) load(next);
+    if (next - lane_head < n) load(next);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int at = h0 + u * step;
@@ -197,17 +204,25 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
   const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
   const int heads = a.rows[0].heads + a.rows[1].heads;
-  // Four tokens a block, a wave each, with twice its heads at once, or a single one with its heads dealt to more blocks and waves where
-  // that would be fewer than two blocks for each of the chip's 256 compute units.  us, one / four tokens a block: 28 / 4 heads of 128 x bf16 x
-  // 32 tokens 3.7 / 7.8, 500 5.3 / 8.4, 2000 11.4 / 11.6, 5000 21.4 / 19.6; 8192 of 40 / 8 48.4 / 45.6; 16384 appended of 8 (key and value) heads 47.2 / 30.8.
-  // (More loads of a wave at once take more registers than they hide: four instead of two 46.6 and 32.1 in the last two.)
-  if (tokens >= 2048) {
-    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec>), dim3(static_cast<unsigned>((tokens + 3) / 4)), dim3(kBlock), 0, stream, a);
+  // Three ways, us with one token a block (its heads dealt to four waves, and to more blocks) / four (a wave each) / one for every L
+  // lanes; (128 x bf16, query + key heads x tokens; the last two: appended key and value heads)
+  //   28 + 4 x 32   3.7 / 7.8 /  -      28 + 4 x 500     5.3 / 8.4 /  -      28 + 4 x 5000   21.4 / 19.6 /  -
+  //   40 + 8 x 8192 48.4 / 45.6 / -     1 + 1 x 8000    14.7 / 9.4 / 6.0     1 + 1 x 196608     - / 160.6 / 64.6
+  //   10 + 2 x 2000 7.5 / 7.1 / 12.6    10 + 2 x 16000  41.7 / 29.6 / 24.1   4 + 1 x 4000    10.1 / 6.5 / 8.2
+  //   8 + 8 x 16384 47.2 / 30.8 / -     1 + 1 x 131072     - / 99.5 / 41.1
+  // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
+  // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
+  // for 40 + 8 x 8192, 32.1 for 8 + 8 x 16384.)
+  const unsigned all = static_cast<unsigned>(tokens);
+  if (heads < 4 * kRows && tokens >= 1024ll * heads) {
+    constexpr int kTokens = kWaves * kRows;
+    hipLaunchKernelGGL((rope_kernel<T, D, kTokens, 2, kVec>), dim3((all + kTokens - 1) / kTokens), dim3(kBlock), 0, stream, a);
+  } else if (tokens >= 1536) {
+    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec>), dim3((all + 3) / 4), dim3(kBlock), 0, stream, a);
   } else {
     const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
     const int want = static_cast<int>((2048 + tokens - 1) / tokens);
-    hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec>), dim3(static_cast<unsigned>(tokens), static_cast<unsigned>(shares < want ? shares : want)),
-                       dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec>), dim3(all, static_cast<unsigned>(shares < want ? shares : want)), dim3(kBlock), 0, stream, a);
   }
   return hipGetLastError();
 }
