@@ -244,31 +244,10 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   const bool have = r0 < M;
   const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
 
-  const float lse_other = lse_joined(a, place);
-
-  // entries of this block: first .. end - 1; what its rows see of them
+  // entries of this block: first .. last - 1
   const int first = split * a.split_keys, last = min(first + a.split_keys, a.length);
-  int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
-  if (!have) seen = 0;
-  int most = seen, least = seen;
-  if (a.visible) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      most = max(most, __shfl_xor(most, o));
-      least = min(least, __shfl_xor(least, o));
-    }
-  }
-  most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
   const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
-  // the first window of page numbers
-  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
-  int window_at = page_of(a.pages, first);
-  auto fill_window = [&]() __attribute__((always_inline)) {
-    for (int i = threadIdx.x; i < kWindow && window_at + i <= page_last; i += S::kBlock) window[i] = table[window_at + i];
-  };
-  if (last > first) fill_window();
-
+  // everything that is read before the first stage is worked on is asked for at once
   u32x4_t qb[kOps];
   {
     const T *q = static_cast<const T *>(a.q) + place.row * D + h * (16 / sizeof(T));
@@ -285,9 +264,67 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
       }
     }
   }
+  const float lse_other = lse_joined(a, place);
+  int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
 
-  // ---- stages on their way to LDS
+  // ---- stages on their way to LDS.  Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as
+  // the compiler has every read of LDS wait for all loads into it: they leave nothing in registers, and the waits for
+  // them are in `arrived`.)
+  const bool once = gridDim.z == 1;                // nobody else reads these entries (uniform): they need not stay in the caches
+  const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
+  auto load_1k = [&](const char *from, unsigned to) __attribute__((always_inline)) {
+    if (once) __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
+    else __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+  };
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
+  // Entries from e0 on, none beyond `limit`, to a stage's place; page numbers by number(page of the entry, load).  -> was one of them none?
+  auto load_stage = [&](int e0, int limit, int buf, auto number) __attribute__((always_inline)) {
+    bool hole = false;
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+      const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
+      const int entry = min(e0 + r, limit), pg = page_of(a.pages, entry);
+      unsigned no = static_cast<unsigned>(number(pg, u));
+      if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
+        hole = true;
+        no = 0;
+      }
+      const unsigned in_page = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+      const size_t row = static_cast<size_t>(no * page_rows + in_page) * (D * sizeof(T));
+      const unsigned to = stages_at + buf * S::kStage + (u * S::kWaves + wave) * 1024;
+      load_1k(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16, to);
+      load_1k(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16, to + S::kHalf);
+    }
+    return hole;
+  };
+  // stage 0 before anything else is known of the block (last > first but for no entries at all)
+  bool hole_0 = false;
+  if (last > first) {
+    int page[S::kLoads];
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) page[u] = table[page_of(a.pages, min(first + (u * S::kWaves + wave) * S::kPerLoad + lane / C, last - 1))];
+    hole_0 = load_stage(first, last - 1, 0, [&](int, int u) __attribute__((always_inline)) { return page[u]; });
+  }
+  // the first window of page numbers
+  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
+  int window_at = page_of(a.pages, first);
+  auto fill_window = [&]() __attribute__((always_inline)) {
+    for (int i = threadIdx.x; i < kWindow && window_at + i <= page_last; i += S::kBlock) window[i] = table[window_at + i];
+  };
+  if (last > first) fill_window();
+
+  // what the block's rows see of the entries
+  if (!have) seen = 0;
+  int most = seen, least = seen;
+  if (a.visible) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      most = max(most, __shfl_xor(most, o));
+      least = min(least, __shfl_xor(least, o));
+    }
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
   if (lane == 0) {
     shared_most[wave] = most;
     shared_least[wave] = have ? least : a.length;
@@ -295,6 +332,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   if (threadIdx.x < kBufs) shared_hole[threadIdx.x] = 0;
   if (threadIdx.x == 0) shared_odd = 0;
   __syncthreads();
+  if (hole_0) shared_hole[0] = 1;
   int end = 0, block_least = a.length;
 #pragma unroll
   for (int w = 0; w < S::kWaves; ++w) {
@@ -307,14 +345,6 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
   const int clean_from = max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
   int cleaned = INT_MAX;                           // ... and the first one that was cleaned
 
-  // Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as the compiler has every read of
-  // LDS wait for all loads into it: they leave nothing in registers, and the waits for them are in `arrived`.)
-  const bool once = gridDim.z == 1;                // nobody else reads these entries (uniform): they need not stay in the caches
-  const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
-  auto load_1k = [&](const char *from, unsigned to) __attribute__((always_inline)) {
-    if (once) __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
-    else __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
-  };
   auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
     const int e0 = first + st * kKeys;
     if (page_of(a.pages, min(e0 + kKeys, end) - 1) >= window_at + kWindow) {   // (uniform)
@@ -323,22 +353,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
       fill_window();
       __syncthreads();
     }
-    bool hole = false;
-#pragma unroll
-    for (int u = 0; u < S::kLoads; ++u) {
-      const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
-      const int entry = min(e0 + r, end - 1), pg = page_of(a.pages, entry);
-      unsigned no = static_cast<unsigned>(window[pg - window_at]);
-      if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
-        hole = true;
-        no = 0;
-      }
-      const unsigned in_page = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
-      const size_t row = static_cast<size_t>(no * page_rows + in_page) * (D * sizeof(T));
-      const unsigned to = stages_at + buf * S::kStage + (u * S::kWaves + wave) * 1024;
-      load_1k(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16, to);
-      load_1k(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16, to + S::kHalf);
-    }
+    const bool hole = load_stage(e0, end - 1, buf, [&](int pg, int) __attribute__((always_inline)) { return window[pg - window_at]; });
     if (hole) shared_hole[buf] = st + 1;           // (by the barrier before the stage is worked on)
   };
   // Waits for this wave's loads of a stage, of which `younger` more stages are on their way behind it, and for the other waves.
@@ -364,7 +379,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[t][x] = 0.f;
   float m = -FLT_MAX, l = 0.f;                     // l: over this lane's entries
-  bool plain = true;                               // (of the wave) no reference beyond kHuge
+  bool plain = true, fresh = true;                 // (of the wave) no reference beyond kHuge; none at all
 
   // Where this lane's operands lie in a stage: of K chunk 2 j + h of entry c of a sub-tile, of V the first entry's part of the
   // columns 32 t ..  All other entries lie at fixed distances (the places among an entry's chunks repeat).
@@ -476,15 +491,24 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
         for (int i = 0; i < 16; ++i)
           s[x][i] = 32 * x + 8 * (i / 4) + i % 4 < limit && (there[x] >> i & 1u) != 0 ? s[x][i] : -INFINITY;
     }
-    float sum = weights(s, p);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > kFar) != 0, 0)) {
+    auto top_of = [&]() __attribute__((always_inline)) {
       float top = s[0][0];
 #pragma unroll
       for (int x = 0; x < kSub; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
+      return max_of_halves(top) * c2;
+    };
+    auto look_for_huge = [&]() __attribute__((always_inline)) { plain = __builtin_amdgcn_ballot_w64(fabsf(m) > kHuge && m != -FLT_MAX) == 0; };
+    if (fresh) {                                   // (wave-uniform) the first entries: no reference yet, and no output
+      fresh = false;
+      m = fmaxf(m, top_of());
+      look_for_huge();
+    }
+    float sum = weights(s, p);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > kFar) != 0, 0)) {
       const bool far = max_of_halves(sum) > kFar;  // (of this row)
-      const float up = far ? fmaxf(m, max_of_halves(top) * c2) : m;
+      const float up = far ? fmaxf(m, top_of()) : m;
       const float keep = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l = far ? l * keep : l;
@@ -492,7 +516,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[t][x] = far ? o[t][x] * keep : o[t][x];
-      plain = __builtin_amdgcn_ballot_w64(fabsf(m) > kHuge && m != -FLT_MAX) == 0;
+      look_for_huge();
       sum = weights(s, p);
     }
     l += sum;
@@ -523,8 +547,9 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
 
   // Stages 0 .. kBufs - 2 are on their way before the first one is worked on; one barrier a stage: behind it the stage is
   // complete and the one before it, whose place the next load takes, no longer read.
+  if (n_stages == 0) arrived(0);                   // (nobody sees an entry: stage 0 is not for a later block's LDS)
 #pragma unroll
-  for (int st = 0; st < kBufs - 1; ++st)
+  for (int st = 1; st < kBufs - 1; ++st)
     if (st < n_stages) fetch(st, st);
   int buf = 0;
 #pragma unroll 1
@@ -709,22 +734,28 @@ struct Plan { int wr, wk, keys, n_split, split_keys; };
 //   8 KV heads, 20480 rows, their past     (64, 4) x  1 299    (128, 2) x  1 214    (256, 1) x  1 193.5
 //   8 KV heads,   80 rows, 100003          (64, 4) x 16 107    (128, 2) x 32 81.7   (256, 1) x 32 89.4
 struct BlockShape { int wr, wk, keys; float stage_us; };
+// (fp32 products run at a sixteenth of the rate of bf16 ones: a stage is a wave's products.  fp32 rows of 128: fewer entries a stage, and
+// waves, than LDS and registers hold of the others.)
 template <typename T, int D>
 struct Shapes {
-  static constexpr int kBytes = D * static_cast<int>(sizeof(T));
-  static constexpr float kCost = sizeof(T) == 4 ? (D == 128 ? 8.f : 4.f) : D == 128 ? 1.f : 0.6f;   // (fp32 products run at a sixteenth of the rate)
+  static constexpr BlockShape kAll[] = {{1, 4, 128, D == 128 ? 2.0f : 1.2f}, {2, 4, 128, D == 128 ? 1.65f : 1.2f},
+                                        {4, 2, 128, D == 128 ? 2.1f : 1.4f}, {8, 1, 64, D == 128 ? 1.9f : 1.3f}};
 };
-// fp32 rows of 128 (512 bytes): fewer entries a stage, and waves, than LDS and registers hold of the others
-constexpr BlockShape kShapes[] = {{1, 4, 128, 1.2f}, {2, 4, 128, 1.65f}, {4, 2, 128, 2.1f}, {8, 1, 64, 1.9f}};
-constexpr BlockShape kShapesLong[] = {{2, 2, 64, 1.2f}, {4, 1, 64, 2.0f}};
+template <>
+struct Shapes<float, 64> {
+  static constexpr BlockShape kAll[] = {{1, 4, 128, 2.2f}, {2, 4, 128, 4.0f}, {4, 2, 128, 7.8f}, {8, 1, 64, 7.8f}};
+};
+template <>
+struct Shapes<float, 128> {
+  static constexpr BlockShape kAll[] = {{2, 2, 64, 4.0f}, {4, 1, 64, 7.8f}};
+};
 
 template <typename T, int D>
 Plan plan_of(const AttendArgs &a) {
-  constexpr bool kLong = Shapes<T, D>::kBytes == 512;
-  const BlockShape *shapes = kLong ? kShapesLong : kShapes;
-  const int n_shapes = kLong ? 2 : 4;
+  constexpr const auto &shapes = Shapes<T, D>::kAll;
+  constexpr int n_shapes = sizeof(shapes) / sizeof(shapes[0]);
   const int M = a.n_tokens * a.group, units = a.n_seqs * a.n_kv_heads, tiles = (M + 31) / 32;
-  const float bytes_us = 2.f * units * a.length * Shapes<T, D>::kBytes / 5.4e6f;
+  const float bytes_us = 2.f * units * a.length * (D * sizeof(T)) / 5.4e6f;
   Plan best = {0, 0, 0, 1, 0};
   float best_us = FLT_MAX;
   for (int i = 0; i < n_shapes; ++i) {
@@ -743,10 +774,9 @@ Plan plan_of(const AttendArgs &a) {
       n = (stages + each - 1) / each;
       const float full = static_cast<float>(blocks) * n / 256.f;
       const float rounds = full > 3.f ? full : full > 2.f ? 3.f : full > 1.f ? 2.f : 1.f;
-      const float work = rounds * each * s.stage_us * Shapes<T, D>::kCost;
-      const float join = n > 1 ? 4.f + 0.04f * n + 2.f * units * tiles * n * (32.f * D * 4.f) / 5e6f : 0.f;
-      const float read = bytes_us / (full < 1.f ? full : 1.f);
-      const float us = 7.f + (work > read ? work : read) + join;
+      const float work = rounds * each * s.stage_us;
+      const float join = n > 1 ? 4.f + 0.06f * n + 2.f * units * tiles * n * (32.f * D * 4.f) / 5e6f : 0.f;
+      const float us = 7.f + (work > bytes_us ? work : bytes_us) + join;
       if (us < best_us) {
         best_us = us;
         best = {s.wr, s.wk, s.keys, n, each * s.keys};
@@ -777,7 +807,7 @@ hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
 
 template <typename T, int D>
 hipError_t launch(AttendArgs a, hipStream_t stream) {
-  constexpr bool kLong = Shapes<T, D>::kBytes == 512;
+  constexpr bool kLong = D * sizeof(T) == 512;
   const Plan p = plan_of<T, D>(a);
   a.n_split = p.n_split;
   a.split_keys = p.split_keys;
