@@ -53,7 +53,9 @@ class Case:
 SHAPES = [  # tables, tokens, query and KV heads, page, length
     (1, 1, 1, 1, 16, 1), (1, 1, 7, 1, 16, 15), (2, 1, 28, 4, 16, 17), (1, 5, 8, 8, 24, 64), (1, 3, 14, 2, 16, 1003),
     (1, 32, 28, 4, 64, 500), (3, 33, 8, 2, 48, 257), (1, 20, 32, 1, 128, 333), (2, 10, 64, 1, 1, 70), (1, 1, 8, 8, 32, 9001),
-    (1, 150, 7, 1, 500, 700), (1, 600, 4, 2, 4096, 130), (2, 63, 5, 1, 17, 40), (1, 1, 28, 4, 256, 40000), (1, 257, 2, 2, 64, 129)]
+    (1, 150, 7, 1, 500, 700), (1, 600, 4, 2, 4096, 130), (2, 63, 5, 1, 17, 40), (1, 1, 28, 4, 256, 40000), (1, 257, 2, 2, 64, 129),
+    # many rows: wide blocks, with splits of the entries and without
+    (1, 600, 7, 1, 24, 130), (1, 600, 7, 1, 16, 700), (1, 900, 2, 1, 100, 1100), (1, 4500, 4, 1, 48, 130), (1, 9000, 1, 1, 32, 65), (1, 9000, 1, 1, 64, 700)]
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
@@ -108,7 +110,7 @@ def test_nothing_to_read(lazyev_lib):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("n,length,Hq,H", [(1, 100, 7, 1), (40, 300, 4, 2), (300, 400, 2, 1)])
+@pytest.mark.parametrize("n,length,Hq,H", [(1, 100, 7, 1), (40, 300, 4, 2), (300, 400, 2, 1), (600, 700, 7, 1), (9000, 130, 1, 1)])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 def test_what_a_token_does_not_see_has_no_influence(lazyev_lib, dtype, d, n, length, Hq, H, value):
     """Entries beyond what a token sees hold infinities and NaN, in keys and values; tokens that see such a value have it."""
@@ -149,7 +151,7 @@ def test_what_a_token_does_not_see_has_no_influence(lazyev_lib, dtype, d, n, len
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("n,length,Hq,page", [(1, 200, 7, 16), (2, 2000, 4, 16), (70, 200, 4, 24), (200, 500, 2, 1)])
+@pytest.mark.parametrize("n,length,Hq,page", [(1, 200, 7, 16), (2, 2000, 4, 16), (70, 200, 4, 24), (200, 500, 2, 1), (900, 300, 4, 8), (4500, 130, 2, 16)])
 def test_pages_that_are_none(lazyev_lib, dtype, d, n, length, Hq, page):
     """Numbers outside the pages are not followed: their entries are not there for anybody."""
     c = Case(lazyev_lib, dtype, d, 2, n, Hq, 1, page, length, seed=4)
@@ -172,7 +174,7 @@ def test_pages_that_are_none(lazyev_lib, dtype, d, n, length, Hq, page):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("n,length,Hq", [(1, 3000, 7), (40, 600, 4), (300, 100, 2)])
+@pytest.mark.parametrize("n,length,Hq", [(1, 3000, 7), (40, 600, 4), (300, 100, 2), (600, 700, 7), (9000, 200, 1)])
 def test_large_logits(lazyev_lib, dtype, d, n, length, Hq):
     """Logits that rise and fall by thousands along the entries, so that weights leave the range of 32 bits on the way; all alike; all
     far below zero."""
@@ -209,6 +211,23 @@ def test_places_of_any_element_and_guards(lazyev_lib, dtype, d, n, length):
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
         for b, x in ((bo, out), (bl, lse)):
             assert bool((b[:shifts[1]] == 9).all()) and bool((b[shifts[1] + x.numel():] == 9).all())
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_more_pages_than_a_block_keeps_the_numbers_of(lazyev_lib, dtype, d):
+    """Pages of one entry, more than a thousand of them for every block, some of them none."""
+    n, length = 9000, 2500
+    c = Case(lazyev_lib, dtype, d, 1, n, 4, 1, 1, length, seed=9)
+    vis = torch.randint(0, length + 1, (1, n), generator=c.gen, device="cuda").int()
+    vis[:, n // 2:] = length
+    c.check(c.cache.attend(length, c.q, visible=vis), visible=vis)
+    good = c.table.clone()
+    there = torch.ones((1, length), dtype=torch.bool, device="cuda")
+    there[0, 1100:2400:7] = False
+    c.table[~there] = -1
+    got = c.cache.attend(length, c.q)
+    c.table.copy_(good)
+    c.check(got, there=there)
 
 
 def test_rows_of_the_table_may_share_pages(lazyev_lib):
