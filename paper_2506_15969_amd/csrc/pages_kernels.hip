@@ -209,7 +209,7 @@ __device__ __forceinline__ void ahead() {
 }
 
 // kWR x kWK waves: kWR of 32 rows each, kWK that share the entries of a stage.
-template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
+template <typename T, int D, int kWR, int kWK, int kKeys>
 struct Shape {
   using R = Rows<T, D>;
   static constexpr int kWaves = kWR * kWK, kBlock = 64 * kWaves;
@@ -220,17 +220,17 @@ struct Shape {
   static constexpr int kPerSimd = D * sizeof(T) == 512 ? 1 : 2;   // (fp32 rows of 128: queries and output take 128 registers, the products' operands more)
   static constexpr int kHalf = kKeys * D * static_cast<int>(sizeof(T)), kStage = 2 * kHalf;   // bytes of a stage: of K, then of V
 };
-constexpr int kWindow = 1024;           // page numbers that a block keeps in LDS
+constexpr int kWindow = 512;            // page numbers that a block keeps in LDS
 
-template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
-__global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs>::kPerSimd)) void attend_kernel(const AttendArgs a) {
+template <typename T, int D, int kWR, int kWK, int kKeys>
+__global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPerSimd)) void attend_kernel(const AttendArgs a) {
   using R = Rows<T, D>;
-  using S = Shape<T, D, kWR, kWK, kKeys, kBufs>;
+  using S = Shape<T, D, kWR, kWK, kKeys>;
   constexpr int kSub = S::kSub, kOps = R::kOps, kTiles = R::kTiles, C = R::kChunks;
-  __shared__ __align__(16) char stages[kBufs * S::kStage];
+  __shared__ __align__(16) char stages[2 * S::kStage];
   __shared__ int window[kWindow];
   __shared__ float shared_ml[kWK][kWR][64];
-  __shared__ int shared_most[S::kWaves], shared_least[S::kWaves], shared_hole[kBufs], shared_odd;
+  __shared__ int shared_most[S::kWaves], shared_least[S::kWaves], shared_hole[2], shared_odd;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
@@ -297,21 +297,28 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     }
     return hole;
   };
-  // stage 0 before anything else is known of the block (last > first but for no entries at all)
+  // stage 0 before anything else is known of the block (last > first but for no entries at all), behind the first window of page
+  // numbers: what the compiler waits for after a stage's loads would wait for them too
+  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
+  int window_at = page_of(a.pages, first);
+  auto fill_window = [&]() __attribute__((always_inline)) {
+    int no[kWindow / S::kBlock];
+#pragma unroll
+    for (int i = 0; i < kWindow / S::kBlock; ++i) {
+      const int pg = window_at + i * S::kBlock + static_cast<int>(threadIdx.x);
+      no[i] = pg <= page_last ? table[pg] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kWindow / S::kBlock; ++i) window[i * S::kBlock + threadIdx.x] = no[i];
+  };
   bool hole_0 = false;
   if (last > first) {
     int page[S::kLoads];
 #pragma unroll
     for (int u = 0; u < S::kLoads; ++u) page[u] = table[page_of(a.pages, min(first + (u * S::kWaves + wave) * S::kPerLoad + lane / C, last - 1))];
+    fill_window();
     hole_0 = load_stage(first, last - 1, 0, [&](int, int u) __attribute__((always_inline)) { return page[u]; });
   }
-  // the first window of page numbers
-  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
-  int window_at = page_of(a.pages, first);
-  auto fill_window = [&]() __attribute__((always_inline)) {
-    for (int i = threadIdx.x; i < kWindow && window_at + i <= page_last; i += S::kBlock) window[i] = table[window_at + i];
-  };
-  if (last > first) fill_window();
 
   // what the block's rows see of the entries
   if (!have) seen = 0;
@@ -329,7 +336,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     shared_most[wave] = most;
     shared_least[wave] = have ? least : a.length;
   }
-  if (threadIdx.x < kBufs) shared_hole[threadIdx.x] = 0;
+  if (threadIdx.x < 2) shared_hole[threadIdx.x] = 0;
   if (threadIdx.x == 0) shared_odd = 0;
   __syncthreads();
   if (hole_0) shared_hole[0] = 1;
@@ -356,18 +363,10 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     const bool hole = load_stage(e0, end - 1, buf, [&](int pg, int) __attribute__((always_inline)) { return window[pg - window_at]; });
     if (hole) shared_hole[buf] = st + 1;           // (by the barrier before the stage is worked on)
   };
-  // Waits for this wave's loads of a stage, of which `younger` more stages are on their way behind it, and for the other waves.
-  auto arrived = [&](int younger) __attribute__((always_inline)) {
-    constexpr int kOps2 = 2 * S::kLoads;
-    auto wait = [&](auto n) __attribute__((always_inline)) {   // vmcnt(n), lgkmcnt(0)
-      constexpr int x = decltype(n)::value;
-      __asm__ volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt((x & 15) | 7 << 4 | (x >> 4) << 14);
-    };
-    static_assert((kBufs - 2) * kOps2 < 64, "the counter has six bits");
-    if (kBufs > 3 && younger >= 2) wait(std::integral_constant<int, (kBufs > 3 ? 2 : 0) * kOps2>{});
-    else if (kBufs > 2 && younger >= 1) wait(std::integral_constant<int, (kBufs > 2 ? 1 : 0) * kOps2>{});
-    else wait(std::integral_constant<int, 0>{});
+  // Waits for this wave's loads and for the other waves.
+  auto arrived = [&]() __attribute__((always_inline)) {
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4);            // vmcnt(0), lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     __asm__ volatile("" ::: "memory");
   };
@@ -545,25 +544,20 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     __syncthreads();
   };
 
-  // Stages 0 .. kBufs - 2 are on their way before the first one is worked on; one barrier a stage: behind it the stage is
-  // complete and the one before it, whose place the next load takes, no longer read.
-  if (n_stages == 0) arrived(0);                   // (nobody sees an entry: stage 0 is not for a later block's LDS)
-#pragma unroll
-  for (int st = 1; st < kBufs - 1; ++st)
-    if (st < n_stages) fetch(st, st);
-  int buf = 0;
+  // One barrier a stage: behind it the stage is complete and the one before it, whose place the next load takes, no longer
+  // read.  (A third place, with two stages on their way: 79.5 instead of 81.5 us for 80 rows over 100003 entries of 8 KV heads, the same elsewhere.)
+  if (n_stages == 0) arrived();                    // (nobody sees an entry: stage 0 is not for a later block's LDS)
 #pragma unroll 1
   for (int st = 0; st < n_stages; ++st) {
-    arrived(n_stages - 1 - st);
-    if (st + kBufs - 1 < n_stages) fetch(st + kBufs - 1, buf == 0 ? kBufs - 1 : buf - 1);
-    char *at = stages + buf * S::kStage;
-    const bool holes = __builtin_amdgcn_readfirstlane(shared_hole[buf]) == st + 1;
+    arrived();
+    if (st + 1 < n_stages) fetch(st + 1, (st + 1) & 1);
+    char *at = stages + (st & 1) * S::kStage;
+    const bool holes = __builtin_amdgcn_readfirstlane(shared_hole[st & 1]) == st + 1;
     if (holes || st >= clean_from) {
       cleaned = min(cleaned, st);
       clean(at + S::kHalf);
     }
     work(at, at + S::kHalf, st, holes);
-    buf = buf + 1 == kBufs ? 0 : buf + 1;
   }
   l = sum_of_halves(l);
 
@@ -577,9 +571,9 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
     for (int k = 0; k < kOwn; ++k) part[k] = f32x4_t{o[k / 4][k % 4 * 4], o[k / 4][k % 4 * 4 + 1], o[k / 4][k % 4 * 4 + 2], o[k / 4][k % 4 * 4 + 3]};
   } else {
     // (where the stages were, in rounds of what these hold)
-    constexpr int kAll = S::kWaves * 32 * D * 4, kRounds = (kAll + kBufs * S::kStage - 1) / (kBufs * S::kStage), kPer = kOwn / kRounds;
+    constexpr int kAll = S::kWaves * 32 * D * 4, kRounds = (kAll + 2 * S::kStage - 1) / (2 * S::kStage), kPer = kOwn / kRounds;
     static_assert(kPer * kRounds == kOwn, "whole rounds");
-    static_assert(S::kWaves * kWK * kPer * 64 * 16 <= kBufs * S::kStage, "every wave has a place");
+    static_assert(S::kWaves * kWK * kPer * 64 * 16 <= 2 * S::kStage, "every wave has a place");
     auto place_of_wave = [&](int w) __attribute__((always_inline)) { return reinterpret_cast<f32x4_t *>(stages) + w * (kWK * kPer * 64) + lane; };
     __syncthreads();                               // (every wave is past its last stage)
     shared_ml[wk][wr][lane] = h == 0 ? m : l;
@@ -662,7 +656,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys, kBufs
 // of up to kMost splits each.
 template <typename T, int D, int kGroups, int kMost>
 __global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const AttendArgs a) {
-  constexpr int kTiles = D / 32, kBatch = 8;
+  constexpr int kTiles = D / 32, kBatch = kGroups == 1 ? kMost : 8;   // (one round trip)
   __shared__ float ml[kMost * 64];
   __shared__ f32x4_t sums[kGroups > 1 ? kGroups - 1 : 1][256];
   __shared__ float lsums[kGroups][32];
@@ -675,7 +669,8 @@ __global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const Atten
   f32x4_t x[kBatch];
   auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) x[k] = from[static_cast<size_t>(min(s0 + k * kGroups, n - 1)) * (4 * kTiles * 64)];
+    for (int k = 0; k < kBatch; ++k)
+      if (s0 + k * kGroups < n) x[k] = from[static_cast<size_t>(s0 + k * kGroups) * (4 * kTiles * 64)];   // (uniform)
   };
   for (int k = threadIdx.x; k < n * 64; k += 256 * kGroups) ml[k] = a.part_ml[p0 * 64 + k];
   load(g);
@@ -796,12 +791,12 @@ size_t bytes_of(const AttendArgs &a, const Plan &p) {
   return align_up(parts * 32 * a.head_dim * sizeof(float)) + align_up(parts * 64 * sizeof(float)) + align_up(tiles_of(a) * 32 * sizeof(float));
 }
 
-template <typename T, int D, int kWR, int kWK, int kKeys, int kBufs>
+template <typename T, int D, int kWR, int kWK, int kKeys>
 hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
   const long long M = static_cast<long long>(a.n_tokens) * a.group, spans = (M + 32 * kWR - 1) / (32 * kWR);
   if (spans > 65535) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(a.n_seqs * a.n_kv_heads), static_cast<unsigned>(a.n_split), static_cast<unsigned>(spans));
-  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kBufs>), grid, dim3(64 * kWR * kWK), 0, stream, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys>), grid, dim3(64 * kWR * kWK), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -824,19 +819,20 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
   }
   hipError_t e = hipErrorInvalidValue;
   if constexpr (kLong) {
-    if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64, 2>(a, stream);
-    else if (p.wr == 4) e = launch_shape<T, D, 4, 1, 64, 2>(a, stream);
+    if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64>(a, stream);
+    else if (p.wr == 4) e = launch_shape<T, D, 4, 1, 64>(a, stream);
   } else {
-    if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128, 2>(a, stream);
-    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128, 2>(a, stream);
-    else if (p.wr == 4) e = launch_shape<T, D, 4, 2, 128, 2>(a, stream);
-    else if (p.wr == 8) e = launch_shape<T, D, 8, 1, 64, 2>(a, stream);
+    if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128>(a, stream);
+    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128>(a, stream);
+    else if (p.wr == 4) e = launch_shape<T, D, 4, 2, 128>(a, stream);
+    else if (p.wr == 8) e = launch_shape<T, D, 8, 1, 64>(a, stream);
   }
   if (e != hipSuccess || p.n_split <= 1) return e;
   const size_t blocks = tiles_of(a);
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(blocks), D / 32);
-  if (p.n_split <= 16) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 16>), grid, dim3(256), 0, stream, a);
+  if (p.n_split <= 4) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 4>), grid, dim3(256), 0, stream, a);
+  else if (p.n_split <= 16) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 16>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((attend_merge_kernel<T, D, 4, kSplitMax>), grid, dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
