@@ -286,7 +286,7 @@ int lazyev_score_pairs(const int32_t *delta_t /*device*/, const int32_t *mri /*d
  * belongs to the current device) and return without waiting.  Two calls may run at once, on any streams, if neither writes what
  * the other reads or writes (the workspace of lazyev_pages_attend included).  They can be captured into a HIP graph; a replay
  * works on what the pointers hold then, with the lengths of the captured call.  No alignment beyond the element's
- * is asked for (multiples of 16 bytes are faster) but for the workspace. */
+ * is asked for (multiples of 16 bytes are faster) but for a cache's pages and the workspace. */
 
 /* Heads of the tokens of a batch, head_dim elements each: element e of head h of token i of sequence s lies at
  * rows[s * seq_stride + i * token_stride + h * head_stride + e] (strides in elements, of any sign, so that a head
@@ -332,7 +332,7 @@ int lazyev_norm_rope(int32_t n_seqs, int32_t n_tokens, int32_t head_dim, int32_t
  * calls fill a sequence's prompt (table row {sequence}) and attend over it. */
 typedef struct {
   int32_t n_kv_heads, head_dim, dtype;             /* head_dim 64 or 128                                */
-  int32_t n_pages, page_size;                      /* page_size up to 2^20                              */
+  int32_t n_pages, page_size;                      /* page_size up to 2^20, 2^32 rows of all pages and heads */
   int32_t n_seqs, table_stride;                    /* rows of the table, entries from one to the next   */
   void    *k_pages, *v_pages;                      /* (device) [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
   const int32_t *table;                            /* (device) [n_seqs][table_stride]                   */

@@ -310,13 +310,13 @@ class PagedCache:
                   x.dtype == k_pages.dtype and x.device == k_pages.device and x.numel() > 0,
                   "pages are [n_pages, Hkv, page_size, head_dim], contiguous, fp32 or bf16, on a GPU")
         _need(table.dtype == torch.int32 and table.dim() == 2 and table.numel() > 0 and table.device == k_pages.device and
-              table.stride(1) == 1 and (table.shape[0] == 1 or table.stride(0) >= table.shape[1]),
+              table.stride(1) == 1 and (table.shape[0] == 1 or table.shape[1] <= table.stride(0) < 1 << 31),
               "the table is [S, pages of a row], int32, rows side by side, on the pages' GPU")
         n_pages, heads, page_size, d = k_pages.shape
         _need(d in (64, 128), "rows of 64 or 128 elements")
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
         self.n_q_heads, self.device, self.dtype = n_q_heads, k_pages.device, k_pages.dtype
-        self.entries = table.shape[1] * page_size      # of a row
+        self.entries = min(table.shape[1] * page_size, 1 << 30)   # of a row: entries have 32-bit numbers
         self.pages = Pages(heads, d, _DTYPES[self.dtype], n_pages, page_size, table.shape[0],
                            table.stride(0) if table.shape[0] > 1 else table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr())
 
@@ -334,11 +334,15 @@ class PagedCache:
               "keys and values are [S, n, Hkv, head_dim] of the table's rows")
         n = shape[-3]
         _need(0 <= start and start + n <= self.entries, "entries beyond the table's row")
+        if position0 is None:
+            position0 = start
+        _need(-1 << 31 <= position0 < 1 << 31, "position0 is a 32-bit number")
         hk, hv = rope.heads(k, k, rope.k_weight), rope.heads(v, v, None)
-        code = _launch(self.device, lib.lazyev_pages_append, pg, start, n, hk, hv, rope.rotation, start if position0 is None else position0)
+        code = _launch(self.device, lib.lazyev_pages_append, pg, start, n, hk, hv, rope.rotation, position0)
         _check(code, "lazyev_pages_append")
 
     def workspace_bytes(self, length, n_tokens, n_q_heads=None) -> int:
+        _need(0 <= length <= self.entries, "entries beyond the table's row")
         return lib.lazyev_pages_attend_workspace(self.pages, length, n_tokens, n_q_heads or self.n_q_heads or self.pages.n_kv_heads)
 
     def attend(self, length, q, visible=None, joined=None, out=None, lse=None, scale=0.0, workspace=None):
@@ -378,6 +382,7 @@ class PagedCache:
 
     def _workspace(self, length, n_tokens, n_q_heads, given):
         """(workspace, its bytes) for a call: the given one, or one from torch's allocator for the current stream."""
+        _need(-1 << 31 <= length < 1 << 31, "a length is a 32-bit number")
         if given is not None:
             _need(given.dtype == torch.uint8 and given.is_contiguous() and given.device == self.device, "a workspace is bytes on the pages' GPU")
             return given, given.numel()
@@ -452,6 +457,7 @@ class LazyEviction:
         """lazyev_decode_step_shared: decode_step over the first prefix_len entries of `prefix` (a PagedCache of one
         table row) and the sequences' own caches."""
         cfg = self.cfg
+        _need(prefix.k_pages.get_device() == self.k_cache.get_device(), "the prefix is on the context's GPU")
         with torch.cuda.stream(self.stream):
             workspace, n_bytes = prefix._workspace(prefix_len, cfg.batch, cfg.n_q_heads, workspace)
             code = lib.lazyev_decode_step_shared(self._ctx, layer, t, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),

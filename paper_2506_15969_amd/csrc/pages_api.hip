@@ -15,7 +15,8 @@ bool dtype_ok(int32_t dtype, int32_t head_dim) {
   return (dtype == LAZYEV_DTYPE_FP32 || dtype == LAZYEV_DTYPE_BF16) && (head_dim == 64 || head_dim == 128);
 }
 
-// Pointers start at a whole element (any: there are rows at all); the strides are such that no product with a number of tokens or heads overflows.
+// Pointers start at a whole element (any: there are rows at all); strides beyond any memory are refused, so that no product with a
+// number of tokens or heads that are there overflows.
 bool rows_ok(const lazyev_heads &h, bool has_to, bool any, size_t elem) {
   if (h.n_heads < 1) return false;
   if (!any) return true;
@@ -58,6 +59,8 @@ bool pages_ok(const lazyev_pages *p) {
   if (!p || !dtype_ok(p->dtype, p->head_dim)) return false;
   if (p->n_kv_heads < 1 || p->n_kv_heads > 65535 || p->n_pages < 1 || p->page_size < 1 || p->page_size > (1 << 20)) return false;
   if (p->n_seqs < 1 || p->table_stride < 1) return false;
+  // (a pool's rows have 32-bit numbers; the product of the two is below 2^36)
+  if (p->n_pages > (1ll << 32) / (static_cast<long long>(p->n_kv_heads) * p->page_size)) return false;
   if (!p->k_pages || !p->v_pages || !p->table) return false;
   return reinterpret_cast<uintptr_t>(p->k_pages) % 16 == 0 && reinterpret_cast<uintptr_t>(p->v_pages) % 16 == 0 &&
          reinterpret_cast<uintptr_t>(p->table) % 4 == 0;

@@ -290,3 +290,25 @@ def test_a_cache_beyond_32_bits_of_elements(lazyev_lib):
     want = plain64.attend(q, k, v, torch.full((3,), 2500, device="cuda"), d ** -0.5)
     plain64.check_out(out, want[0], want[2])
     plain64.check_lse(lse, want[1], want[3])
+
+
+def test_numbers_beyond_32_bits_are_refused(lazyev_lib):
+    """A table may have room for more entries than have numbers: such a call is refused, not taken for one of fewer."""
+    b = lazyev_lib
+    page = 1 << 16
+    k = torch.zeros((1, 1, page, 64), dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros((1, (1 << 16) + 1), dtype=torch.int32, device="cuda")
+    cache = b.PagedCache(k, k, table)
+    new = torch.ones((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for entries in ((1 << 32) + 1, (1 << 32), (1 << 31), (1 << 30) + 1, -1):
+        with pytest.raises(ValueError):
+            cache.attend(entries, new)
+        with pytest.raises(ValueError):
+            cache.workspace_bytes(entries, 1)
+        with pytest.raises(ValueError):
+            cache.append(entries, new, new)
+    for position in (1 << 31, 1 << 32, -(1 << 31) - 1):
+        with pytest.raises(ValueError):
+            cache.append(0, new, new, position0=position)
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(k)) == 0

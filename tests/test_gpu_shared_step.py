@@ -145,8 +145,8 @@ def test_without_a_prefix_and_with_one_of_no_pages(lazyev_lib, dtype, d):
 
 
 def test_ranking_by_the_steps_own_weights(lazyev_lib):
-    """Evictions that rank by the weights of their own step take those beside the prefix (one query head to a KV head: another scale
-    of all weights of a unit, so the same survivors as without; the group's heads have different ones)."""
+    """Evictions that rank by the weights of their own step take those beside the prefix: each query head's weights are scaled by a
+    share of its own, so the largest of a group's heads may be another one than without the prefix."""
     w = World(lazyev_lib, "bf16", 128)
     cache, G = w.prefix(), HQ // H
     eng = w.engine(score_flags=lazyev_lib.SCORE_CURRENT_ATTENTION)

@@ -118,3 +118,14 @@ def test_division_by_the_page_size(size):
         n |= {x for x in (m * size - 1, m * size, m * size + 1) if 0 <= x < 1 << 31}
     for x in n:
         assert (x + (x * magic >> 32)) >> shift == x // size and x + (x * magic >> 32) < 1 << 32
+
+
+def test_pools_of_more_rows_than_32_bits_number(lazyev_lib):
+    b = lazyev_lib
+    fits, beyond = dict(n_kv_heads=1 << 10, page_size=1 << 20, n_pages=4), dict(n_kv_heads=1 << 10, page_size=1 << 20, n_pages=5)
+    for over, code in ((fits, b.OK), (beyond, b.EINVAL), (dict(n_kv_heads=65535, page_size=1 << 20, n_pages=0x7FFFFFFF), b.EINVAL)):
+        pages, n = _pages(b, **over), over["n_kv_heads"]
+        assert b.lib.lazyev_pages_attend(pages, 0, 0, n, None, None, None, None, None, None, 0.0, None, 0, None) == code, over
+        heads = _heads(b, n_heads=n)
+        if 2 * n <= 65535:
+            assert b.lib.lazyev_pages_append(pages, 0, 0, heads, heads, _rotation(b), 0, None) == code, over
