@@ -6,12 +6,13 @@
 // A head is L lanes of 16 bytes; the sum of squares is joined over the L lanes and the partner of an element that is
 // turned with the other half's comes from its lane by a permutation, all on fp32 values that never leave the registers.
 // The angle's sine and cosine are the same for all heads of a token: each is worked out once in the block, one pair per
-// thread, and kept in LDS.  The
-// angle is needed modulo a turn only: the product position * inv_freq / 2 pi in binary64 has 2^-52 of itself as its error,
-// so that its fraction is good to 1e-9 at positions of millions, where an fp32 angle is off by a tenth of a turn.
+// thread, and kept in LDS.  The angle is needed modulo a turn only: the product position * inv_freq / 2 pi in binary64 has
+// 2^-52 of itself as its error, so that its fraction is good to 1e-9 at positions of millions, where an fp32 angle is off by a
+// tenth of a turn.
 //
-// Bound by memory: 8192 tokens of 40 + 8 heads of 128 x bf16 (201 MB read and written) 45.6 us, 4.4 TB/s; 16384 tokens appended
-// of 8 heads (134 MB) 30.8 us, 4.4 TB/s; a copy of 1 GiB reaches 5.2 on the same card.
+// Bound by memory: 8192 tokens of 40 + 8 heads of 128 x bf16 (201 MB read and written) 40.3 us, 5.0 TB/s; 16384 tokens appended
+// of 8 heads (134 MB) 25.1 us, 5.3 TB/s; a copy of 1 GiB reaches 5.2 on the same card.  32 tokens of 28 + 4 heads: 3.5 us, of
+// which a kernel that does nothing takes 1.9.
 #include "kernels.h"
 #include "lazyev.h"
 
@@ -64,10 +65,11 @@ __device__ __forceinline__ u32x4_t load_chunk(const T *p) {
   __builtin_memcpy(&w, e, 16);
   return w;
 }
-template <typename T, bool kVec>
+template <typename T, bool kVec, bool kPast>       // kPast: past the caches
 __device__ __forceinline__ void store_chunk(T *p, const u32x4_t &w) {
   if constexpr (kVec) {
-    *reinterpret_cast<u32x4_t *>(p) = w;
+    if constexpr (kPast) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t *>(p));
+    else *reinterpret_cast<u32x4_t *>(p) = w;
     return;
   }
   T e[16 / sizeof(T)];
@@ -194,7 +196,7 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
     for (int u = 0; u < kBatch; ++u) {
       const int at = h0 + u * step;
       const bool second = at >= n0;
-      if (at < n) store_chunk<T, kVec>((second ? out[1] : out[0]) + (second ? at - n0 : at) * (second ? out_head[1] : out_head[0]), done[u]);
+      if (at < n) store_chunk<T, kVec, (kTokens > 1)>((second ? out[1] : out[0]) + (second ? at - n0 : at) * (second ? out_head[1] : out_head[0]), done[u]);
     }
   }
 }
@@ -213,6 +215,8 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
   // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
   // for 40 + 8 x 8192, 32.1 for 8 + 8 x 16384.)
+  // Of many tokens the results go past the caches: 40 + 8 x 2048 15.3 -> 13.2, x 8192 38.2 -> 37.2, x 32768 158 -> 153, 8 + 8 x 16384
+  // 27.0 -> 25.6, x 65536 103 -> 87.4, and the attention that reads 4096 rotated tokens next takes no longer; the one over 300 does (20.9 -> 21.4).
   const unsigned all = static_cast<unsigned>(tokens);
   if (heads < 4 * kRows && tokens >= 1024ll * heads) {
     constexpr int kTokens = kWaves * kRows;
