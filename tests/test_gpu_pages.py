@@ -312,3 +312,33 @@ def test_numbers_beyond_32_bits_are_refused(lazyev_lib):
             cache.append(0, new, new, position0=position)
     torch.cuda.synchronize()
     assert int(torch.count_nonzero(k)) == 0
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n,length,Hq,page", [(1, 300, 7, 16), (50, 1500, 7, 1), (700, 1500, 7, 1), (9000, 1300, 4, 1)])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_values_behind_masks_in_long_rows(lazyev_lib, dtype, d, n, length, Hq, page, value):
+    """Infinities and NaN at the end of what some tokens see, and in the page whose rows stand in for those of pages that are none: the other
+    tokens' bits are the same as without, over more pages than a block keeps the numbers of."""
+    c = Case(lazyev_lib, dtype, d, 1, n, Hq, 1, page, length, seed=11)
+    entries = torch.arange(length, device="cuda") // page
+    c.table[0, ::5] = -1
+    c.table[c.table == 0] = c.k_pages.shape[0]
+    vis = torch.randint(1, length + 1, (1, n), generator=c.gen, device="cuda").int()
+    vis[0, -1] = length - 40
+    want = c.cache.attend(length, c.q, visible=vis)
+    c.k_pages[0], c.v_pages[0] = value, value
+    got = c.cache.attend(length, c.q, visible=vis)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    page_of_last = c.table[0].long()[entries[length - 40:]]
+    place = torch.arange(length - 40, length, device="cuda") % page
+    on = (page_of_last >= 0) & (page_of_last < c.k_pages.shape[0])
+    c.v_pages[page_of_last[on], 0, place[on], ::3] = value
+    got = c.cache.attend(length, c.q, visible=vis)
+    low = vis[0] <= length - 40
+    assert bool(low.any()) and torch.equal(got[1], want[1])
+    assert torch.equal(got[0][0][low], want[0][0][low])
+    first_on = length - 40 + int(on.nonzero()[0])
+    hit = vis[0] > first_on
+    assert bool((~torch.isfinite(got[0][0][hit][:, :, ::3])).all())
+    assert bool(torch.isfinite(got[0][0][..., 1::3]).all())
