@@ -10,8 +10,8 @@
 // 2^-52 of itself as its error, so that its fraction is good to 1e-9 at positions of millions, where an fp32 angle is off by a
 // tenth of a turn.
 //
-// Bound by memory: 8192 tokens of 40 + 8 heads of 128 x bf16 (201 MB read and written) 40.3 us, 5.0 TB/s; 16384 tokens appended
-// of 8 heads (134 MB) 25.1 us, 5.3 TB/s; a copy of 1 GiB reaches 5.2 on the same card.  32 tokens of 28 + 4 heads: 3.5 us, of
+// Bound by memory: 8192 tokens of 40 + 8 heads of 128 x bf16 (201 MB read and written) 40.6 us, 5.0 TB/s; 16384 tokens appended
+// of 8 heads (134 MB) 25.0 us, 5.4 TB/s; a copy of 1 GiB reaches 5.2 on the same card.  32 tokens of 28 + 4 heads: 3.5 us, of
 // which a kernel that does nothing takes 1.9.
 #include "kernels.h"
 #include "lazyev.h"
@@ -81,7 +81,7 @@ __device__ __forceinline__ void store_chunk(T *p, const u32x4_t &w) {
 // grid: x = spans of kTokens tokens (of all sequences in a row), y = shares of their heads.  A wave takes kBatch times its
 // heads at once: their loads are on their way together, the first ones while the sines and cosines are worked out.  Up to
 // four tokens a block: a wave's L-lane groups take heads of one token.  More: each group has a token of its own.
-template <typename T, int D, int kTokens, int kBatch, bool kVec>
+template <typename T, int D, int kTokens, int kBatch, bool kVec, bool kPast>
 __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
   constexpr int E = Chunk<T>::kElems, L = D / E, kRows = 64 / L;   // elements and lanes of a chunk / a head, heads of a wave
   constexpr bool kOwnToken = kTokens > kWaves;     // a token for every group
@@ -196,37 +196,45 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
     for (int u = 0; u < kBatch; ++u) {
       const int at = h0 + u * step;
       const bool second = at >= n0;
-      if (at < n) store_chunk<T, kVec, (kTokens > 1)>((second ? out[1] : out[0]) + (second ? at - n0 : at) * (second ? out_head[1] : out_head[0]), done[u]);
+      if (at < n) store_chunk<T, kVec, kPast>((second ? out[1] : out[0]) + (second ? at - n0 : at) * (second ? out_head[1] : out_head[0]), done[u]);
     }
   }
 }
+
+constexpr long long kPastBytes = 4ll << 20;        // (an XCD's L2)
 
 template <typename T, int D, bool kVec>
 hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
   const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
   const int heads = a.rows[0].heads + a.rows[1].heads;
-  // Three ways, us with one token a block (its heads dealt to four waves, and to more blocks) / four (a wave each) / one for every L
-  // lanes; (128 x bf16, query + key heads x tokens; the last two: appended key and value heads)
-  //   28 + 4 x 32   3.7 / 7.8 /  -      28 + 4 x 500     5.3 / 8.4 /  -      28 + 4 x 5000   21.4 / 19.6 /  -
-  //   40 + 8 x 8192 48.4 / 45.6 / -     1 + 1 x 8000    14.7 / 9.4 / 6.0     1 + 1 x 196608     - / 160.6 / 64.6
-  //   10 + 2 x 2000 7.5 / 7.1 / 12.6    10 + 2 x 16000  41.7 / 29.6 / 24.1   4 + 1 x 4000    10.1 / 6.5 / 8.2
-  //   8 + 8 x 16384 47.2 / 30.8 / -     1 + 1 x 131072     - / 99.5 / 41.1
+  // Three ways, us with one token a block (its heads dealt to four waves, and of few tokens to more blocks) / four (a wave each) / one
+  // for every L lanes; query + key heads x tokens, or appended key and value heads, rows that no cache holds yet:
+  //   128 x bf16  28 + 4 x 32     3.8 /  7.8 / 22.2    28 + 4 x 512   5.8 /  9.4 / 28.1    28 + 4 x 4096  20.0 / 17.7 / 34.8
+  //               40 + 8 x 1024   9.1 / 14.1 / 43.0    40 + 8 x 4096 26.1 / 23.4 / 49.5    56 + 8 x 8192  58.6 / 57.5 / 69.0
+  //               8 + 8 x 2048    8.7 /  7.8 / 17.3    8 + 8 x 65536  157 /  102 / 116     1 + 1 x 8192   16.4 /  9.3 /  6.8
+  //               2 + 2 x 65536   116 / 55.1 / 35.5    1 + 1 x 65536  111 / 51.2 / 23.8
+  //   64 x fp32   12 + 4 x 2048   6.5 /  6.9 /  -      12 + 4 x 4096 11.3 / 10.1 /  -      32 + 8 x 4096  18.1 / 19.8 / 33.9
+  //   128 x fp32  8 + 2 x 2048    7.8 /  8.7 /  -      8 + 2 x 8192  21.7 / 20.2 /  -      32 + 8 x 8192  63.4 / 68.1 / 70.5
   // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
   // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
-  // for 40 + 8 x 8192, 32.1 for 8 + 8 x 16384.)
-  // Of many tokens the results go past the caches: 40 + 8 x 2048 15.3 -> 13.2, x 8192 38.2 -> 37.2, x 32768 158 -> 153, 8 + 8 x 16384
-  // 27.0 -> 25.6, x 65536 103 -> 87.4, and the attention that reads 4096 rotated tokens next takes no longer; the one over 300 does (20.9 -> 21.4).
+  // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)
+  // Results beyond an XCD's L2 go past the caches: 40 + 8 x 512 8.3 -> 7.5, 28 + 4 x 4096 20.0 -> 17.8, 8 + 8 x 65536 106 -> 102, and the
+  // attention that reads 4096 rotated tokens next takes no longer; the one over 300 would (20.9 -> 21.4).
   const unsigned all = static_cast<unsigned>(tokens);
+  const int lanes = heads * (64 / kRows);          // of a token
+  const bool past = tokens * heads * static_cast<long long>(D * sizeof(T)) >= kPastBytes;
   if (heads < 4 * kRows && tokens >= 1024ll * heads) {
     constexpr int kTokens = kWaves * kRows;
-    hipLaunchKernelGGL((rope_kernel<T, D, kTokens, 2, kVec>), dim3((all + kTokens - 1) / kTokens), dim3(kBlock), 0, stream, a);
-  } else if (tokens >= 1536) {
-    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec>), dim3((all + 3) / 4), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((rope_kernel<T, D, kTokens, 2, kVec, true>), dim3((all + kTokens - 1) / kTokens), dim3(kBlock), 0, stream, a);
+  } else if (tokens >= 1536 && (sizeof(T) == 2 ? tokens >= 4ll * lanes : tokens >= 8ll * lanes && lanes <= 384)) {
+    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec, true>), dim3((all + 3) / 4), dim3(kBlock), 0, stream, a);
   } else {
     const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
-    const int want = static_cast<int>((2048 + tokens - 1) / tokens);
-    hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec>), dim3(all, static_cast<unsigned>(shares < want ? shares : want)), dim3(kBlock), 0, stream, a);
+    const int want = static_cast<int>((512 + tokens - 1) / tokens);
+    const dim3 grid(all, static_cast<unsigned>(shares < want ? shares : want));
+    if (past) hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, true>), grid, dim3(kBlock), 0, stream, a);
+    else hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, false>), grid, dim3(kBlock), 0, stream, a);
   }
   return hipGetLastError();
 }

@@ -35,7 +35,7 @@ def _check(got, x, positions, weight, rope, layout):
                                               ("halves", 2, True), ("pairs", 2, False), ("halves", 48, True), ("pairs", 16, True)])
 @pytest.mark.parametrize("S,n,Hq,H", [(1, 1, 1, 1), (1, 32, 28, 4), (3, 7, 5, 5), (2, 2250, 3, 1), (2, 900, 20, 3)])
 def test_heads_against_64_bits(lazyev_lib, dtype, d, layout, dims, norm, S, n, Hq, H):
-    """dims: 0 no rotation, 1 the whole head, 2 half of it.  Of 4500 tokens each lane group has one, 1800 go four to a block."""
+    """dims: 0 no rotation, 1 the whole head, 2 half of it.  Of 4500 tokens each lane group has one; 1800 of bf16 rows go four to a block."""
     dt, gen = _dt(dtype), torch.Generator(device="cuda").manual_seed(n + d)
     dims = {0: 0, 1: d, 2: d // 2}.get(dims, dims)
     rope = _rope(lazyev_lib, dt, d, dims, layout, norm, gen)
@@ -48,6 +48,21 @@ def test_heads_against_64_bits(lazyev_lib, dtype, d, layout, dims, norm, S, n, H
     none, ko = rope(None, k, start=11)             # keys alone, positions in a row
     assert none is None
     _check(ko, k, at, rope.k_weight, rope, layout)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("layout,dims", [("halves", 64), ("pairs", 32)])
+@pytest.mark.parametrize("S,n,Hq,H", [(1, 4099, 9, 3), (5, 820, 10, 1), (1, 1100, 40, 8), (1, 700, 3, 30), (3, 171, 70, 1)])
+def test_many_tokens_of_many_heads(lazyev_lib, dtype, d, layout, dims, S, n, Hq, H):
+    """Four tokens to a block, also where the last block has fewer; one to a block, with results beyond a cache's size and below."""
+    dt, gen = _dt(dtype), torch.Generator(device="cuda").manual_seed(n + d)
+    rope = _rope(lazyev_lib, dt, d, dims, layout, True, gen)
+    qkv = torch.randn((S, n, Hq + 2 * H, d), generator=gen, device="cuda").to(dt)
+    q, k = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H]
+    pos = torch.randint(0, 1 << 16, (S, n), generator=gen, device="cuda").int()
+    qo, ko = rope(q, k, positions=pos)
+    _check(qo, q, pos, rope.q_weight, rope, layout)
+    _check(ko, k, pos, rope.k_weight, rope, layout)
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
