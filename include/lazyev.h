@@ -318,7 +318,8 @@ typedef struct {
 /* Norms of the query and key heads and the rotation by the token's position, in one pass: what lazyev_decode_step and
  * lazyev_prefill_track take their rows after.  Arithmetic in fp32, rounded once to the rows' type.
  * Token i of sequence s is at position start + positions[s * n_tokens + i], or start + i without `positions`.
- * q or k may be null (not both).  head_dim 64 or 128, dtype LAZYEV_DTYPE_*.  n_seqs or n_tokens 0: nothing to do.
+ * q or k may be null (not both).  head_dim 64 or 128, dtype LAZYEV_DTYPE_*.  n_seqs or n_tokens 0: nothing to do; n_seqs * n_tokens
+ * is at most 2^30, here and in lazyev_pages_append.
  * Errors: EINVAL, EHIP. */
 int lazyev_norm_rope(int32_t n_seqs, int32_t n_tokens, int32_t head_dim, int32_t dtype,
                      const lazyev_heads *q /*host, nullable*/, const lazyev_heads *k /*host, nullable*/,
@@ -341,7 +342,7 @@ typedef struct {
 /* Writes the keys and values of n_tokens tokens of every table row to the row's entries start .. start + n_tokens - 1: the keys
  * normed (k->weight) and rotated on the way, by the position position0 + i of the i-th token, the values as they are
  * (v->weight null).  k and v describe the source only: their `to` members are ignored.
- * A page that several of the written entries lead to (one number twice in the table) holds unspecified ones of their rows.
+ * A page that several of the written entries lead to (one number twice in the table) holds unspecified parts of their rows.
  * start + n_tokens <= table_stride * page_size.  Errors: EINVAL, EHIP. */
 int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32_t n_tokens,
                         const lazyev_heads *k /*host*/, const lazyev_heads *v /*host*/,
@@ -358,7 +359,7 @@ int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32
  *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  `out` is not q.
  * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; bf16 weights
  * are rounded to bf16 for the product with V.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times;
- * n_tokens * n_q_heads / n_kv_heads is at most 65535 * 32.
+ * n_tokens * n_q_heads / n_kv_heads is at most 65535 * 32, n_seqs * n_kv_heads 2^22, n_seqs * n_tokens * n_q_heads 2^30, length 2^30.
  * Workspace: lazyev_pages_attend_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).
  * Errors: EINVAL (length 0 .. table_stride * page_size among them), EWORKSPACE, EHIP. */
 int lazyev_pages_attend(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,

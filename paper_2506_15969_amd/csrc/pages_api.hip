@@ -9,8 +9,6 @@
 
 namespace {
 
-constexpr long long kIntMax = 0x7FFFFFFFLL;
-
 bool dtype_ok(int32_t dtype, int32_t head_dim) {
   return (dtype == LAZYEV_DTYPE_FP32 || dtype == LAZYEV_DTYPE_BF16) && (head_dim == 64 || head_dim == 128);
 }
@@ -82,7 +80,8 @@ bool attend_args(const lazyev_pages *p, int32_t length, int32_t n_tokens, int32_
   if (n_q_heads / p->n_kv_heads > 64 || static_cast<long long>(length) > static_cast<long long>(p->table_stride) * p->page_size) return false;
   // (rows and a table row's entries have 32-bit numbers; those of a table row and KV head are cut into at most 65535 blocks)
   if (static_cast<long long>(n_tokens) * (n_q_heads / p->n_kv_heads) > 65535 * 32) return false;
-  if (length > (1 << 30) || static_cast<long long>(p->n_seqs) * p->n_kv_heads > kIntMax / 64) return false;
+  // (a launch has 2^32 threads at most from one end to the other: 512 for each of the two)
+  if (length > (1 << 30) || static_cast<long long>(p->n_seqs) * p->n_kv_heads > (1 << 22)) return false;
   if (n_tokens > 0 && static_cast<long long>(p->n_seqs) * n_tokens > (1ll << 30) / n_q_heads) return false;
   AttendArgs a;
   std::memset(&a, 0, sizeof(a));

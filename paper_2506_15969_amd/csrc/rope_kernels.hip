@@ -218,7 +218,7 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   //   128 x fp32  8 + 2 x 2048    7.8 /  8.7 /  -      8 + 2 x 8192  21.7 / 20.2 /  -      32 + 8 x 8192  63.4 / 68.1 / 70.5
   // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
   // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
-  // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)
+  // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)  A launch has 2^32 threads at most: of 2^24 tokens four share a block.
   // Results beyond an XCD's L2 go past the caches: 40 + 8 x 512 8.3 -> 7.5, 28 + 4 x 4096 20.0 -> 17.8, 8 + 8 x 65536 106 -> 102, and the
   // attention that reads 4096 rotated tokens next takes no longer; the one over 300 would (20.9 -> 21.4).
   const unsigned all = static_cast<unsigned>(tokens);
@@ -227,7 +227,7 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   if (heads < 4 * kRows && tokens >= 1024ll * heads) {
     constexpr int kTokens = kWaves * kRows;
     hipLaunchKernelGGL((rope_kernel<T, D, kTokens, 2, kVec, true>), dim3((all + kTokens - 1) / kTokens), dim3(kBlock), 0, stream, a);
-  } else if (tokens >= 1536 && (sizeof(T) == 2 ? tokens >= 4ll * lanes : tokens >= 8ll * lanes && lanes <= 384)) {
+  } else if (tokens >= 1536 && (sizeof(T) == 2 ? tokens >= 4ll * lanes : (tokens >= 8ll * lanes && lanes <= 384) || tokens >= (1 << 23))) {
     hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec, true>), dim3((all + 3) / 4), dim3(kBlock), 0, stream, a);
   } else {
     const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);

@@ -129,3 +129,10 @@ def test_pools_of_more_rows_than_32_bits_number(lazyev_lib):
         heads = _heads(b, n_heads=n)
         if 2 * n <= 65535:
             assert b.lib.lazyev_pages_append(pages, 0, 0, heads, heads, _rotation(b), 0, None) == code, over
+
+
+def test_more_blocks_than_a_launch_has(lazyev_lib):
+    b = lazyev_lib
+    for seqs, code in ((1 << 20, b.OK), ((1 << 20) + 1, b.EINVAL)):
+        pages = _pages(b, n_seqs=seqs)
+        assert b.lib.lazyev_pages_attend(pages, 1, 0, 4, None, None, None, None, None, None, 0.0, None, 0, None) == code
