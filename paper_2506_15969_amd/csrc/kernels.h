@@ -231,7 +231,15 @@ struct RopeArgs {
   int64_t start;                    // position of token 0, or what is added to `positions`
   PageTable pages;                  // of the results, ...
   int32_t first_entry;              // ... from this entry on
+  // filled in by the launch: the token (of all sequences) that its first block begins with
+  int32_t token0;
 };
+// How the tokens of a call are cut: tokens of a block, shares of a token's heads (a block each), results past the caches or not, tokens of a launch.
+struct RopeCut {
+  int32_t tokens, shares, past;
+  int64_t launch;
+};
+RopeCut rope_cut(long long tokens, int heads, int elem /*bytes*/, int head_dim);
 hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
 
 // Attention over pages (see lazyev_pages_attend).

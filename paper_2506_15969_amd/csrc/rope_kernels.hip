@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
   __shared__ float2 turn[kTokens][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tokens = a.n_seqs * a.n_tokens;
-  const int token0 = static_cast<int>(blockIdx.x) * kTokens;
+  const int token0 = a.token0 + static_cast<int>(blockIdx.x) * kTokens;
   const int my_k = kOwnToken ? wave * kRows + lane / L : kTokens == 1 ? 0 : wave / kWavesPerToken;
   const int tk = min(token0 + my_k, tokens - 1);   // (a wave without a token works on the last one and leaves nothing)
   const int seq = a.n_seqs == 1 ? 0 : tk / a.n_tokens, token = tk - seq * a.n_tokens;
@@ -202,12 +202,13 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(const RopeArgs a) {
 }
 
 constexpr long long kPastBytes = 4ll << 20;        // (an XCD's L2)
+// Blocks of a launch, which has fewer than 2^32 threads from one end to the other; calls of more tokens take several, one after the other.
+constexpr long long kLaunchBlocks = 1ll << 23;
 
-template <typename T, int D, bool kVec>
-hipError_t launch(const RopeArgs &a, hipStream_t stream) {
-  constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
-  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
-  const int heads = a.rows[0].heads + a.rows[1].heads;
+}  // namespace
+
+RopeCut rope_cut(long long tokens, int heads, int elem, int head_dim) {
+  const int row_lanes = head_dim * elem / 16, rows = 64 / row_lanes;   // of a head, heads of a wave
   // Three ways, us with one token a block (its heads dealt to four waves, and of few tokens to more blocks) / four (a wave each) / one
   // for every L lanes; query + key heads x tokens, or appended key and value heads, rows that no cache holds yet:
   //   128 x bf16  28 + 4 x 32     3.8 /  7.8 / 22.2    28 + 4 x 512   5.8 /  9.4 / 28.1    28 + 4 x 4096  20.0 / 17.7 / 34.8
@@ -218,25 +219,47 @@ hipError_t launch(const RopeArgs &a, hipStream_t stream) {
   //   128 x fp32  8 + 2 x 2048    7.8 /  8.7 /  -      8 + 2 x 8192  21.7 / 20.2 /  -      32 + 8 x 8192  63.4 / 68.1 / 70.5
   // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
   // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
-  // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)  A launch has 2^32 threads at most: of 2^24 tokens four share a block.
+  // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)
   // Results beyond an XCD's L2 go past the caches: 40 + 8 x 512 8.3 -> 7.5, 28 + 4 x 4096 20.0 -> 17.8, 8 + 8 x 65536 106 -> 102, and the
   // attention that reads 4096 rotated tokens next takes no longer; the one over 300 would (20.9 -> 21.4).
-  const unsigned all = static_cast<unsigned>(tokens);
-  const int lanes = heads * (64 / kRows);          // of a token
-  const bool past = tokens * heads * static_cast<long long>(D * sizeof(T)) >= kPastBytes;
-  if (heads < 4 * kRows && tokens >= 1024ll * heads) {
-    constexpr int kTokens = kWaves * kRows;
-    hipLaunchKernelGGL((rope_kernel<T, D, kTokens, 2, kVec, true>), dim3((all + kTokens - 1) / kTokens), dim3(kBlock), 0, stream, a);
-  } else if (tokens >= 1536 && (sizeof(T) == 2 ? tokens >= 4ll * lanes : (tokens >= 8ll * lanes && lanes <= 384) || tokens >= (1 << 23))) {
-    hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec, true>), dim3((all + 3) / 4), dim3(kBlock), 0, stream, a);
+  const int lanes = heads * row_lanes;             // of a token
+  RopeCut c;
+  c.past = tokens * heads * (static_cast<long long>(head_dim) * elem) >= kPastBytes;
+  c.shares = 1;
+  if (heads < 4 * rows && tokens >= 1024ll * heads) {
+    c.tokens = kWaves * rows;
+    c.past = true;
+  } else if (tokens >= 1536 && (elem == 2 ? tokens >= 4ll * lanes : tokens >= 8ll * lanes && lanes <= 384)) {
+    c.tokens = 4;
+    c.past = true;
   } else {
-    const int shares = (heads + kRows * kWaves - 1) / (kRows * kWaves);
-    const int want = static_cast<int>((512 + tokens - 1) / tokens);
-    const dim3 grid(all, static_cast<unsigned>(shares < want ? shares : want));
-    if (past) hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, true>), grid, dim3(kBlock), 0, stream, a);
-    else hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, false>), grid, dim3(kBlock), 0, stream, a);
+    c.tokens = 1;
+    const int shares = (heads + rows * kWaves - 1) / (rows * kWaves), want = static_cast<int>((512 + tokens - 1) / tokens);
+    c.shares = shares < want ? shares : want;
   }
-  return hipGetLastError();
+  c.launch = kLaunchBlocks * c.tokens;
+  return c;
+}
+
+namespace {
+
+template <typename T, int D, bool kVec>
+hipError_t launch(RopeArgs a, hipStream_t stream) {
+  constexpr int kRows = 64 / (D * static_cast<int>(sizeof(T)) / 16);
+  const long long tokens = static_cast<long long>(a.n_seqs) * a.n_tokens;
+  const RopeCut c = rope_cut(tokens, a.rows[0].heads + a.rows[1].heads, sizeof(T), D);
+  for (long long first = 0; first < tokens; first += c.launch) {
+    const long long n = tokens - first < c.launch ? tokens - first : c.launch;
+    const dim3 grid(static_cast<unsigned>((n + c.tokens - 1) / c.tokens), static_cast<unsigned>(c.shares));
+    a.token0 = static_cast<int32_t>(first);
+    if (c.tokens == kWaves * kRows) hipLaunchKernelGGL((rope_kernel<T, D, kWaves * kRows, 2, kVec, true>), grid, dim3(kBlock), 0, stream, a);
+    else if (c.tokens == 4) hipLaunchKernelGGL((rope_kernel<T, D, 4, 2, kVec, true>), grid, dim3(kBlock), 0, stream, a);
+    else if (c.past) hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, true>), grid, dim3(kBlock), 0, stream, a);
+    else hipLaunchKernelGGL((rope_kernel<T, D, 1, 1, kVec, false>), grid, dim3(kBlock), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int D>
