@@ -220,20 +220,21 @@ RopeCut rope_cut(long long tokens, int heads, int elem, int head_dim) {
   // The first needs blocks for the whole chip, 256 compute units; the last leaves no lane without a head where these are
   // fewer than four times those of a wave, and shares a sine and cosine among fewer of them.  (Four loads of a wave at once instead of two: 46.6
   // instead of 45.6 for 40 + 8 x 8192, 32.1 instead of 30.8 for 8 + 8 x 16384.)
-  // Results beyond an XCD's L2 go past the caches: 40 + 8 x 512 8.3 -> 7.5, 28 + 4 x 4096 20.0 -> 17.8, 8 + 8 x 65536 106 -> 102, and the
-  // attention that reads 4096 rotated tokens next takes no longer; the one over 300 would (20.9 -> 21.4).
+  // Results go past the caches: 28 + 4 x 4096 20.0 -> 17.8, 8 + 8 x 65536 106 -> 102, and an attention that reads them next takes no longer, also where they are
+  // few (the two calls together, through the caches / past them: 2048 tokens of 1 + 1 heads, 1 MB, 17.0 / 16.9, 4096 17.8 / 17.5; 1600 of 4 + 4 16.5 / 16.4; 4096
+  // of 1 + 1 of 64 x bf16 15.2 / 15.1; 2000 of 2 + 2 of 64 x fp32 17.0 / 17.1).  But not those of one token a block below an XCD's L2: 40 + 8 x 512, beyond
+  // it, 8.3 -> 7.5, the attention over 300 rotated tokens 20.9 -> 21.4.
   const int lanes = heads * row_lanes;             // of a token
   RopeCut c;
-  c.past = tokens * heads * (static_cast<long long>(head_dim) * elem) >= kPastBytes;
+  c.past = 1;
   c.shares = 1;
   if (heads < 4 * rows && tokens >= 1024ll * heads) {
     c.tokens = kWaves * rows;
-    c.past = true;
   } else if (tokens >= 1536 && (elem == 2 ? tokens >= 4ll * lanes : tokens >= 8ll * lanes && lanes <= 384)) {
     c.tokens = 4;
-    c.past = true;
   } else {
     c.tokens = 1;
+    c.past = tokens * heads * (static_cast<long long>(head_dim) * elem) >= kPastBytes;
     const int shares = (heads + rows * kWaves - 1) / (rows * kWaves), want = static_cast<int>((512 + tokens - 1) / tokens);
     c.shares = shares < want ? shares : want;
   }

@@ -35,3 +35,12 @@ def test_launches_within_the_grid(lazyev_lib, elem, d):
             blocks = -(-min(tokens, c.launch) // c.tokens)
             assert blocks * BLOCK < 1 << 32, (heads, tokens)
             assert -(-tokens // c.launch) * c.launch <= (1 << 30) + c.launch     # (token numbers stay in 32 bits)
+
+
+@pytest.mark.parametrize("elem,d", TYPES)
+def test_results_past_the_caches(lazyev_lib, elem, d):
+    """All but those of one token a block that an XCD's L2 (4 MB) holds."""
+    for heads in HEADS:
+        for tokens in TOKENS:
+            c = _cut(lazyev_lib, tokens, heads, elem, d)
+            assert c.past == (c.tokens > 1 or tokens * heads * d * elem >= 4 << 20), (heads, tokens)
