@@ -357,8 +357,8 @@ int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32
  * A token that sees nothing gets zeros, and lse = -inf.  What a token does not see has no influence on it, whatever it holds.
  * joined_out, joined_lse (nullable, together): the output and lse of the same queries over other entries, for instance the
  *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  `out` is not q.
- * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; bf16 weights
- * are rounded to bf16 for the product with V.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times;
+ * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; for the product with V
+ * weights of 128 x bf16 rows are rounded to bf16 (as in lazyev_decode_step), those of 64 x bf16 rows taken as two bf16 terms.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times;
  * n_tokens * n_q_heads / n_kv_heads is at most 65535 * 32, n_seqs * n_kv_heads 2^22, n_seqs * n_tokens * n_q_heads 2^30, length 2^30.
  * Workspace: lazyev_pages_attend_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).
  * Errors: EINVAL (length 0 .. table_stride * page_size among them), EWORKSPACE, EHIP. */

@@ -7,16 +7,17 @@
 // rows takes its own kKeys / kWK entries, 32 at a time:
 //   S^T = K Q^T    v_mfma_f32_32x32x16_bf16 (fp32 rows: 32x32x2_f32): lane (c, h) = (l % 32, l / 32) holds, of row c, the
 //                  logits of the entries 8 i + 4 h + j (i, j < 4)
-//   P = exp2(S)    in place; rounded to bf16 for the product with bf16 values (half a step, 2^-8, of each weight, in place of
-//                  two products; the sum l is that of the weights before, as it also is a result of its own)
+//   P = exp2(S)    in place; for the product with bf16 values rounded to bf16 (128 x bf16: half a step, 2^-8, of each weight) or taken as two bf16 terms
+//                  (64 x bf16: 2^-16), as the decode step does with rows of the same types; the sum l is that of the weights before, as it also
+//                  is a result of its own
 //   O^T += V^T P^T lane (c, h) already holds 8 entries of row c, in an order that the products take from V as well: V
 //                  is read transposed (ds_read_b64_tr_b16), 4 entries of 16 columns to 16 lanes
 // The reference is raised only when a sum of 16 weights relative to it exceeds 2^12 (never rescaled otherwise): a sum
 // is as exact relative to any reference in the range of fp32.  Every decision that changes a row's arithmetic
 // is taken for that row alone: what other rows see has no influence on it.
 // Entries that a row does not see (or that lead to no page) are masked to weight zero, which leaves a NaN of the output where V
-// holds an infinity or NaN.  A block that masked something and ends up with such an output starts over, with those taken out of V
-// in the stages where it masks; the rows that do see one get it at the end.
+// holds an infinity or NaN, as a weight's second term does.  A block that masked something, or has second terms, and ends up with such an output starts
+// over, with those taken out of V in the stages where it masks (all of them); the rows that do see one get it at the end.
 //
 // Few rows: the entries are also cut into splits, which leave (m, l, O) in the workspace for a second kernel.
 //
@@ -56,6 +57,11 @@ struct Rows {
   static constexpr int kChunks = D * static_cast<int>(sizeof(T)) / 16;   // 16-byte chunks of a row
   static constexpr int kOps = kChunks / 2;         // chunks of a row that a lane holds as an operand
   static constexpr int kTiles = D / 32;            // output tiles of 32 columns
+  // Terms of a weight in the product with V.  128 x bf16 weights are rounded, as the decode step rounds them: two terms take a third longer where
+  // products bind (4096 tokens of 40 / 8 heads over their past 207 -> 269 us, 80 rows over 100003 entries 81 -> 99) and lower the error against 64 bits from 0.0020 - 0.0022
+  // to the 0.0016 - 0.0017 of the output's own rounding.  64 x bf16 rows the decode step keeps exact with three terms; two are as far below that rounding
+  // here (the same calls with one / two / three terms 142 / 183 / 219 us, 52 / 56 - 61 / 71; 224 rows over 8192 entries 16.2 / 17.3 / 18.2).
+  static constexpr int kTerms = kF32 || D == 128 ? 1 : 2;
   // Where chunk x of entry r of a stage lies among the entry's chunks: keys are read by 16 entries at a time, one chunk of
   // each; values by 4 (bf16) entries, 64 bytes of each, or (fp32) an entry and the one four further, 128 bytes of each.
   __device__ static int k_slot(int r, int x) { return x ^ (kChunks == 8 ? (r >> 1) & 7 : r & 15); }
@@ -356,7 +362,8 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   end = __builtin_amdgcn_readfirstlane(min(end, last));
   const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
   // the first stage that some row does not see all of
-  const int mask_from = max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
+  // (with weights in terms, of which the second may be negative or zero: as if it were the first of all)
+  const int mask_from = R::kTerms > 1 ? 0 : max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
   int masked = INT_MAX;                            // ... and the first one with anything masked
 
   auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
@@ -434,10 +441,13 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
   };
   constexpr int kProducts = R::kF32 ? 16 : 2;      // of a sub-tile and a tile of columns
-  using Weights = std::conditional_t<R::kF32, f32x16_t, u32x4_t[2]>;
+  using Weights = std::conditional_t<R::kF32, f32x16_t, u32x4_t[R::kTerms][2]>;
   auto product = [&](auto v, const Weights &p, int g, f32x16_t &to) __attribute__((always_inline)) {
     if constexpr (R::kF32) to = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), p[g], to, 0, 0, 0);
-    else to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, p[g]), to, 0, 0, 0);
+    else
+#pragma unroll
+      for (int i = 0; i < R::kTerms; ++i)
+        to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, p[i][g]), to, 0, 0, 0);
   };
   auto weights_of = [&](const f32x16_t &s, Weights &p, auto fast) __attribute__((always_inline)) {   // -> their sum
     float w[16], sum = 0.f;
@@ -450,7 +460,16 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       for (int x = 0; x < 16; ++x) p[x] = w[x];
     } else {
 #pragma unroll
-      for (int x = 0; x < 16; x += 2) p[x / 8][x % 8 / 2] = pair_to_bf16(w[x], w[x + 1]);
+      for (int i = 0; i < R::kTerms; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; x += 2) {
+          const unsigned both = pair_to_bf16(w[x], w[x + 1]);
+          p[i][x / 8][x % 8 / 2] = both;
+          if (i + 1 < R::kTerms) {                 // what is left
+            w[x] -= bf16_low(both);
+            w[x + 1] -= bf16_high(both);
+          }
+        }
     }
     return sum;
   };
@@ -532,7 +551,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       for (int g = 0; g < kProducts; ++g)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) product(values(vs, 32 * x, t, g), p[x], g, o[t]);
-    ahead<kSub * kProducts * kTiles, 1, R::kF32 ? 1 : 2, 4>();
+    ahead<kSub * kProducts * kTiles, R::kF32 ? 1 : R::kTerms, R::kF32 ? 1 : 2, 4>();
   };
   // (of a stage's values; the stage is complete and nobody's yet)
   auto take_out = [&](char *vs) __attribute__((always_inline)) {
@@ -540,7 +559,10 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     for (int u = 0; u < S::kLoads; ++u) {
       u32x4_t *at = reinterpret_cast<u32x4_t *>(vs) + u * S::kBlock + threadIdx.x;
       u32x4_t w = *at;
-      if (take_out_odd<R::kF32>(w)) *at = w;
+      if (take_out_odd<R::kF32>(w)) {
+        *at = w;
+        shared_odd = 2;
+      }
     }
     __syncthreads();
   };
@@ -639,7 +661,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   }
   if (!have) return;
 
-  if (__builtin_expect(again, 0)) {
+  if (__builtin_expect(again, 0) && __builtin_amdgcn_readfirstlane(shared_odd) == 2) {
     // the infinities and NaN that were taken out and that a row sees (with a weight above zero, however small)
     for (int key = first + masked * kKeys; key < min(last, most); ++key) {
       const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
