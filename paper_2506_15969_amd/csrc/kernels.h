@@ -218,9 +218,11 @@ inline void page_div(PageTable &t) {
   while ((1u << t.shift) < static_cast<uint32_t>(t.page_size)) ++t.shift;
   t.magic = static_cast<uint32_t>(((((1ull << t.shift) - t.page_size) << 32) / t.page_size) + 1);
 }
-__device__ inline int page_of(const PageTable &t, int entry) {
-  return static_cast<int>((__umulhi(static_cast<unsigned>(entry), t.magic) + static_cast<unsigned>(entry)) >> t.shift);
+__host__ __device__ inline int page_of(const PageTable &t, int entry) {
+  const uint32_t n = static_cast<uint32_t>(entry);
+  return static_cast<int>((static_cast<uint32_t>((static_cast<uint64_t>(n) * t.magic) >> 32) + n) >> t.shift);
 }
+int page_of_entry(int page_size, int entry);       // both, on the host
 struct RopeArgs {
   RopeRows rows[2];                 // rows[1].heads may be 0
   int32_t n_seqs, n_tokens;

@@ -75,6 +75,13 @@ lazyev::PageTable page_table(const lazyev_pages &p) {
 
 namespace lazyev {
 
+int page_of_entry(int page_size, int entry) {
+  PageTable t;
+  t.page_size = page_size;
+  page_div(t);
+  return page_of(t, entry);
+}
+
 bool attend_args(const lazyev_pages *p, int32_t length, int32_t n_tokens, int32_t n_q_heads, AttendArgs *out) {
   if (!pages_ok(p) || length < 0 || n_tokens < 0 || n_q_heads < 1 || n_q_heads % p->n_kv_heads != 0) return false;
   if (n_q_heads / p->n_kv_heads > 64 || static_cast<long long>(length) > static_cast<long long>(p->table_stride) * p->page_size) return false;
