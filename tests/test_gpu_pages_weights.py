@@ -50,3 +50,24 @@ def test_infinities_that_every_token_sees(lazyev_lib, dtype, d, S, n, Hq, H, pag
     others = torch.ones(d, dtype=torch.bool, device="cuda")
     others[[3, 17, 40, 41]] = False
     assert torch.equal(out[..., others], clean[0][..., others])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n,length,Hq,H,page", [(1, 100, 7, 1, 16), (40, 300, 4, 2, 16), (300, 400, 2, 1, 24), (600, 700, 7, 1, 16), (9000, 130, 1, 1, 16)])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_other_columns_keep_their_bits(lazyev_lib, dtype, d, n, length, Hq, H, page, value):
+    """Infinities or NaN in some columns of entries that some tokens see: the other columns and the log-sum-exps are the same bits for every token,
+    those that see the entries among them."""
+    c = Case(lazyev_lib, dtype, d, 1, n, Hq, H, page, length, seed=23)
+    vis = torch.randint(1, length + 1, (1, n), generator=c.gen, device="cuda").int()
+    vis[0, -1], vis[0, 0] = length // 2, length
+    clean = c.cache.attend(length, c.q, visible=vis)
+    dense = torch.arange(length // 2, length, device="cuda")
+    pages = c.table[0].long()[dense // page]
+    c.v_pages[pages[::3], :, dense[::3] % page, 1::7] = value
+    out, lse = c.cache.attend(length, c.q, visible=vis)
+    others = torch.ones(d, dtype=torch.bool, device="cuda")
+    others[1::7] = False
+    assert torch.equal(lse, clean[1]) and torch.equal(out[..., others], clean[0][..., others])
+    low = vis[0] <= length // 2
+    assert torch.equal(out[0][low], clean[0][0][low]) and bool((~torch.isfinite(out[0][~low][..., 1::7])).all())
