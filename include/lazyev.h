@@ -293,7 +293,8 @@ int lazyev_score_pairs(const int32_t *delta_t /*device*/, const int32_t *mri /*d
  * may be a view into a joint projection), its result at `to` by the to_ strides: any places, the entries of
  * a cache for instance, of which no two heads share one.  `to` may be `rows` with the same strides; an
  * overlap of any other kind gives unspecified rows.
- * weight (nullable): [head_dim] of the rows' type: the head is normed, x / sqrt(mean(x^2) + eps) * weight. */
+ * weight (nullable): [head_dim] of the rows' type: the head is normed, x / sqrt(mean(x^2) + eps) * weight.  The squares are summed in
+ * fp32: elements of up to 2^60 in size, and, where eps does not outweigh them, from 2^-60 on. */
 typedef struct {
   const void *rows;             /* (device)                                                             */
   void       *to;               /* (device)                                                             */
@@ -342,7 +343,8 @@ typedef struct {
 /* Writes the keys and values of n_tokens tokens of every table row to the row's entries start .. start + n_tokens - 1: the keys
  * normed (k->weight) and rotated on the way, by the position position0 + i of the i-th token, the values as they are
  * (v->weight null).  k and v describe the source only: their `to` members are ignored.
- * A page that several of the written entries lead to (one number twice in the table) holds unspecified parts of their rows.
+ * A page that several of the written entries lead to (one number twice in the table) holds unspecified parts of their rows.  The
+ * sources do not overlap the written entries.
  * start + n_tokens <= table_stride * page_size.  Errors: EINVAL, EHIP. */
 int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32_t n_tokens,
                         const lazyev_heads *k /*host*/, const lazyev_heads *v /*host*/,
@@ -356,7 +358,9 @@ int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32
  * prefix: likewise.  A prompt over itself: visible = i + 1.
  * A token that sees nothing gets zeros, and lse = -inf.  What a token does not see has no influence on it, whatever it holds.
  * joined_out, joined_lse (nullable, together): the output and lse of the same queries over other entries, for instance the
- *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  `out` is not q.
+ *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  No other argument
+ *   overlaps what the call writes (out is not q: EINVAL).
+ * Values of up to 2^89 in size stay in the range of fp32 on the way; of larger ones sums may leave it as infinities.
  * scale 0 selects 1/sqrt(head_dim).  Sums, maxima and the output are fp32 until out is rounded to its type; for the product with V
  * weights of 128 x bf16 rows are rounded to bf16 (as in lazyev_decode_step), those of 64 x bf16 rows taken as two bf16 terms.  n_q_heads is any multiple of the pages' n_kv_heads up to 64 times;
  * n_tokens * n_q_heads / n_kv_heads is at most 65535 * 32, n_seqs * n_kv_heads 2^22, n_seqs * n_tokens * n_q_heads 2^30, length 2^30.
@@ -376,7 +380,8 @@ size_t lazyev_pages_attend_workspace(const lazyev_pages *pages /*host*/, int32_t
 /* lazyev_decode_step of a batch whose sequences share a prefix: the same append and the same tracking, with attention over
  * the first prefix_len entries of the pages' one table row AND the sequences' own caches.  The softmax is over both: p of the
  * activation test (and p_out) is the weight that an own entry has beside the prefix.  The prefix takes no part in tracking and is
- * never evicted.  `out` is not q.  prefix_len 0 is lazyev_decode_step.  With per-sequence timing, sequences that take no part are left alone.
+ * never evicted.  (lazyev_prefill_track knows no prefix: its weights are those of the prompt alone, so that after one it counts
+ * more activations than the test beside the prefix would, unless p_override holds the weights.)  `out` is not q.  prefix_len 0 is lazyev_decode_step.  With per-sequence timing, sequences that take no part are left alone.
  * The pages' head_dim, dtype and n_kv_heads are the context's and n_seqs is 1; scale is the context's.  Own and prefix parts
  * are rounded to the rows' type once each.
  * workspace: lazyev_pages_attend_workspace(prefix, prefix_len, batch, n_q_heads) bytes, on the context's stream.

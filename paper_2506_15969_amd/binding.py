@@ -229,7 +229,8 @@ def _launch(device, call, *args):
 
 
 class NormRope:
-    """Norms of the query and key heads of a layer and the rotation by the token's position (lazyev_norm_rope).
+    """Norms of the query and key heads of a layer and the rotation by the token's position (lazyev_norm_rope).  For serving, as everything
+    here: results carry no gradients, whether the inputs ask for them or not.
 
     q_weight, k_weight [head_dim] of the rows' type, or None: not normed.  inv_freq [dims / 2] fp32, or None: not
     rotated; layout ROPE_HALVES (elements j and j + dims / 2 form a pair) or ROPE_PAIRS (2 j and 2 j + 1).
@@ -302,7 +303,7 @@ class NormRope:
 class PagedCache:
     """Keys and values of one layer in pages: k_pages, v_pages [n_pages,Hkv,page_size,d] and table [S,m] int32 (entry i of row s is
     place i % page_size of page table[s, i // page_size]), all the caller's tensors.  A layer's caches of a LazyEviction are such
-    pages too: PagedCache(eng.k_cache[l], eng.v_cache[l], table) with one page per sequence, a page number = a sequence."""
+    pages too: PagedCache(eng.k_cache[l], eng.v_cache[l], table) with one page per sequence, a page number = a sequence.  Results carry no gradients."""
 
     def __init__(self, k_pages, v_pages, table, n_q_heads=None):
         for x in (k_pages, v_pages):

@@ -3,8 +3,8 @@
 //
 // A wave keeps 32 rows: their queries, their output O^T (fp32) and, per row, a reference m and the sum l of the weights
 // relative to it, exp2(s log2 e - m).  Entries come in stages of kKeys, fetched straight into LDS by the whole block while the
-// stage before is worked on, a page number one stage further ahead.  Of a stage each of the kWK waves that share 32
-// rows takes its own kKeys / kWK entries, 32 at a time:
+// stage before is worked on, by page numbers that the block keeps in LDS, kWindow at a time.  Of a stage each of the kWK waves that
+// share 32 rows takes its own kKeys / kWK entries, 32 at a time:
 //   S^T = K Q^T    v_mfma_f32_32x32x16_bf16 (fp32 rows: 32x32x2_f32): lane (c, h) = (l % 32, l / 32) holds, of row c, the
 //                  logits of the entries 8 i + 4 h + j (i, j < 4)
 //   P = exp2(S)    in place; for the product with bf16 values rounded to bf16 (128 x bf16: half a step, 2^-8, of each weight) or taken as two bf16 terms
@@ -12,8 +12,9 @@
 //                  is a result of its own
 //   O^T += V^T P^T lane (c, h) already holds 8 entries of row c, in an order that the products take from V as well: V
 //                  is read transposed (ds_read_b64_tr_b16), 4 entries of 16 columns to 16 lanes
-// The reference is raised only when a sum of 16 weights relative to it exceeds 2^12 (never rescaled otherwise): a sum
-// is as exact relative to any reference in the range of fp32.  Every decision that changes a row's arithmetic
+// The reference is raised only when a lane's sum of weights relative to it in a stage (16 or, with 64 entries of a stage to a wave, 32 of
+// them) exceeds 2^12 (never rescaled otherwise): a sum is as exact relative to any reference in the range of fp32, and with weights of 2^8 on average at
+// most over 2^30 entries values of up to 2^89 stay in it.  Every decision that changes a row's arithmetic
 // is taken for that row alone: what other rows see has no influence on it.
 // Entries that a row does not see (or that lead to no page) are masked to weight zero, which leaves a NaN of the output where V
 // holds an infinity or NaN, as a weight's second term does.  A block that masked something, or has second terms, and ends up with such an output starts
@@ -22,8 +23,10 @@
 // Few rows: the entries are also cut into splits, which leave (m, l, O) in the workspace for a second kernel.
 //
 // Bound by memory where few rows read many entries: 80 rows over 100003 entries of each of 8 KV heads, 128 x bf16 (410 MB), 79 us, 5.2
-// TB/s, the rate of a copy of 1 GiB.  Bound by the matrix cores and their power where many do: 4096 tokens of 40 / 8 heads over
-// their past (172 GFLOP) 193 - 198 us, 870 - 890 TFLOP/s, against 1213 of a bf16 product of 8192^3 on the same card (order and depth
+// TB/s, the rate of a copy of 1 GiB.  Bound by the products and the vector instructions beside them where many do: 4096 tokens of 40 / 8 heads over
+// their past (172 GFLOP) 193 - 198 us in a loop of passes, 870 - 890 TFLOP/s, against 1213 - 1358 of a bf16 product of 8192^3 on the same card.  By counters
+// the matrix cores are busy in 45 % of the cycles (73 % in that product), vector instructions are issued in 44 %: together most of the time, as
+// where the two waves of a SIMD seldom do both at once.  The clock is 2.24 GHz meanwhile, of 2.4, and 1.97 in the product, so power is not what binds (order and depth
 // of the operands' reads, wave priorities and a third stage on its way change nothing).  Bound by its own length where both are
 // few: one token's 28 heads over 8192 entries 13.3 us, of which the second launch 5.5, the products 1.3 and the entries' arrival 1.0.
 #include "kernels.h"
@@ -765,7 +768,8 @@ __global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const Atten
 // How a call is cut: rows of a block (32 wr), waves that share rows, entries of a stage, splits of the entries.
 struct Plan { int wr, wk, keys, n_split, split_keys; };
 
-// The shapes of blocks, and what a stage of theirs takes on a full chip of 256 (us; rows of 128 x bf16).  More rows in a block
+// The shapes of blocks, and what a stage of theirs takes on a full chip of 256 compute units (us; the rule asks for no device, so that a workspace's
+// size is the same everywhere; a part of the chip takes the same shapes).  More rows in a block
 // share an entry's way to LDS, and a wave with 64 entries a stage has two chains of products; fewer rows make more blocks of few
 // tokens without splits.  The cheapest by the sum of these is taken: stages one after the other, or the bytes where they take longer, a
 // fixed part, and for splits a second launch that reads what the first left (16 KB for 32 rows and split).  Measured, us, 128 x bf16,
@@ -776,6 +780,19 @@ struct Plan { int wr, wk, keys, n_split, split_keys; };
 //   4 KV heads, 4480 rows,   4096          (64, 4) x  1 99.8   (128, 2) x  3 64.0   (256, 1) x  3 55.7
 //   8 KV heads, 20480 rows, their past     (64, 4) x  1 299    (128, 2) x  1 214    (256, 1) x  1 193.5
 //   8 KV heads,   80 rows, 100003          (64, 4) x 16 107    (128, 2) x 32 81.7   (256, 1) x 32 89.4
+// Other rows, us of what the rule takes / of the best of all shapes and splits:
+//                                                64 x bf16      64 x fp32      128 x fp32
+//   4 KV heads,    7 rows, 8192 entries          11.6 / 11.6    16.3 / 16.2    25.2 / 25.2
+//   8 KV heads,    8 rows, 4096                  10.4 / 10.4    15.0 / 13.5    22.0 / 22.0
+//   4 KV heads,  224 rows, 8192                  17.6 / 17.6    32.5 / 32.3    55.4 / 51.6
+//   8 KV heads,   80 rows, 100003 (fp32: 25000)  56.4 / 56.4    78.7 / 69.2    145 / 131
+//   4 KV heads,  512 rows, 8192 (2048)           22.5 / 21.5    23.4 / 21.7    36.2 / 36.2
+//   4 KV heads, 2048 rows, 4096 (1024)           28.6 / 27.9    33.3 / 31.0    55.9 / 54.0
+//   4 KV heads, 4480 rows, 4096 (1024)           51.2 / 51.2    67.8 / 63.6    126 / 126
+//   8 KV heads, 20480 (5120) rows, their past    174 / 174      85.5 / 74.2    153 / 148
+//   4 KV heads, 7000 rows, their past            20.9 / 20.1    74.8 / 50.4    151 / 99.0
+//   16 x 4 KV heads, 7 rows each, 8192           29.6 / 28.1    64.5 / 64.5    176 / 176
+// (The last but one: the rule counts all entries where rows see half of them, and leaves out blocks of few rows, see plan_of.)
 struct BlockShape { int wr, wk, keys; float stage_us; };
 // (fp32 products run at a sixteenth of the rate of bf16 ones: a stage is a wave's products.  fp32 rows of 128: fewer entries a stage, and
 // waves, than LDS and registers hold of the others.)
@@ -804,7 +821,7 @@ Plan plan_of(const AttendArgs &a) {
   for (int i = 0; i < n_shapes; ++i) {
     const BlockShape &s = shapes[i];
     if (i > 0 && 32 * shapes[i - 1].wr >= M) break;            // (rows enough for the shape before)
-    if (i + 1 < n_shapes && M > 32 * s.wr * 64) continue;      // (far more rows than blocks of few are for)
+    if (i + 1 < n_shapes && M > 32 * s.wr * 64) continue;      // (far more rows than blocks of few are for: 4480 and 20480 rows above)
     const long long blocks = static_cast<long long>(units) * ((M + 32 * s.wr - 1) / (32 * s.wr));
     const int stages = a.length > 0 ? (a.length + s.keys - 1) / s.keys : 1;
     const int fill = static_cast<int>(256 / blocks);
