@@ -356,7 +356,7 @@ int lazyev_pages_append(const lazyev_pages *pages /*host*/, int32_t start, int32
  * over the entries below visible[s * n_tokens + i] (null: all; values beyond 0 .. length count as the nearest of the two).
  * A batch's decode step over its common prefix: one table row, every sequence's query a token of it.  A prompt after the
  * prefix: likewise.  A prompt over itself: visible = i + 1.
- * A token that sees nothing gets zeros, and lse = -inf.  What a token does not see has no influence on it, whatever it holds.
+ * A token that sees nothing, or nothing but logits of -inf, gets zeros, and lse = -inf.  What a token does not see has no influence on it, whatever it holds.
  * joined_out, joined_lse (nullable, together): the output and lse of the same queries over other entries, for instance the
  *   sequences' own caches; out and lse are then those over both.  They may be `out` and `lse` themselves.  No other argument
  *   overlaps what the call writes (out is not q: EINVAL).
