@@ -8,8 +8,7 @@
 //   S^T = K Q^T    v_mfma_f32_32x32x16_bf16 (fp32 rows: 32x32x2_f32): lane (c, h) = (l % 32, l / 32) holds, of row c, the
 //                  logits of the entries 8 i + 4 h + j (i, j < 4)
 //   P = exp2(S)    in place; for the product with bf16 values rounded to bf16 (128 x bf16: half a step, 2^-8, of each weight) or taken as two bf16 terms
-//                  (64 x bf16: 2^-16), as the decode step does with rows of the same types; the sum l is that of the weights before, as it also
-//                  is a result of its own
+//                  (64 x bf16: 2^-16), see kTerms; the sum l is that of the weights before, as it also is a result of its own
 //   O^T += V^T P^T lane (c, h) already holds 8 entries of row c, in an order that the products take from V as well: V
 //                  is read transposed (ds_read_b64_tr_b16), 4 entries of 16 columns to 16 lanes
 // The reference is raised only when a lane's sum of weights relative to it in a stage (16 or, with 64 entries of a stage to a wave, 32 of
