@@ -393,6 +393,96 @@ int lazyev_decode_step_shared(lazyev_ctx *ctx, int32_t layer, int32_t t, const v
                               void *workspace /*device*/, size_t workspace_bytes,
                               float *p_out /*device, nullable*/, const float *p_override /*device, nullable*/);
 
+/* ---- A long cache in pages: which of its blocks a token reads, and which of its entries stay.  The calls keep no state, as those of the section
+ * above, of which the same holds (streams, graphs, calls at once, alignment, page numbers that stand for no page).
+ *
+ * Blocks.  Block b of a table row is its entries b * block .. b * block + block - 1, whatever pages they lie in.  Per KV head its bounds are
+ * the smallest and the largest of each element of its keys. */
+typedef struct {
+  int32_t n_kv_heads, head_dim, dtype;             /* head_dim 64 or 128                                */
+  int32_t n_seqs, n_blocks;                        /* blocks of a table row and KV head that `bounds` has room for */
+  int32_t block;                                   /* entries of a block: 16, 32, 64 or 128             */
+  void    *bounds;                                 /* (device) [n_seqs][n_kv_heads][n_blocks][2][head_dim] of the rows' type, 16-byte aligned */
+} lazyev_blocks;
+
+/* Bounds of the blocks that the entries start .. start + n_tokens - 1 of every table row lie in, over those entries; where `start` lies inside a block, that
+ * block's bounds are extended, so that the same call after every append keeps all of them.  Other blocks are left alone.  (Entries that change otherwise, by
+ * an eviction for instance, are counted in anew from their block's first one on.)  A NaN among a block's keys is in its bounds; entries of no page are
+ * not counted: a block of nothing else has bounds of +inf and -inf.
+ * Sizes agree between pages and blocks; start + n_tokens <= n_blocks * block.  Errors: EINVAL, EHIP. */
+int lazyev_blocks_bound(const lazyev_pages *pages /*host*/, const lazyev_blocks *blocks /*host*/, int32_t start, int32_t n_tokens,
+                        void *stream);
+
+/* The blocks that tokens read, by a bound of what their logits can be: for a block, a token and a KV head
+ *   score = max over the heads of the group of (sum of q[e] largest[e] where q[e] > 0, and of q[e] smallest[e] where q[e] < 0).
+ * A token that sees v entries (visible as in lazyev_pages_attend) has ceil(v / block) blocks.  If these are more than n_chosen, it reads the first
+ * n_first, the last n_last (of which one may be seen in part: it has no score) and those of the others with the highest scores,
+ * of equal ones the lowest; otherwise all.  The ranks are those of the exact sums: in binary64, which the scores are worked out
+ * in where a rounded one does not decide.  A sum that is no number counts as +inf: such a block is read rather than passed over.
+ * Bounds are read of the blocks that some token ranks; what others hold has no influence (but may be read).
+ * chosen (device): [n_seqs][n_tokens][n_kv_heads][n_chosen], ascending, -1 behind the last.
+ * n_first >= 0, n_last >= 1, n_first + n_last <= n_chosen <= 2^20; length 0 .. n_blocks * block, at most 2^30; heads and tokens as in lazyev_pages_attend;
+ * n_seqs * n_kv_heads * (length / block / 128 + 1) at most 2^22.
+ * Workspace: lazyev_blocks_choose_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).
+ * Errors: EINVAL, EWORKSPACE, EHIP. */
+int lazyev_blocks_choose(const lazyev_blocks *blocks /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,
+                         const int32_t *visible /*device, nullable*/, const void *q /*device, [n_seqs][n_tokens][n_q_heads][head_dim]*/,
+                         int32_t n_first, int32_t n_last, int32_t n_chosen, int32_t *chosen /*device*/, void *workspace /*device*/,
+                         size_t workspace_bytes, void *stream);
+/* Bytes for such a call; 0 also for arguments that the call refuses. */
+size_t lazyev_blocks_choose_workspace(const lazyev_blocks *blocks /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,
+                                      int32_t n_last, int32_t n_chosen);
+
+/* lazyev_pages_attend over the entries of listed blocks alone: for every token and KV head those of the blocks chosen[s][i][kvh][..] that the token
+ * sees, visible and all else as there (a token that sees nothing of its blocks gets zeros and lse = -inf; what it does not see has no influence).  A number that is
+ * no block of the row's first `length` entries, -1 for instance, stands for none; a number twice counts its entries twice.
+ * block: 16, 32, 64 or 128; n_chosen >= 1, n_chosen * block at most 2^30; a group of up to 64 heads; n_seqs * n_tokens * n_kv_heads at most 2^22.
+ * Pools of up to 2^32 - 1 rows.  Errors: those of lazyev_pages_attend. */
+int lazyev_blocks_attend(const lazyev_pages *pages /*host*/, int32_t length, int32_t block, int32_t n_chosen,
+                         const int32_t *chosen /*device, [n_seqs][n_tokens][n_kv_heads][n_chosen]*/, int32_t n_tokens, int32_t n_q_heads,
+                         const int32_t *visible /*device, nullable*/, const void *q /*device*/, const void *joined_out /*device, nullable*/,
+                         const float *joined_lse /*device, nullable*/, void *out /*device*/, float *lse /*device, nullable*/, float scale,
+                         void *workspace /*device*/, size_t workspace_bytes, void *stream);
+size_t lazyev_blocks_attend_workspace(const lazyev_pages *pages /*host*/, int32_t length, int32_t block, int32_t n_chosen,
+                                      int32_t n_tokens, int32_t n_q_heads);
+
+/* The attention weight that every entry received, over the tokens that see it and the heads of its group:
+ *   weights[s][kvh][e] = (e < known ? decay * old[s][kvh][e] : 0) + sum of exp(scale * q k - lse),  e < length
+ * with the lse that lazyev_pages_attend (or lazyev_blocks_attend) gave these queries; one over more than the row's entries, a joined one, gives
+ * the weights beside those.  Called for a prompt and then for every step, with decay 1, it keeps the sum of all weights; with decay 0 those of
+ * the call alone.  A token whose lse is -inf adds nothing, nor does any token to an entry that it does not see or that lies in no page.
+ * old, weights: fp32, `stride` elements from one KV head to the next (at least length), and n_kv_heads times that from one row to the next; weights may be
+ * old (known 0: old may be null).  No other argument overlaps weights.  scale as in lazyev_pages_attend, decay finite.
+ * Logits, weights and sums are fp32; the sums are taken in an order that depends on sizes alone.  length up to 2^30, n_seqs * n_kv_heads * (length / 128 + 1) below 2^24,
+ * heads and tokens as in lazyev_pages_attend.
+ * Workspace: lazyev_pages_weigh_workspace bytes, 256-byte aligned, needing no initial contents (0 bytes: may be null).  Errors: EINVAL, EWORKSPACE, EHIP. */
+int lazyev_pages_weigh(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads,
+                       const int32_t *visible /*device, nullable*/, const void *q /*device*/,
+                       const float *lse /*device, [n_seqs][n_tokens][n_q_heads]*/, float scale, const float *old /*device*/, int32_t known,
+                       float decay, float *weights /*device*/, int64_t stride, void *workspace /*device*/, size_t workspace_bytes,
+                       void *stream);
+size_t lazyev_pages_weigh_workspace(const lazyev_pages *pages /*host*/, int32_t length, int32_t n_tokens, int32_t n_q_heads);
+
+/* Eviction by weight: of the first n entries of every table row and KV head (n = lengths[s], values beyond 0 .. length counting as the nearest of the two; null:
+ * length), `keep` stay if there are more: the newest, whose position is above the largest one - n_recent, the first, whose position is below n_first, and of the
+ * others those of the largest weights, a NaN being the largest; equal ones (and, if there are more than `keep` of them, newest and first ones) in
+ * the entries' order.  Positions are those of `positions`, null: the entries' own numbers.
+ * Entries that stay below `keep` are left where they are; those from `keep` on go, in their order, to the places that became free, lowest first, with
+ * their keys and values.  So no more rows are moved than entries go; the order of entries is not that of positions any more, which
+ * attention does not ask for.  Entries from `keep` on are left as they are.
+ * sources (device): [n_seqs][n_kv_heads][keep], the entry that each place holds now, -1 from n on.
+ * weights, positions (device): `stride` elements from one KV head to the next (at least length).  weights_to, positions_to (device, nullable): weights and positions
+ *   of the places, 0 and -1 from n on, `to_stride` elements from one KV head to the next (at least keep); they may be weights and positions with the same
+ *   stride, and overlap nothing else.  Rows of entries of no page are not moved.  An entry below `keep` that two table rows share holds an unspecified one of their rows.
+ * keep >= 1, n_recent, n_first >= 0, n_recent + n_first <= keep; n_seqs * n_kv_heads below 2^22, n_seqs * n_kv_heads * (keep / 64 + 1) below 2^24; length up to 2^30.
+ * Workspace: lazyev_pages_evict_workspace bytes, 256-byte aligned, needing no initial contents.  Errors: EINVAL, EWORKSPACE, EHIP. */
+int lazyev_pages_evict(const lazyev_pages *pages /*host*/, int32_t length, const int32_t *lengths /*device, nullable*/, int32_t keep,
+                       int32_t n_recent, int32_t n_first, const float *weights /*device*/, const int32_t *positions /*device, nullable*/,
+                       int64_t stride, int32_t *sources /*device*/, float *weights_to /*device, nullable*/,
+                       int32_t *positions_to /*device, nullable*/, int64_t to_stride, void *workspace /*device*/, size_t workspace_bytes,
+                       void *stream);
+size_t lazyev_pages_evict_workspace(const lazyev_pages *pages /*host*/, int32_t keep);
+
 void lazyev_destroy(lazyev_ctx *ctx);              /* frees host memory only; NULL is allowed */
 const char *lazyev_strerror(int code);
 int lazyev_last_hip_error(const lazyev_ctx *ctx);  /* hipError_t of the last EHIP, else 0 */

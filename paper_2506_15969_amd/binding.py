@@ -65,13 +65,20 @@ class Pages(C.Structure):
                 ("table", C.c_void_p)]
 
 
+class Blocks(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("n_seqs", C.c_int32),
+                ("n_blocks", C.c_int32), ("block", C.c_int32), ("bounds", C.c_void_p)]
+
+
 # what include/lazyev.h declares (the contract) ...
 EXPORTS = ["lazyev_capacity", "lazyev_workspace_size", "lazyev_init", "lazyev_decode_step",
            "lazyev_prefill_track", "lazyev_prefill_track_seq", "lazyev_evict", "lazyev_evict_all",
            "lazyev_evict_static", "lazyev_stats", "lazyev_admit", "lazyev_retire",
            "lazyev_cached_before_step", "lazyev_mri_histogram", "lazyev_window_from_histogram",
            "lazyev_score_pairs", "lazyev_norm_rope", "lazyev_pages_append", "lazyev_pages_attend",
-           "lazyev_pages_attend_workspace", "lazyev_decode_step_shared", "lazyev_destroy", "lazyev_strerror", "lazyev_last_hip_error"]
+           "lazyev_pages_attend_workspace", "lazyev_decode_step_shared", "lazyev_blocks_bound", "lazyev_blocks_choose",
+           "lazyev_blocks_choose_workspace", "lazyev_blocks_attend", "lazyev_blocks_attend_workspace", "lazyev_pages_weigh",
+           "lazyev_pages_weigh_workspace", "lazyev_pages_evict", "lazyev_pages_evict_workspace", "lazyev_destroy", "lazyev_strerror", "lazyev_last_hip_error"]
 # ... and include/lazyev_bench.h (knobs and the per-kernel timer in the same library; the plain
 # streaming probes in liblazyev_bench.so, loaded by bench_lib() when somebody measures)
 BENCH_EXPORTS = ["lazyev_set_chunk", "lazyev_set_target_blocks", "lazyev_set_variant", "lazyev_set_spin_ticks",
@@ -148,6 +155,29 @@ lib.lazyev_decode_step_shared.restype = C.c_int
 lib.lazyev_decode_step_shared.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_void_p, C.POINTER(Pages), C.c_int32, C.c_void_p, C.c_size_t,
                                           C.c_void_p, C.c_void_p]
+lib.lazyev_blocks_bound.restype = C.c_int
+lib.lazyev_blocks_bound.argtypes = [C.POINTER(Pages), C.POINTER(Blocks), C.c_int32, C.c_int32, C.c_void_p]
+lib.lazyev_blocks_choose_workspace.restype = C.c_size_t
+lib.lazyev_blocks_choose_workspace.argtypes = [C.POINTER(Blocks), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+lib.lazyev_blocks_choose.restype = C.c_int
+lib.lazyev_blocks_choose.argtypes = [C.POINTER(Blocks), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                     C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+lib.lazyev_blocks_attend_workspace.restype = C.c_size_t
+lib.lazyev_blocks_attend_workspace.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+lib.lazyev_blocks_attend.restype = C.c_int
+lib.lazyev_blocks_attend.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_size_t,
+                                     C.c_void_p]
+lib.lazyev_pages_weigh_workspace.restype = C.c_size_t
+lib.lazyev_pages_weigh_workspace.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32]
+lib.lazyev_pages_weigh.restype = C.c_int
+lib.lazyev_pages_weigh.argtypes = [C.POINTER(Pages), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                   C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+lib.lazyev_pages_evict_workspace.restype = C.c_size_t
+lib.lazyev_pages_evict_workspace.argtypes = [C.POINTER(Pages), C.c_int32]
+lib.lazyev_pages_evict.restype = C.c_int
+lib.lazyev_pages_evict.argtypes = [C.POINTER(Pages), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                   C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
 lib.lazyev_set_chunk.restype = C.c_int
 lib.lazyev_set_chunk.argtypes = [C.c_void_p, C.c_int32]
 lib.lazyev_set_target_blocks.restype = C.c_int
@@ -381,6 +411,123 @@ class PagedCache:
         _check(code, "lazyev_pages_attend")
         return out, lse
 
+    def attend_blocks(self, length, q, blocks, block, visible=None, joined=None, out=None, lse=None, scale=0.0, workspace=None):
+        """lazyev_blocks_attend: `attend` over the entries of listed blocks alone.  blocks int32 [S,n,Hkv,m] (or [n,Hkv,m] of a single
+        row), as KeyBounds.choose gives them: numbers of blocks of `block` entries for every token and KV head, -1: none."""
+        pg, shape, device = self.pages, q.shape, self.device
+        n, n_q_heads, rows, seen, other = self._queries(length, q, visible, joined)
+        _need(blocks.dtype is torch.int32 and blocks.shape[:-1] == shape[:-2] + (pg.n_kv_heads,) and blocks.shape[-1] > 0 and
+              blocks.is_contiguous() and blocks.device == device,
+              "blocks are int32, [S, n, Hkv, m], contiguous, on the pages' GPU")
+        m = blocks.shape[-1]
+        _need(block in (16, 32, 64, 128) and m * block <= 1 << 30, "blocks of 16, 32, 64 or 128 entries")
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _need(out.shape == shape and out.dtype is q.dtype and out.is_contiguous() and out.device == device, "out is like q")
+        if lse is None:
+            lse = q.new_empty(rows, dtype=torch.float32)
+        else:
+            _need(lse.shape == rows and lse.dtype is torch.float32 and lse.is_contiguous() and lse.device == device, "lse is fp32, one for each row of q")
+        workspace, at, n_bytes = self._bytes(workspace, lib.lazyev_blocks_attend_workspace, pg, length, block, m, n, n_q_heads)
+        code = _launch(device, lib.lazyev_blocks_attend, pg, length, block, m, blocks.data_ptr(), n, n_q_heads, seen, q.data_ptr(), other[0], other[1],
+                       out.data_ptr(), lse.data_ptr(), scale, at, n_bytes)
+        _check(code, "lazyev_blocks_attend")
+        return out, lse
+
+    def weigh(self, length, q, lse, weights=None, old=None, known=None, decay=1.0, visible=None, scale=0.0, workspace=None):
+        """lazyev_pages_weigh: the attention weight that each of the first `length` entries received from the queries q [S,n,Hq,d] (or
+        [n,Hq,d]), whose log-sum-exps `attend` gave, over the tokens that see it and its group's heads, added to `decay` times what the first `known`
+        entries had in `old` (known None: all of them if `old` is given) -> weights fp32 [S,Hkv,m], m >= length (None: a new tensor like `old`, or of
+        `length` entries; what lies behind `length` is left as it is).  weights may be `old`."""
+        pg, device = self.pages, self.device
+        n, n_q_heads, rows, seen, _ = self._queries(length, q, visible, None)
+        _need(lse.shape == rows and lse.dtype is torch.float32 and lse.is_contiguous() and lse.device == device, "lse is fp32, one for each row of q")
+        if weights is None:
+            weights = q.new_empty((pg.n_seqs, pg.n_kv_heads, length if old is None else old.shape[-1]), dtype=torch.float32)
+        self._per_entry(length, torch.float32, weights, old)
+        if known is None:
+            known = 0 if old is None else length
+        _need(0 <= known <= length and (known == 0 or old is not None), "known entries are some of the first `length`, and in `old`")
+        workspace, at, n_bytes = self._bytes(workspace, lib.lazyev_pages_weigh_workspace, pg, length, n, n_q_heads)
+        code = _launch(device, lib.lazyev_pages_weigh, pg, length, n, n_q_heads, seen, q.data_ptr(), lse.data_ptr(), scale,
+                       None if old is None else old.data_ptr(), known, decay, weights.data_ptr(), weights.shape[-1], at, n_bytes)
+        _check(code, "lazyev_pages_weigh")
+        return weights
+
+    def evict(self, length, weights, keep, recent=0, first=0, positions=None, lengths=None, weights_out=None, positions_out=None, sources=None,
+              workspace=None):
+        """lazyev_pages_evict: of the first `length` entries of each row and KV head (lengths int32 [S]: of each row its own number) `keep`
+        stay: the `recent` newest and the `first` ones by `positions` (int32 like weights, None: the entries' numbers) and those of the largest weights
+        (fp32 [S,Hkv,m], m >= length); those that stay from `keep` on move to free places below it -> (sources int32 [S,Hkv,keep],
+        weights_out, positions_out of the places: new tensors [S,Hkv,keep] where none are given; in place: weights and positions themselves)."""
+        pg, device = self.pages, self.device
+        _need(0 <= length <= self.entries, "entries beyond the table's row")
+        _need(1 <= keep < 1 << 30 and 0 <= recent and 0 <= first and recent + first <= keep, "newest and first entries are some of those that stay")
+        self._per_entry(length, torch.float32, weights, None)
+        if positions is not None:
+            self._per_entry(length, torch.int32, positions, weights)
+        if lengths is not None:
+            _need(lengths.dtype is torch.int32 and lengths.shape == (pg.n_seqs,) and lengths.is_contiguous() and lengths.device == device,
+                  "lengths are int32, one for each row, contiguous, on the pages' GPU")
+        shape = (pg.n_seqs, pg.n_kv_heads, keep)
+        if sources is None:
+            sources = weights.new_empty(shape, dtype=torch.int32)
+        if weights_out is None:
+            weights_out = weights.new_empty(shape if positions_out is None else positions_out.shape)
+        if positions_out is None:
+            positions_out = weights.new_empty(weights_out.shape, dtype=torch.int32)
+        _need(sources.shape == shape and sources.dtype is torch.int32 and sources.is_contiguous() and sources.device == device,
+              "sources are int32, [S, Hkv, keep], contiguous, on the pages' GPU")
+        self._per_entry(keep, torch.float32, weights_out, None)
+        self._per_entry(keep, torch.int32, positions_out, weights_out)
+        _need(weights_out.data_ptr() != weights.data_ptr() or weights_out.shape == weights.shape, "in place: the same tensor")
+        workspace, at, n_bytes = self._bytes(workspace, lib.lazyev_pages_evict_workspace, pg, keep)
+        code = _launch(device, lib.lazyev_pages_evict, pg, length, None if lengths is None else lengths.data_ptr(), keep, recent, first,
+                       weights.data_ptr(), None if positions is None else positions.data_ptr(), weights.shape[-1], sources.data_ptr(),
+                       weights_out.data_ptr(), positions_out.data_ptr(), weights_out.shape[-1], at, n_bytes)
+        _check(code, "lazyev_pages_evict")
+        return sources, weights_out, positions_out
+
+    def _queries(self, length, q, visible, joined):
+        """Checks of a call's queries -> (tokens, query heads, the shape of their rows, address of `visible`, addresses of `joined`)."""
+        pg, shape, device = self.pages, q.shape, self.device
+        _need(q.dtype is self.dtype and (len(shape) == 4 and shape[0] == pg.n_seqs or len(shape) == 3 and pg.n_seqs == 1) and
+              shape[-1] == pg.head_dim and q.is_contiguous() and q.device == device,
+              "queries are [S, n, Hq, head_dim] of the table's rows, contiguous, of the pages' type, on their GPU")
+        rows = shape[:-1]
+        _need(self.n_q_heads in (None, shape[-2]), "another number of query heads")
+        _need(0 <= length <= self.entries, "entries beyond the table's row")
+        seen, other = None, (None, None)
+        if joined is not None:
+            o, l = joined
+            _need(o.shape == shape and o.dtype is q.dtype and o.is_contiguous() and o.device == device and
+                  l.shape == rows and l.dtype is torch.float32 and l.is_contiguous() and l.device == device,
+                  "outputs are like q, log-sum-exps fp32, one for each row of q")
+            other = o.data_ptr(), l.data_ptr()
+        if visible is not None:
+            _need(visible.dtype is torch.int32 and visible.shape == shape[:-2] and visible.is_contiguous() and visible.device == device,
+                  "visible is int32, one for each token, contiguous, on the pages' GPU")
+            seen = visible.data_ptr()
+        return shape[-3], shape[-2], rows, seen, other
+
+    def _per_entry(self, length, dtype, x, like):
+        pg = self.pages
+        _need(x.dtype is dtype and x.dim() == 3 and x.shape[:2] == (pg.n_seqs, pg.n_kv_heads) and x.shape[2] >= length and
+              x.is_contiguous() and x.device == self.device and (like is None or like.shape == x.shape and like.dtype in (torch.float32, dtype) and
+                                                                 like.is_contiguous() and like.device == self.device),
+              "numbers of entries are [S, Hkv, m] of at least as many entries, contiguous, on the pages' GPU, of one size in a call")
+
+    def _bytes(self, given, size, *args):
+        """(workspace, its address and bytes) for a call: the given one, or one from torch's allocator for the current stream, to be held until
+        the call is made."""
+        if given is not None:
+            _need(given.dtype == torch.uint8 and given.is_contiguous() and given.device == self.device, "a workspace is bytes on the pages' GPU")
+            return given, given.data_ptr(), given.numel()
+        n = size(*args)
+        given = self.k_pages.new_empty(n, dtype=torch.uint8) if n else None
+        return given, given.data_ptr() if n else None, n
+
     def _workspace(self, length, n_tokens, n_q_heads, given):
         """(workspace, its bytes) for a call: the given one, or one from torch's allocator for the current stream."""
         _need(-1 << 31 <= length < 1 << 31, "a length is a 32-bit number")
@@ -389,6 +536,65 @@ class PagedCache:
             return given, given.numel()
         n = lib.lazyev_pages_attend_workspace(self.pages, length, n_tokens, n_q_heads)
         return (self.k_pages.new_empty(n, dtype=torch.uint8), n) if n else (None, 0)
+
+
+class KeyBounds:
+    """Bounds of the keys of a cache's blocks, and the blocks that tokens read by them.  bounds [S,Hkv,n_blocks,2,d] (smallest, largest
+    element of each of a block's keys), the caller's tensor, whose contents `update` makes; block: entries of a block, 16, 32, 64 or 128."""
+
+    def __init__(self, bounds, block):
+        _need(bounds.is_cuda and bounds.dtype in _DTYPES and bounds.dim() == 5 and bounds.is_contiguous() and bounds.shape[3] == 2 and
+              bounds.shape[4] in (64, 128) and bounds.numel() > 0,
+              "bounds are [S, Hkv, n_blocks, 2, head_dim], contiguous, fp32 or bf16, on a GPU")
+        _need(block in (16, 32, 64, 128), "blocks of 16, 32, 64 or 128 entries")
+        S, H, n, _, d = bounds.shape
+        self.bounds, self.block, self.device, self.dtype = bounds, block, bounds.device, bounds.dtype
+        self.entries = min(n * block, 1 << 30)
+        self.blocks = Blocks(H, d, _DTYPES[self.dtype], S, n, block, bounds.data_ptr())
+
+    @classmethod
+    def of(cls, cache, block, entries=None):
+        """For the rows of a PagedCache, with room for `entries` of each (None: for all that its table has)."""
+        pg = cache.pages
+        n = -(-(cache.entries if entries is None else entries) // block)
+        return cls(cache.k_pages.new_empty((pg.n_seqs, pg.n_kv_heads, n, 2, pg.head_dim)), block)
+
+    def update(self, cache, start, n):
+        """lazyev_blocks_bound: the entries start .. start + n - 1 of the rows of `cache` are counted in (after every append)."""
+        _need(cache.device == self.device, "bounds are on the pages' GPU")
+        _need(0 <= start and 0 <= n and start + n <= min(self.entries, cache.entries), "entries beyond the table's row or the bounds")
+        _check(_launch(self.device, lib.lazyev_blocks_bound, cache.pages, self.blocks, start, n), "lazyev_blocks_bound")
+
+    def choose(self, length, q, n, visible=None, first=0, last=1, out=None, workspace=None):
+        """lazyev_blocks_choose: for each token of q [S,n,Hq,d] (or [n,Hq,d] of a single row) and KV head the `n` blocks it reads of
+        the first `length` entries (visible int32 [S,n]: of those it sees): the first `first`, the last `last` and those with the highest
+        scores -> int32 [S,n,Hkv,n], ascending, -1 behind the last."""
+        b, shape, device = self.blocks, q.shape, self.device
+        _need(q.dtype is self.dtype and (len(shape) == 4 and shape[0] == b.n_seqs or len(shape) == 3 and b.n_seqs == 1) and
+              shape[-1] == b.head_dim and q.is_contiguous() and q.device == device,
+              "queries are [S, n, Hq, head_dim] of the bounds' rows, contiguous, of their type, on their GPU")
+        _need(0 <= length <= self.entries, "entries beyond the bounds")
+        _need(0 <= first and 1 <= last and first + last <= n <= 1 << 20, "first and last blocks are some of those chosen, the last one among them")
+        seen = None
+        if visible is not None:
+            _need(visible.dtype is torch.int32 and visible.shape == shape[:-2] and visible.is_contiguous() and visible.device == device,
+                  "visible is int32, one for each token, contiguous, on the bounds' GPU")
+            seen = visible.data_ptr()
+        to = shape[:-2] + (b.n_kv_heads, n)
+        if out is None:
+            out = q.new_empty(to, dtype=torch.int32)
+        else:
+            _need(out.shape == to and out.dtype is torch.int32 and out.is_contiguous() and out.device == device, "blocks are int32, [S, n, Hkv, chosen]")
+        if workspace is None:
+            n_bytes = lib.lazyev_blocks_choose_workspace(b, length, shape[-3], shape[-2], last, n)
+            workspace = q.new_empty(n_bytes, dtype=torch.uint8) if n_bytes else None
+        else:
+            _need(workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == device, "a workspace is bytes on the bounds' GPU")
+            n_bytes = workspace.numel()
+        code = _launch(device, lib.lazyev_blocks_choose, b, length, shape[-3], shape[-2], seen, q.data_ptr(), first, last, n, out.data_ptr(),
+                       None if workspace is None else workspace.data_ptr(), n_bytes)
+        _check(code, "lazyev_blocks_choose")
+        return out
 
 
 class LazyEviction:

@@ -34,6 +34,11 @@ SOURCES = {"decode_kernels": ("decode_kernels.hip", []),
            "rope_kernels": ("rope_kernels.hip", []),
            "pages_kernels": ("pages_kernels.hip", []),
            "pages_api": ("pages_api.hip", []),
+           # a long cache: which of its blocks a token reads, which entries stay
+           "blocks_kernels": ("blocks_kernels.hip", []),
+           "weigh_kernels": ("weigh_kernels.hip", []),
+           "pages_evict_kernels": ("pages_evict_kernels.hip", []),
+           "blocks_api": ("blocks_api.hip", []),
            "prefill_kernels": ("prefill_kernels.hip", ["-fno-honor-nans"])}
 # measuring aids (plain streaming probes): a library of their own, not part of the path
 BENCH_LIB = os.path.join(LIBDIR, "liblazyev_bench.so")

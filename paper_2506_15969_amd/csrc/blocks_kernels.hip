@@ -1,0 +1,577 @@
+// Blocks of a long cache: bounds of their keys (lazyev_blocks_bound) and the blocks that a token reads (lazyev_blocks_choose).
+//
+// Bounds.  lo[e], hi[e] = smallest and largest element e of the block's keys.  A wave takes a block: its rows in 16-byte chunks, 1 KB
+// a load, minima and maxima in fp32 (exact), then over the lanes that hold the same chunk.  Bound by memory.
+//
+// Choice.  score(b) = max over the heads g of the group of sum_e max(q_ge lo_be, q_ge hi_be): of the keys between the bounds none has a
+// larger product with any of the queries.  The larger of the two terms is the one with hi where q_ge > 0 and with lo where q_ge < 0, so
+// the sums are products of matrices, [q+ | q-] [hi | lo]^T with twice the length, on matrix instructions:
+//   32x32x16_bf16 (fp32 rows: 32x32x2_f32), rows of q as A, blocks as B: lane (c, h) = (l % 32, l / 32) holds, of block c,
+//   the sums of the rows 8 i + 4 h + j (i, j < 4)
+// Rows are heads, every token's filled up to a power of two of them with copies of its last, so that the maximum over a group is one of registers.
+// Numbers that rank are to be the exact ones, whatever order a sum is taken in, and these sums are rounded: each of at most 128 terms that are not zero
+// (the products of bf16 elements are exact) comes with an addition, off by at most 2^-22 of what is added up so far whichever way the
+// matrix instruction rounds, fp32 products with another rounding: a score is within E = 2^-14 max_g |q_g|_1 max_b,e |bound_be| of the exact one.
+// With T the largest but k - 1 of the rounded scores, the exact score of a block
+//   beyond T + 2 E is among the k best: it is above T + E, and so are only blocks whose rounded score is above T, at most k - 1
+//   below T - 2 E is not: it is below T - E, and the k blocks from T on are not
+// and those between, a few, are summed again in binary64, where products are exact and equal blocks give equal sums.
+#include "kernels.h"
+#include "lazyev.h"
+
+#include <cfloat>
+#include <climits>
+
+namespace lazyev {
+namespace {
+
+typedef unsigned short bf16_t;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
+
+__device__ __forceinline__ float bf16_low(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// (a NaN stays)
+__device__ __forceinline__ float lower(float m, float x) { return x < m || x != x ? x : m; }
+__device__ __forceinline__ float upper(float m, float x) { return x > m || x != x ? x : m; }
+
+// ------------------------------------------------------------------------------------ bounds
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void bound_kernel(const BoundArgs a) {
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int C = D * static_cast<int>(sizeof(T)) / 16, kRows = 64 / C, kElems = 16 / static_cast<int>(sizeof(T));
+  constexpr int kAhead = 4;                        // loads of a wave on their way together
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long at = static_cast<long long>(blockIdx.x) * 4 + wave;
+  if (at >= static_cast<long long>(a.units) * a.touched) return;
+  const int unit = static_cast<int>(at / a.touched), b = a.first_block + static_cast<int>(at - static_cast<long long>(unit) * a.touched);
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+  const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
+  const int first = max(a.start, b * a.block), end = min(a.end, (b + 1) * a.block);
+  const int chunk = lane % C;
+  float lo[kElems], hi[kElems];
+#pragma unroll
+  for (int e = 0; e < kElems; ++e) {
+    lo[e] = INFINITY;
+    hi[e] = -INFINITY;
+  }
+  auto count = [&](u32x4_t w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) {
+      const float x = kF32 ? __uint_as_float(w[e % 4]) : e % 2 ? bf16_high(w[e / 2]) : bf16_low(w[e / 2]);
+      lo[e] = lower(lo[e], x);
+      hi[e] = upper(hi[e], x);
+    }
+  };
+  for (int e0 = first + lane / C; e0 - lane / C < end; e0 += kRows * kAhead) {
+    u32x4_t w[kAhead];
+    bool there[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int entry = min(e0 + u * kRows, end - 1), pg = page_of(a.pages, entry);
+      const unsigned no = static_cast<unsigned>(table[pg]);
+      there[u] = e0 + u * kRows < end && no < static_cast<unsigned>(a.pages.n_pages);
+      const unsigned row = (there[u] ? no : 0u) * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+      w[u] = *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(a.k_pages) + static_cast<size_t>(row) * (D * sizeof(T)) + chunk * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (there[u]) count(w[u]);
+  }
+  char *to = static_cast<char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + chunk * 16;
+  if (b * a.block < a.start) {                     // entries before have been counted
+    const u32x4_t l = *reinterpret_cast<const u32x4_t *>(to), u = *reinterpret_cast<const u32x4_t *>(to + D * sizeof(T));
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) {
+      lo[e] = lower(lo[e], kF32 ? __uint_as_float(l[e % 4]) : e % 2 ? bf16_high(l[e / 2]) : bf16_low(l[e / 2]));
+      hi[e] = upper(hi[e], kF32 ? __uint_as_float(u[e % 4]) : e % 2 ? bf16_high(u[e / 2]) : bf16_low(u[e / 2]));
+    }
+  }
+#pragma unroll
+  for (int o = C; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) {
+      lo[e] = lower(lo[e], __shfl_xor(lo[e], o));
+      hi[e] = upper(hi[e], __shfl_xor(hi[e], o));
+    }
+  if (lane >= 2 * C) return;                       // (the first C lanes store the lower bounds, the next ones the upper)
+  const bool up = lane >= C;
+  u32x4_t w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (kF32) w[e] = __float_as_uint(up ? hi[e] : lo[e]);
+    else w[e] = __float_as_uint(up ? hi[2 * e] : lo[2 * e]) >> 16 | (__float_as_uint(up ? hi[2 * e + 1] : lo[2 * e + 1]) & 0xFFFF0000u);
+  }
+  *reinterpret_cast<u32x4_t *>(to + (up ? D * sizeof(T) : 0)) = w;
+}
+
+// ------------------------------------------------------------------------------------ scores
+
+// 16 bytes of a row of queries: its elements above zero, and those below.  (Of a NaN's two copies one is a NaN.)
+template <bool kF32>
+__device__ __forceinline__ void by_sign(u32x4_t w, u32x4_t &pos, u32x4_t &neg) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    unsigned minus;
+    if constexpr (kF32) minus = static_cast<unsigned>(static_cast<int>(w[e]) >> 31);
+    else minus = ((w[e] >> 15) & 0x00010001u) * 0xFFFFu;
+    pos[e] = w[e] & ~minus;
+    neg[e] = w[e] & minus;
+  }
+}
+
+template <bool kF32>
+__device__ __forceinline__ float largest_of(u32x4_t w) {                // in size; a NaN, if there is one
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (kF32) m = upper(m, fabsf(__uint_as_float(w[e])));
+    else m = upper(upper(m, fabsf(bf16_low(w[e]))), fabsf(bf16_high(w[e])));
+  }
+  return m;
+}
+
+// Elements at any address of their own type.
+template <typename T>
+__device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
+  if (wide) return *reinterpret_cast<const u32x4_t *>(p);
+  T e[16 / sizeof(T)];
+#pragma unroll
+  for (int x = 0; x < static_cast<int>(16 / sizeof(T)); ++x) e[x] = p[x];
+  u32x4_t w;
+  __builtin_memcpy(&w, e, 16);
+  return w;
+}
+
+// A wave has 32 blocks of a unit (x: the unit and 128 blocks of it) and goes over the tokens of its share (y) of the launch's, 32 / kPad of
+// them at a time; a token's group of up to 64 heads comes in passes of 32.
+template <typename T, int D, int kPad>
+__global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = lane & 31, h = lane >> 5;
+  const int across = (a.scored + 127) / 128, unit = static_cast<int>(blockIdx.x) / across;
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  const int b0 = (static_cast<int>(blockIdx.x) - unit * across) * 128 + wave * 32;
+  if (b0 >= a.scored) return;
+  const int b = min(b0 + c, a.scored - 1);
+  u32x4_t lo[kOps], hi[kOps];
+  const char *from = static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + h * 16;
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+  if (blockIdx.y == 0) {
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) m = upper(upper(m, largest_of<kF32>(lo[j])), largest_of<kF32>(hi[j]));
+    m = upper(m, __shfl_xor(m, 32));
+    if (h == 0 && b0 + c < a.scored) a.peak[static_cast<size_t>(unit) * a.scored + b0 + c] = m;
+  }
+  const int tiles = (a.tokens + kTokens - 1) / kTokens;
+  const T *q = static_cast<const T *>(a.q) + static_cast<size_t>(kvh) * a.group * D + h * (16 / sizeof(T));
+  for (int tile = static_cast<int>(blockIdx.y); tile < tiles; tile += static_cast<int>(gridDim.y)) {
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};        // (passes of 32 heads)
+    float out[16];
+    for (int pass = 0; pass < (kPad == 32 ? (a.group + 31) / 32 : 1); ++pass) {
+      const int token = a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1), head = min(pass * 32 + c % kPad, a.group - 1);
+      const T *row = q + ((static_cast<size_t>(seq) * a.n_tokens + token) * a.n_q_heads + head) * D;
+      f32x16_t s;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        u32x4_t pos, neg;
+        by_sign<kF32>(load_chunk(row + j * (32 / sizeof(T)), a.wide), pos, neg);
+        if constexpr (kF32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[j][e]), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[j][e]), s, 0, 0, 0);
+          }
+        } else {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi[j]), s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo[j]), s, 0, 0, 0);
+        }
+      }
+      // rows 8 i + 4 h + j in s[4 i + j]: the maxima of kPad rows next to one another
+      if constexpr (kPad == 1) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) out[x] = s[x];
+      } else if constexpr (kPad == 2) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) out[x] = upper(s[2 * x], s[2 * x + 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float m = upper(upper(s[4 * i], s[4 * i + 1]), upper(s[4 * i + 2], s[4 * i + 3]));
+          if constexpr (kPad > 4) m = upper(m, __shfl_xor(m, 32));
+          out[i] = m;
+        }
+        if constexpr (kPad >= 16) {
+          out[0] = upper(out[0], out[1]);
+          out[1] = upper(out[2], out[3]);
+        }
+        if constexpr (kPad == 32) {
+          top[0] = upper(top[0], upper(out[0], out[1]));
+          out[0] = top[0];
+        }
+      }
+    }
+    auto store = [&](int token, float x) __attribute__((always_inline)) {
+      const int t = tile * kTokens + token;
+      if (t < a.tokens && b0 + c < a.scored)
+        a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b0 + c] = x;
+    };
+    if constexpr (kPad == 1) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) store(8 * (x / 4) + 4 * h + x % 4, out[x]);
+    } else if constexpr (kPad == 2) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) store(4 * (x / 2) + 2 * h + x % 2, out[x]);
+    } else if constexpr (kPad == 4) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) store(2 * x + h, out[x]);
+    } else if (h == 0) {
+#pragma unroll
+      for (int x = 0; x < kTokens; ++x) store(x, out[x]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ choice
+
+// Numbers in the order of the values (a NaN: the largest); 0 is below all of them.
+__device__ __forceinline__ unsigned order_of(float x) {
+  const unsigned u = __float_as_uint(x + 0.f);     // (-0 and 0 are one)
+  return x != x ? 0xFFFFFFFFu : u ^ (static_cast<unsigned>(static_cast<int>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ unsigned long long order_of(double x) {
+  const unsigned long long u = __double_as_longlong(x + 0.0);
+  return x != x ? ~0ull : u ^ (static_cast<unsigned long long>(static_cast<long long>(u) >> 63) | 1ull << 63);
+}
+
+constexpr int kChooseBlock = 256, kChooseWaves = kChooseBlock / 64;
+constexpr int kAgain = 512;             // blocks between the borders whose exact scores LDS holds
+
+// The largest key that at least `want` of n keys key(i) reach, 1 <= want <= n, in steps of a bit; counts in LDS.  All threads call it.
+template <typename K, typename F>
+__device__ K kth_largest(int n, int want, int *counts /*[2][kChooseWaves]*/, F key) {
+  K t = 0;
+  int turn = 0;
+  for (int bit = static_cast<int>(sizeof(K)) * 8 - 1; bit >= 0; --bit, turn ^= 1) {
+    const K cand = t | static_cast<K>(1) << bit;
+    int have = 0;
+    for (int i0 = 0; i0 < n; i0 += kChooseBlock) {
+      const int i = i0 + static_cast<int>(threadIdx.x);
+      have += __popcll(__ballot(i < n && key(min(i, n - 1)) >= cand));
+    }
+    if ((threadIdx.x & 63) == 0) counts[turn * kChooseWaves + (threadIdx.x >> 6)] = have;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kChooseWaves; ++w) all += counts[turn * kChooseWaves + w];
+    if (all >= want) t = cand;
+    if (all == want) break;                        // (exactly these)
+  }
+  __syncthreads();
+  return t;
+}
+
+// One block for a token and KV head.
+template <typename T, int D>
+__global__ __launch_bounds__(kChooseBlock) void choose_kernel(const ChooseArgs a) {
+  constexpr bool kF32 = sizeof(T) == 4;
+  __shared__ int counts[2 * kChooseWaves];
+  __shared__ float wave_f[2][kChooseWaves];
+  __shared__ double exact[kAgain];
+  __shared__ int again[kAgain], n_shared[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long row = blockIdx.x;                // (sequence, token of the launch, KV head)
+  const int kvh = static_cast<int>(row % a.n_kv_heads);
+  const int t = static_cast<int>(row / a.n_kv_heads % a.tokens), seq = static_cast<int>(row / a.n_kv_heads / a.tokens);
+  const long long token = static_cast<long long>(seq) * a.n_tokens + a.token0 + t;
+  int32_t *to = a.chosen + (token * a.n_kv_heads + kvh) * a.n_chosen;
+  const int seen = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
+  const int nb = (seen + a.block - 1) / a.block;
+  if (nb <= a.n_chosen) {
+    for (int i = threadIdx.x; i < a.n_chosen; i += kChooseBlock) to[i] = i < nb ? i : -1;
+    return;
+  }
+  // candidates are the blocks first .. first + n - 1, of which `want` go
+  const int n = nb - a.n_last - a.n_first, want = a.n_chosen - a.n_last - a.n_first;
+  const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + kvh;
+  const float *score = a.score + static_cast<size_t>(row) * a.scored + a.n_first, *peak = a.peak + unit * a.scored + a.n_first;
+  const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + static_cast<long long>(kvh) * a.group) * D;
+  for (int i = threadIdx.x; i < a.n_first; i += kChooseBlock) to[i] = i;
+  for (int i = threadIdx.x; i < a.n_last; i += kChooseBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
+  if (want == 0) return;
+
+  // how far a score may be off
+  float most = 0.f, size = 0.f;                    // largest bound; largest |q|_1
+  bool odd = false;
+  for (int i = threadIdx.x; i < n; i += kChooseBlock) {
+    most = upper(most, peak[i]);
+    odd |= !(fabsf(score[i]) <= FLT_MAX);
+  }
+  for (int g = wave; g < a.group; g += kChooseWaves) {
+    float s = 0.f;
+    for (int e = lane; e < D; e += 64) {
+      float x;
+      if constexpr (kF32) x = q[g * D + e];
+      else x = __uint_as_float(static_cast<unsigned>(q[g * D + e]) << 16);
+      s += fabsf(x);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+    size = upper(size, s);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) most = upper(most, __shfl_xor(most, o));
+  if (lane == 0) {
+    wave_f[0][wave] = most;
+    wave_f[1][wave] = size;
+  }
+  odd = __syncthreads_or(odd);
+#pragma unroll
+  for (int w = 0; w < kChooseWaves; ++w) {
+    most = upper(most, wave_f[0][w]);
+    size = upper(size, wave_f[1][w]);
+  }
+  // (2^-100: products too small for fp32; none of a row of zeros)
+  const float off = size == 0.f && most <= FLT_MAX ? 0.f : size * most * 0x1p-14f + 0x1p-100f;
+  const bool all_again = odd || !(size * most < 0x1p120f);
+
+  // the borders: surely taken from `sure` on, surely not below `out`
+  unsigned sure = 0xFFFFFFFFu, out = 0u;
+  if (!all_again) {
+    const unsigned kth = kth_largest<unsigned>(n, want, counts, [&](int i) { return order_of(score[i]); });
+    const float x = value_of(kth);
+    // (both borders are moved outwards by a step of their own rounding)
+    sure = order_of(x + 2.f * off) + (off > 0.f ? 1 : 0);
+    out = order_of(x - 2.f * off) - (off > 0.f ? 1 : 0);
+    if (!(off > 0.f)) sure += 1;                   // above T, surely; equal scores: by their numbers
+  }
+  auto key = [&](int i) __attribute__((always_inline)) { return all_again ? 1u : order_of(score[i]); };
+  // their numbers, and the list of those between
+  if (threadIdx.x < 4) n_shared[threadIdx.x] = 0;
+  __syncthreads();
+  int n_sure = 0, n_between = 0;
+  for (int i0 = 0; i0 < n; i0 += kChooseBlock) {
+    const int i = i0 + static_cast<int>(threadIdx.x);
+    const unsigned k = i < n ? key(i) : 0u;
+    n_sure += __popcll(__ballot(i < n && !all_again && k >= sure));
+    n_between += __popcll(__ballot(i < n && (all_again || (k < sure && k >= out))));
+  }
+  if (lane == 0) {
+    atomicAdd(&n_shared[0], n_sure);
+    atomicAdd(&n_shared[1], n_between);
+  }
+  __syncthreads();
+  n_sure = n_shared[0];
+  n_between = n_shared[1];
+  const int rest = want - n_sure;                  // to take of those between, 1 .. n_between
+  auto between = [&](unsigned k) __attribute__((always_inline)) { return all_again || (k < sure && k >= out); };
+
+  // exact score of a block, for all lanes: a lane has D / 8 elements of one of eight heads
+  auto exact_score = [&](int i) __attribute__((always_inline)) {
+    constexpr int kPart = D / 8;
+    const T *bounds = static_cast<const T *>(a.bounds) + (unit * a.n_blocks + a.n_first + i) * (2 * D) + lane % 8 * kPart;
+    double best = -INFINITY;
+    for (int g0 = 0; g0 < a.group; g0 += 8) {
+      const T *mine = q + min(g0 + lane / 8, a.group - 1) * D + lane % 8 * kPart;
+      double s = 0.0;
+#pragma unroll 4
+      for (int e = 0; e < kPart; ++e) {
+        double x, l, u;
+        if constexpr (kF32) {
+          x = mine[e]; l = bounds[e]; u = bounds[D + e];
+        } else {
+          x = __uint_as_float(static_cast<unsigned>(mine[e]) << 16);
+          l = __uint_as_float(static_cast<unsigned>(bounds[e]) << 16);
+          u = __uint_as_float(static_cast<unsigned>(bounds[D + e]) << 16);
+        }
+        const double y = x > 0.0 ? x * u : x * l;  // (a NaN is a NaN)
+        s += x == 0.0 ? 0.0 : y;
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
+      s = s != s ? INFINITY : s;
+      best = s > best ? s : best;
+    }
+#pragma unroll
+    for (int o = 8; o < 64; o <<= 1) {
+      const double x = __shfl_xor(best, o);
+      best = x > best ? x : best;
+    }
+    return best;
+  };
+
+  unsigned long long border = 0;                   // of the exact scores of those between: taken above it, and `equal` of those at it
+  int equal = INT_MAX;
+  const bool few = n_between <= kAgain;
+  unsigned long long *wide = a.exact ? a.exact + static_cast<size_t>(row) * a.scored : nullptr;
+  const bool ask = off > 0.f || all_again;         // (without: rounded scores are the exact ones)
+  if (!ask) {
+    equal = rest;
+  } else if (rest == 0) {
+    border = ~0ull;
+    equal = 0;
+  } else if (rest < n_between) {
+    if (few) {                                     // the list, in the order of the blocks
+      if (wave == 0) {
+        int at = 0;
+        for (int i0 = 0; i0 < n; i0 += 64) {
+          const bool mine = i0 + lane < n && between(key(min(i0 + lane, n - 1)));
+          const unsigned long long m = __ballot(mine);
+          if (mine) again[at + __popcll(m & ((1ull << lane) - 1))] = i0 + lane;
+          at += __popcll(m);
+        }
+      }
+      __syncthreads();
+      for (int x = wave; x < n_between; x += kChooseWaves) {
+        const double s = exact_score(again[x]);
+        if (lane == 0) exact[x] = s;
+      }
+      __syncthreads();
+      border = kth_largest<unsigned long long>(n_between, rest, counts, [&](int i) { return order_of(exact[i]); });
+    } else {
+      for (int i = wave; i < n; i += kChooseWaves) {
+        unsigned long long k = 0;
+        if (between(key(i))) k = order_of(exact_score(i));
+        if (lane == 0) wide[i] = k;
+      }
+      __syncthreads();
+      border = kth_largest<unsigned long long>(n, rest, counts, [&](int i) { return wide[i]; });
+    }
+    int above = 0;
+    for (int i0 = 0; i0 < (few ? n_between : n); i0 += kChooseBlock) {
+      const int i = i0 + static_cast<int>(threadIdx.x);
+      above += __popcll(__ballot(i < (few ? n_between : n) && (few ? order_of(exact[min(i, n_between - 1)]) : wide[min(i, n - 1)]) > border));
+    }
+    if (lane == 0) atomicAdd(&n_shared[2], above);
+    __syncthreads();
+    equal = rest - n_shared[2];
+  }
+  // the list, by one wave
+  if (wave != 0) return;
+  int at = a.n_first, met = 0, seen_between = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int i = i0 + lane;
+    const unsigned k = i < n ? key(i) : 0u;
+    bool take = i < n && !all_again && k >= sure;
+    const bool mid = i < n && between(k) && !take;
+    const unsigned long long m_mid = __ballot(mid), below = (1ull << lane) - 1;
+    bool same = false;
+    if (mid) {
+      if (!ask) same = true;
+      else if (rest >= n_between) take = true;
+      else {
+        const unsigned long long x = few ? order_of(exact[seen_between + __popcll(m_mid & below)]) : wide[i];
+        take = x > border;
+        same = x == border;
+      }
+    }
+    const unsigned long long m_same = __ballot(same);
+    if (same && met + __popcll(m_same & below) < equal) take = true;
+    const unsigned long long m = __ballot(take);
+    if (take) to[at + __popcll(m & below)] = a.n_first + i;
+    at += __popcll(m);
+    met += __popcll(m_same);
+    seen_between += __popcll(m_mid);
+  }
+}
+
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Tokens of a launch: the scores of all of them stay in the on-chip cache (256 MB).
+constexpr size_t kScoreBytes = 96u << 20;
+int tokens_of(const ChooseArgs &a) {
+  const size_t per_token = static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.scored * 12;
+  const size_t most = (1u << 23) / (static_cast<size_t>(a.n_seqs) * a.n_kv_heads);   // (a launch has 2^32 threads at most)
+  size_t n = per_token > 0 ? kScoreBytes / per_token : a.n_tokens;
+  n = n < most ? n : most;
+  return static_cast<int>(n < 1 ? 1 : n < static_cast<size_t>(a.n_tokens) ? n : a.n_tokens);
+}
+
+template <typename T, int D>
+hipError_t launch_scores(const ChooseArgs &a, int pad, hipStream_t stream) {
+  const int tiles = (a.tokens + 32 / pad - 1) / (32 / pad);
+  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.scored + 127) / 128);
+  if (blocks > (1 << 22)) return hipErrorInvalidValue;
+  int shares = 1;                                  // of the tokens: a few blocks for every compute unit
+  while (shares < tiles && shares * blocks < 1024) shares *= 2;
+  if (shares > tiles) shares = tiles;
+  const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(shares));
+  switch (pad) {
+    case 1: hipLaunchKernelGGL((score_kernel<T, D, 1>), grid, dim3(256), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((score_kernel<T, D, 2>), grid, dim3(256), 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((score_kernel<T, D, 4>), grid, dim3(256), 0, stream, a); break;
+    case 8: hipLaunchKernelGGL((score_kernel<T, D, 8>), grid, dim3(256), 0, stream, a); break;
+    case 16: hipLaunchKernelGGL((score_kernel<T, D, 16>), grid, dim3(256), 0, stream, a); break;
+    default: hipLaunchKernelGGL((score_kernel<T, D, 32>), grid, dim3(256), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch(ChooseArgs a, hipStream_t stream) {
+  int pad = 1;
+  while (pad < a.group && pad < 32) pad *= 2;
+  a.wide = reinterpret_cast<uintptr_t>(a.q) % 16 == 0;
+  const int each = tokens_of(a);
+  const size_t rows = static_cast<size_t>(a.n_seqs) * each * a.n_kv_heads;
+  if (a.scored > 0) {
+    char *w = static_cast<char *>(a.workspace);
+    a.peak = reinterpret_cast<float *>(w);
+    w += align_up(static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.scored * 4);
+    a.score = reinterpret_cast<float *>(w);
+    w += align_up(rows * a.scored * 4);
+    a.exact = reinterpret_cast<unsigned long long *>(w);
+  }
+  for (a.token0 = 0; a.token0 < a.n_tokens; a.token0 += each) {
+    a.tokens = a.n_tokens - a.token0 < each ? a.n_tokens - a.token0 : each;
+    if (a.scored > 0) {
+      const hipError_t e = launch_scores<T, D>(a, pad, stream);
+      if (e != hipSuccess) return e;
+    }
+    const long long blocks = static_cast<long long>(a.n_seqs) * a.tokens * a.n_kv_heads;
+    if (blocks > (1ll << 23)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((choose_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kChooseBlock), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_bound(const BoundArgs &a, hipStream_t stream) {
+  const long long blocks = (static_cast<long long>(a.units) * a.touched + 3) / 4;
+  if (blocks < 1 || blocks > (1ll << 23)) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 64) hipLaunchKernelGGL((bound_kernel<float, 64>), grid, dim3(256), 0, stream, a);
+  else if (a.dtype == LAZYEV_DTYPE_FP32) hipLaunchKernelGGL((bound_kernel<float, 128>), grid, dim3(256), 0, stream, a);
+  else if (a.head_dim == 64) hipLaunchKernelGGL((bound_kernel<bf16_t, 64>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((bound_kernel<bf16_t, 128>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+size_t choose_workspace(const ChooseArgs &a) {
+  if (a.scored <= 0) return 0;
+  const size_t rows = static_cast<size_t>(a.n_seqs) * tokens_of(a) * a.n_kv_heads;
+  return align_up(static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.scored * 4) + align_up(rows * a.scored * 4) + align_up(rows * a.scored * 8);
+}
+
+hipError_t launch_choose(const ChooseArgs &a, hipStream_t stream) {
+  if (a.dtype == LAZYEV_DTYPE_FP32) return a.head_dim == 64 ? launch<float, 64>(a, stream) : launch<float, 128>(a, stream);
+  return a.head_dim == 64 ? launch<bf16_t, 64>(a, stream) : launch<bf16_t, 128>(a, stream);
+}
+
+}  // namespace lazyev

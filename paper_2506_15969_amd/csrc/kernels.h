@@ -244,6 +244,15 @@ struct RopeCut {
 RopeCut rope_cut(long long tokens, int heads, int elem /*bytes*/, int head_dim);
 hipError_t launch_rope(const RopeArgs &a, int dtype, int head_dim, hipStream_t stream);
 
+// Attention over the entries of listed blocks (see lazyev_blocks_attend): a "sequence" of the arguments is a token of one, n_tokens is 1, and
+// `length` counts the entries of the list.
+struct ListArgs {
+  const int32_t *list;              // [n_seqs][n_kv_heads][n_listed]
+  int32_t n_listed, block_shift;    // entries of a block: 1 << block_shift
+  int32_t tokens;                   // of a sequence: n_seqs of the arguments / tokens table rows
+  int32_t entries;                  // of a table row: what `visible` goes up to
+  int32_t run_shift;                // entries next to one another in a page and in a block: runs of 1 << run_shift
+};
 // Attention over pages (see lazyev_pages_attend).
 struct AttendArgs {
   int32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
@@ -265,9 +274,79 @@ struct AttendArgs {
   // filled in by the launch: splits of the entries and what they leave in the workspace; all rows at multiples of 16 bytes
   int32_t n_split, split_keys, wide;
   float *part_o, *part_ml, *part_lse;
+  ListArgs list;                    // of launch_attend_list
 };
 size_t attend_workspace(const AttendArgs &a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);
+size_t attend_list_workspace(const AttendArgs &a);
+hipError_t launch_attend_list(const AttendArgs &a, hipStream_t stream);
+
+// Bounds of blocks of keys (see lazyev_blocks_bound).
+struct BoundArgs {
+  int32_t units, n_kv_heads, head_dim, dtype;
+  int32_t start, end;               // the entries to be counted in
+  int32_t block, first_block, touched, n_blocks;   // the blocks that they lie in; blocks of a unit in `bounds`
+  const void *k_pages;
+  PageTable pages;
+  void *bounds;
+};
+hipError_t launch_bound(const BoundArgs &a, hipStream_t stream);
+
+// The blocks that tokens read (see lazyev_blocks_choose).
+struct ChooseArgs {
+  int32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
+  int32_t head_dim, dtype;
+  int32_t length, block, n_blocks;
+  int32_t n_first, n_last, n_chosen;
+  int32_t scored;                   // blocks 0 .. scored - 1 have scores (0: no token has to choose)
+  const int32_t *visible;
+  const void *q, *bounds;
+  int32_t *chosen;
+  void *workspace;
+  // filled in by the launch: the tokens of each sequence that it is for; what it leaves in the workspace
+  int32_t token0, tokens, wide;
+  float *peak;                      // [units][scored] largest bound of a block, in size
+  float *score;                     // [n_seqs][tokens][n_kv_heads][scored]
+  unsigned long long *exact;        // the same, of some blocks
+};
+size_t choose_workspace(const ChooseArgs &a);
+hipError_t launch_choose(const ChooseArgs &a, hipStream_t stream);
+
+// Weights that entries received (see lazyev_pages_weigh).
+struct WeighArgs {
+  int32_t n_seqs, n_tokens, n_q_heads, n_kv_heads, group;
+  int32_t head_dim, dtype;
+  int32_t length, known;
+  float scale, decay;
+  const int32_t *visible;
+  const void *q, *k_pages;
+  const float *lse, *old;
+  PageTable pages;
+  float *weights;
+  int64_t stride;                   // of old and weights, from unit to unit
+  float *part;                      // workspace: [n_split][units][length]
+  int32_t n_split, wide;            // filled in by the launch
+};
+size_t weigh_workspace(const WeighArgs &a);
+hipError_t launch_weigh(WeighArgs a, hipStream_t stream);
+
+// Eviction by weight (see lazyev_pages_evict).
+struct WeightEvictArgs {
+  int32_t n_seqs, n_kv_heads, head_dim, dtype;
+  int32_t length, keep, n_recent, n_first;
+  const int32_t *lengths;
+  const float *weights;
+  const int32_t *positions;
+  int64_t stride, to_stride;        // from unit to unit
+  int32_t *sources;                 // [units][keep]
+  float *weights_to;
+  int32_t *positions_to;
+  void *k_pages, *v_pages;
+  PageTable pages;
+  int32_t *free_places;             // workspace: [units][keep]
+};
+size_t weight_evict_workspace(const WeightEvictArgs &a);
+hipError_t launch_weight_evict(WeightEvictArgs a, hipStream_t stream);
 
 // `ev`, when not null, points at three events recorded before the first kernel, between the two
 // kernels and after the second (per-kernel timing for the profiling aid).

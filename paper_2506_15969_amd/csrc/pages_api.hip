@@ -7,11 +7,37 @@
 
 #include "pages_api.h"
 
-namespace {
+namespace lazyev {
 
 bool dtype_ok(int32_t dtype, int32_t head_dim) {
   return (dtype == LAZYEV_DTYPE_FP32 || dtype == LAZYEV_DTYPE_BF16) && (head_dim == 64 || head_dim == 128);
 }
+
+bool pages_ok(const lazyev_pages *p) {
+  if (!p || !dtype_ok(p->dtype, p->head_dim)) return false;
+  if (p->n_kv_heads < 1 || p->n_kv_heads > 65535 || p->n_pages < 1 || p->page_size < 1 || p->page_size > (1 << 20)) return false;
+  if (p->n_seqs < 1 || p->table_stride < 1) return false;
+  // (a pool's rows have 32-bit numbers; the product of the two is below 2^36)
+  if (p->n_pages > (1ll << 32) / (static_cast<long long>(p->n_kv_heads) * p->page_size)) return false;
+  if (!p->k_pages || !p->v_pages || !p->table) return false;
+  return reinterpret_cast<uintptr_t>(p->k_pages) % 16 == 0 && reinterpret_cast<uintptr_t>(p->v_pages) % 16 == 0 &&
+         reinterpret_cast<uintptr_t>(p->table) % 4 == 0;
+}
+
+PageTable page_table(const lazyev_pages &p) {
+  PageTable t;
+  t.table = p.table; t.stride = p.table_stride; t.n_pages = p.n_pages; t.page_size = p.page_size;
+  page_div(t);
+  return t;
+}
+
+}  // namespace lazyev
+
+namespace {
+
+using lazyev::dtype_ok;
+using lazyev::page_table;
+using lazyev::pages_ok;
 
 // Pointers start at a whole element (any: there are rows at all); strides beyond any memory are refused, so that no product with a
 // number of tokens or heads that are there overflows.
@@ -51,24 +77,6 @@ void set_rotation(lazyev::RopeArgs &a, const lazyev_rotation &r) {
   a.half = r.layout == LAZYEV_ROPE_NONE ? 0 : r.dims / 2;
   a.eps = r.eps;
   a.inv_freq = r.inv_freq;
-}
-
-bool pages_ok(const lazyev_pages *p) {
-  if (!p || !dtype_ok(p->dtype, p->head_dim)) return false;
-  if (p->n_kv_heads < 1 || p->n_kv_heads > 65535 || p->n_pages < 1 || p->page_size < 1 || p->page_size > (1 << 20)) return false;
-  if (p->n_seqs < 1 || p->table_stride < 1) return false;
-  // (a pool's rows have 32-bit numbers; the product of the two is below 2^36)
-  if (p->n_pages > (1ll << 32) / (static_cast<long long>(p->n_kv_heads) * p->page_size)) return false;
-  if (!p->k_pages || !p->v_pages || !p->table) return false;
-  return reinterpret_cast<uintptr_t>(p->k_pages) % 16 == 0 && reinterpret_cast<uintptr_t>(p->v_pages) % 16 == 0 &&
-         reinterpret_cast<uintptr_t>(p->table) % 4 == 0;
-}
-
-lazyev::PageTable page_table(const lazyev_pages &p) {
-  lazyev::PageTable t;
-  t.table = p.table; t.stride = p.table_stride; t.n_pages = p.n_pages; t.page_size = p.page_size;
-  lazyev::page_div(t);
-  return t;
 }
 
 }  // namespace

@@ -237,7 +237,10 @@ struct Shape {
 };
 constexpr int kWindow = 512;            // page numbers that a block keeps in LDS
 
-template <typename T, int D, int kWR, int kWK, int kKeys>
+// Entries of listed blocks (kListed: a unit is a token of a sequence and a KV head): entry x of the list is entry x % block of block list[x / block].
+// What a table of pages says of the others, the window says of runs of 1 << run_shift entries, which lie next to one another in a block
+// and in a page: the row of the first one and how many of them the token sees; those beyond are holes, as pages that are none.
+template <typename T, int D, int kWR, int kWK, int kKeys, bool kListed = false>
 __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPerSimd)) void attend_kernel(const AttendArgs a) {
   using R = Rows<T, D>;
   using S = Shape<T, D, kWR, kWK, kKeys>;
@@ -246,6 +249,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   __shared__ int window[kWindow];
   __shared__ float shared_ml[kWK][kWR][64];
   __shared__ int shared_most[S::kWaves], shared_least[S::kWaves], shared_hole[2], shared_odd;
+  __shared__ int window_seen[kListed ? kWindow : 1], stage_seen[2][kListed ? kKeys : 1];   // (kListed) entries of a run that the token sees
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
@@ -261,7 +265,10 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
 
   // entries of this block: first .. last - 1
   const int first = split * a.split_keys, last = min(first + a.split_keys, a.length);
-  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+  const int32_t *table = a.pages.table + static_cast<long long>(kListed ? seq / a.list.tokens : seq) * a.pages.stride;
+  const int32_t *list = kListed ? a.list.list + static_cast<long long>(unit) * a.list.n_listed : nullptr;
+  // (what the window goes by: a page, or a run)
+  auto slot_of = [&](int entry) __attribute__((always_inline)) { return kListed ? entry >> a.list.run_shift : page_of(a.pages, entry); };
   // everything that is read before the first stage is worked on is asked for at once
   u32x4_t qb[kOps];
   {
@@ -280,32 +287,56 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
   }
   const float lse_other = lse_joined(a, place);
-  int seen = a.visible ? min(max(a.visible[place.token], 0), a.length) : a.length;
+  int seen = a.visible ? min(max(a.visible[place.token], 0), kListed ? a.list.entries : a.length) : kListed ? a.list.entries : a.length;
+  const int reach = seen;                          // (kListed: entries of the table row that the unit's token sees)
+  if constexpr (kListed) seen = reach > 0 ? a.length : 0;
 
   // ---- stages on their way to LDS.  Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as
   // the compiler has every read of LDS wait for all loads into it: they leave nothing in registers, and the waits for
   // them are in `arrived`.)
-  const bool once = gridDim.z == 1;                // nobody else reads these entries (uniform): they need not stay in the caches
+  const bool once = gridDim.z == 1 && (!kListed || a.list.tokens == 1);   // nobody else reads these entries (uniform): they need not stay in the caches
   const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
   auto load_1k = [&](const char *from, unsigned to) __attribute__((always_inline)) {
     if (once) __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
     else __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
   };
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
+  // The row of the pools that a run begins with, and the entries of it that are there and that the token sees.
+  auto run_at = [&](int slot, int &n) __attribute__((always_inline)) {
+    const int shift = a.list.block_shift - a.list.run_shift, b = list[slot >> shift];
+    const int in_block = (slot & ((1 << shift) - 1)) << a.list.run_shift;
+    n = 0;
+    if (b < 0 || b > (reach - 1) >> a.list.block_shift) return 0u;
+    const int entry = (b << a.list.block_shift) + in_block;
+    if (entry >= reach) return 0u;
+    const int pg = page_of(a.pages, entry);
+    const unsigned no = static_cast<unsigned>(table[pg]);
+    if (no >= static_cast<unsigned>(a.pages.n_pages)) return 0u;
+    n = min(1 << a.list.run_shift, reach - entry);
+    return no * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+  };
+  int window_at = slot_of(first);
   // Entries from e0 on, none beyond `limit`, to a stage's place; page numbers by number(page of the entry, load).  -> was one of them none?
   auto load_stage = [&](int e0, int limit, int buf, auto number) __attribute__((always_inline)) {
     bool hole = false;
 #pragma unroll
     for (int u = 0; u < S::kLoads; ++u) {
       const int r = (u * S::kWaves + wave) * S::kPerLoad + lane / C;
-      const int entry = min(e0 + r, limit), pg = page_of(a.pages, entry);
-      unsigned no = static_cast<unsigned>(number(pg, u));
-      if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
-        hole = true;
-        no = 0;
+      const int entry = min(e0 + r, limit), pg = slot_of(entry);
+      unsigned no = static_cast<unsigned>(number(pg, u)), pool_row;
+      if constexpr (kListed) {
+        const int n = window_seen[pg - window_at], at = entry & ((1 << a.list.run_shift) - 1);
+        hole |= at >= n;
+        pool_row = no + static_cast<unsigned>(max(min(at, n - 1), 0));
+      } else {
+        if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
+          hole = true;
+          no = 0;
+        }
+        const unsigned in_page = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+        pool_row = no * page_rows + in_page;
       }
-      const unsigned in_page = kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
-      const size_t row = static_cast<size_t>(no * page_rows + in_page) * (D * sizeof(T));
+      const size_t row = static_cast<size_t>(pool_row) * (D * sizeof(T));
       const unsigned to = stages_at + buf * S::kStage + (u * S::kWaves + wave) * 1024;
       load_1k(static_cast<const char *>(a.k_pages) + row + R::k_slot(r, lane % C) * 16, to);
       load_1k(static_cast<const char *>(a.v_pages) + row + R::v_slot(r, lane % C) * 16, to + S::kHalf);
@@ -314,20 +345,40 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   };
   // stage 0 before anything else is known of the block (last > first but for no entries at all), behind the first window of page
   // numbers: what the compiler waits for after a stage's loads would wait for them too
-  const int page_last = last > first ? page_of(a.pages, last - 1) : 0;
-  int window_at = page_of(a.pages, first);
+  const int page_last = last > first ? slot_of(last - 1) : 0;
   auto fill_window = [&]() __attribute__((always_inline)) {
-    int no[kWindow / S::kBlock];
+    int no[kWindow / S::kBlock], runs[kListed ? kWindow / S::kBlock : 1];
 #pragma unroll
     for (int i = 0; i < kWindow / S::kBlock; ++i) {
       const int pg = window_at + i * S::kBlock + static_cast<int>(threadIdx.x);
-      no[i] = pg <= page_last ? table[pg] : 0;
+      if constexpr (kListed) {
+        no[i] = runs[i] = 0;
+        if (pg <= page_last) no[i] = static_cast<int>(run_at(pg, runs[i]));
+      } else {
+        no[i] = pg <= page_last ? table[pg] : 0;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < kWindow / S::kBlock; ++i) window[i * S::kBlock + threadIdx.x] = no[i];
+    for (int i = 0; i < kWindow / S::kBlock; ++i) {
+      window[i * S::kBlock + threadIdx.x] = no[i];
+      if constexpr (kListed) window_seen[i * S::kBlock + threadIdx.x] = runs[i];
+    }
+  };
+  // (kListed) what the token sees of a stage's runs, for the masks: the window may have moved on by then
+  auto keep_runs = [&](int e0, int buf) __attribute__((always_inline)) {
+    if (static_cast<int>(threadIdx.x) < kKeys >> a.list.run_shift) {
+      const int x = (e0 >> a.list.run_shift) + static_cast<int>(threadIdx.x) - window_at;
+      stage_seen[buf][threadIdx.x] = x < kWindow ? window_seen[x] : 0;
+    }
   };
   bool hole_0 = false;
-  if (last > first) {
+  if (kListed && last > first) {
+    fill_window();
+    __syncthreads();
+    hole_0 = load_stage(first, last - 1, 0, [&](int pg, int) __attribute__((always_inline)) { return window[pg - window_at]; });
+    keep_runs(first, 0);
+  }
+  if (!kListed && last > first) {
     int page[S::kLoads];
 #pragma unroll
     for (int u = 0; u < S::kLoads; ++u) page[u] = table[page_of(a.pages, min(first + (u * S::kWaves + wave) * S::kPerLoad + lane / C, last - 1))];
@@ -370,13 +421,14 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
 
   auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
     const int e0 = first + st * kKeys;
-    if (page_of(a.pages, min(e0 + kKeys, end) - 1) >= window_at + kWindow) {   // (uniform)
-      window_at = page_of(a.pages, e0);
+    if (slot_of(min(e0 + kKeys, end) - 1) >= window_at + kWindow) {   // (uniform)
+      window_at = slot_of(e0);
       __syncthreads();
       fill_window();
       __syncthreads();
     }
     const bool hole = load_stage(e0, end - 1, buf, [&](int pg, int) __attribute__((always_inline)) { return window[pg - window_at]; });
+    if constexpr (kListed) keep_runs(e0, buf);
     if (hole) shared_hole[buf] = st + 1;           // (by the barrier before the stage is worked on)
   };
   // Waits for this wave's loads and for the other waves.
@@ -503,7 +555,17 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       unsigned there[kSub];                        // bit i: the entry is on a page
 #pragma unroll
       for (int x = 0; x < kSub; ++x) there[x] = 0xFFFFu;
-      if (holes) {
+      if (kListed && holes) {
+        const int shift = a.list.run_shift, in_stage = wk * (32 * kSub) + 4 * h;
+#pragma unroll
+        for (int x = 0; x < kSub; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = in_stage + 32 * x + 8 * (i / 4) + i % 4;
+            if ((key & ((1 << shift) - 1)) >= stage_seen[st & 1][key >> shift]) there[x] &= ~(1u << i);
+          }
+      }
+      if (!kListed && holes) {
 #pragma unroll
         for (int x = 0; x < kSub; ++x)
 #pragma unroll 1
@@ -603,7 +665,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     m = -FLT_MAX;
     l = 0.f;
     plain = fresh = true;
-    window_at = page_of(a.pages, first);
+    window_at = slot_of(first);
     fill_window();
     __syncthreads();
     fetch(0, 0);
@@ -666,10 +728,18 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   if (__builtin_expect(again, 0) && __builtin_amdgcn_readfirstlane(shared_odd) == 2) {
     // the infinities and NaN that were taken out and that a row sees (with a weight above zero, however small)
     for (int key = first + masked * kKeys; key < min(last, most); ++key) {
-      const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
-      if (static_cast<unsigned>(no) >= static_cast<unsigned>(a.pages.n_pages)) continue;
-      const T *v = static_cast<const T *>(a.v_pages) +
-                   static_cast<size_t>(no * page_rows + kvh * head_rows + static_cast<unsigned>(key - pg * a.pages.page_size)) * D + 4 * h;
+      unsigned pool_row;
+      if constexpr (kListed) {
+        int n = 0;
+        const int at = key & ((1 << a.list.run_shift) - 1);
+        pool_row = run_at(key >> a.list.run_shift, n) + static_cast<unsigned>(at);
+        if (at >= n) continue;
+      } else {
+        const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
+        if (static_cast<unsigned>(no) >= static_cast<unsigned>(a.pages.n_pages)) continue;
+        pool_row = no * page_rows + kvh * head_rows + static_cast<unsigned>(key - pg * a.pages.page_size);
+      }
+      const T *v = static_cast<const T *>(a.v_pages) + static_cast<size_t>(pool_row) * D + 4 * h;
 #pragma unroll
       for (int k = 0; k < kOwn; ++k)
 #pragma unroll
@@ -855,16 +925,16 @@ size_t bytes_of(const AttendArgs &a, const Plan &p) {
   return align_up(parts * 32 * a.head_dim * sizeof(float)) + align_up(parts * 64 * sizeof(float)) + align_up(tiles_of(a) * 32 * sizeof(float));
 }
 
-template <typename T, int D, int kWR, int kWK, int kKeys>
+template <typename T, int D, int kWR, int kWK, int kKeys, bool kListed = false>
 hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
   const long long M = static_cast<long long>(a.n_tokens) * a.group, spans = (M + 32 * kWR - 1) / (32 * kWR);
   if (spans > 65535) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(a.n_seqs * a.n_kv_heads), static_cast<unsigned>(a.n_split), static_cast<unsigned>(spans));
-  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys>), grid, dim3(64 * kWR * kWK), 0, stream, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kListed>), grid, dim3(64 * kWR * kWK), 0, stream, a);
   return hipGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kListed = false>
 hipError_t launch(AttendArgs a, hipStream_t stream) {
   constexpr bool kLong = D * sizeof(T) == 512;
   const Plan p = plan_of<T, D>(a);
@@ -882,7 +952,11 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
     a.part_lse = reinterpret_cast<float *>(w);
   }
   hipError_t e = hipErrorInvalidValue;
-  if constexpr (kLong) {
+  if constexpr (kListed) {                         // (rows of one token: up to 64)
+    if constexpr (kLong) e = launch_shape<T, D, 2, 2, 64, true>(a, stream);
+    else if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128, true>(a, stream);
+    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128, true>(a, stream);
+  } else if constexpr (kLong) {
     if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64>(a, stream);
     else if (p.wr == 4) e = launch_shape<T, D, 4, 1, 64>(a, stream);
   } else {
@@ -906,6 +980,19 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
 size_t attend_workspace(const AttendArgs &a) {
   if (a.dtype == LAZYEV_DTYPE_FP32) return a.head_dim == 64 ? bytes_of(a, plan_of<float, 64>(a)) : bytes_of(a, plan_of<float, 128>(a));
   return a.head_dim == 64 ? bytes_of(a, plan_of<bf16_t, 64>(a)) : bytes_of(a, plan_of<bf16_t, 128>(a));
+}
+
+size_t attend_list_workspace(const AttendArgs &a) { return attend_workspace(a); }
+
+hipError_t launch_attend_list(const AttendArgs &a, hipStream_t stream) {
+  if (a.n_tokens != 1 || a.group < 1 || a.group > 64 || a.list.tokens < 1 || a.list.run_shift > a.list.block_shift || a.list.run_shift > 6 ||
+      a.length != a.list.n_listed << a.list.block_shift)
+    return hipErrorInvalidValue;
+  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 64) return launch<float, 64, true>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 128) return launch<float, 128, true>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 64) return launch<bf16_t, 64, true>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 128) return launch<bf16_t, 128, true>(a, stream);
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream) {
