@@ -37,6 +37,40 @@ __device__ __forceinline__ float bf16_high(unsigned w) { return __uint_as_float(
 __device__ __forceinline__ float lower(float m, float x) { return x < m || x != x ? x : m; }
 __device__ __forceinline__ float upper(float m, float x) { return x > m || x != x ? x : m; }
 
+// x of the lanes whose numbers differ in the bits kFrom .. kTo (powers of two) joined; a step of 4 takes the steps of 1 and 2 to be done.
+template <int kStep>
+__device__ __forceinline__ unsigned from_lane(unsigned x) {
+  constexpr int kCtrl = kStep == 1 ? 0xB1 : kStep == 2 ? 0x4E : kStep == 4 ? 0x141 : 0x128;   // (quad_perm twice, row_half_mirror, row_ror by 8)
+  return static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, 0xF, 0xF, false));
+}
+template <int kStep, typename V, typename F>
+__device__ __forceinline__ V join_step(V x, F join) {
+  constexpr int kWords = sizeof(V) / 4;
+  unsigned w[kWords], a[kWords], b[kWords];
+  __builtin_memcpy(w, &x, sizeof(V));
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    if constexpr (kStep < 16) {
+      a[i] = w[i];
+      b[i] = from_lane<kStep>(w[i]);
+    } else {
+      const auto r = kStep == 16 ? __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false) : __builtin_amdgcn_permlane32_swap(w[i], w[i], false, false);
+      a[i] = r[0];
+      b[i] = r[1];
+    }
+  }
+  V y, z;
+  __builtin_memcpy(&y, a, sizeof(V));
+  __builtin_memcpy(&z, b, sizeof(V));
+  return join(y, z);
+}
+template <int kFrom, int kTo, typename V, typename F>
+__device__ __forceinline__ V join_lanes(V x, F join) {
+  x = join_step<kFrom>(x, join);
+  if constexpr (kFrom < kTo) x = join_lanes<2 * kFrom, kTo>(x, join);
+  return x;
+}
+
 // ------------------------------------------------------------------------------------ bounds
 
 template <typename T, int D>
@@ -92,12 +126,10 @@ __global__ __launch_bounds__(256) void bound_kernel(const BoundArgs a) {
     }
   }
 #pragma unroll
-  for (int o = C; o < 64; o <<= 1)
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-      lo[e] = lower(lo[e], __shfl_xor(lo[e], o));
-      hi[e] = upper(hi[e], __shfl_xor(hi[e], o));
-    }
+  for (int e = 0; e < kElems; ++e) {
+    lo[e] = join_lanes<C, 32>(lo[e], lower);
+    hi[e] = join_lanes<C, 32>(hi[e], upper);
+  }
   if (lane >= 2 * C) return;                       // (the first C lanes store the lower bounds, the next ones the upper)
   const bool up = lane >= C;
   u32x4_t w;
@@ -257,51 +289,45 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
   return x != x ? ~0ull : u ^ (static_cast<unsigned long long>(static_cast<long long>(u) >> 63) | 1ull << 63);
 }
 
-constexpr int kChooseBlock = 256, kChooseWaves = kChooseBlock / 64;
 constexpr int kAgain = 512;             // blocks between the borders whose exact scores LDS holds
 
-// The largest key that at least `want` of n keys key(i) reach, 1 <= want <= n, in steps of a bit; counts in LDS.  All threads call it.
-template <typename K, typename F>
-__device__ K kth_largest(int n, int want, int *counts /*[2][kChooseWaves]*/, F key) {
-  K t = 0;
-  int turn = 0;
-  for (int bit = static_cast<int>(sizeof(K)) * 8 - 1; bit >= 0; --bit, turn ^= 1) {
-    const K cand = t | static_cast<K>(1) << bit;
-    int have = 0;
-    for (int i0 = 0; i0 < n; i0 += kChooseBlock) {
-      const int i = i0 + static_cast<int>(threadIdx.x);
-      have += __popcll(__ballot(i < n && key(min(i, n - 1)) >= cand));
-    }
-    if ((threadIdx.x & 63) == 0) counts[turn * kChooseWaves + (threadIdx.x >> 6)] = have;
+// x of all waves, by `join`; LDS of one number a wave, of which two take turns.
+template <int kWaves, typename V, typename F>
+__device__ __forceinline__ V over_waves(V x, V (&room)[2][kWaves], int &turn, F join) {
+  if constexpr (kWaves > 1) {
+    if ((threadIdx.x & 63) == 0) room[turn][threadIdx.x >> 6] = x;
     __syncthreads();
-    int all = 0;
+    x = room[turn][0];
 #pragma unroll
-    for (int w = 0; w < kChooseWaves; ++w) all += counts[turn * kChooseWaves + w];
-    if (all >= want) t = cand;
-    if (all == want) break;                        // (exactly these)
+    for (int w = 1; w < kWaves; ++w) x = join(x, room[turn][w]);
+    turn ^= 1;
   }
-  __syncthreads();
-  return t;
+  return x;
 }
 
-// One block for a token and KV head.
-template <typename T, int D>
-__global__ __launch_bounds__(kChooseBlock) void choose_kernel(const ChooseArgs a) {
+// One block of kWaves waves for a token and KV head.  Its candidates' scores stay in registers, kRegs for a thread (candidate 64 (x kWaves + wave) + lane is x
+// of a lane); 0: there are more of them, and they are read anew for every look.
+// T is not needed to its last bit: an interval of T no wider than E does, so the bits of its order are settled from the first one in which candidates
+// differ to about the fourteenth behind, by counts of the candidates from a number on.
+template <typename T, int D, int kWaves, int kRegs>
+__global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a) {
   constexpr bool kF32 = sizeof(T) == 4;
-  __shared__ int counts[2 * kChooseWaves];
-  __shared__ float wave_f[2][kChooseWaves];
+  constexpr int kBlock = 64 * kWaves, C = D * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
+  constexpr int kLooks = kRegs * kWaves, kHeld = kRegs > 0 ? kRegs : 1;
+  __shared__ int room_i[2][kWaves];
+  __shared__ unsigned room_u[2][kWaves];
+  __shared__ float room_f[2][kWaves];
   __shared__ double exact[kAgain];
-  __shared__ int again[kAgain], n_shared[4];
+  __shared__ int again[kAgain], look_count[kLooks > 0 ? kLooks : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long row = blockIdx.x;                // (sequence, token of the launch, KV head)
-  const int kvh = static_cast<int>(row % a.n_kv_heads);
-  const int t = static_cast<int>(row / a.n_kv_heads % a.tokens), seq = static_cast<int>(row / a.n_kv_heads / a.tokens);
+  const unsigned row = blockIdx.x, its = row / a.n_kv_heads;          // (sequence, token of the launch, KV head)
+  const int kvh = static_cast<int>(row - its * a.n_kv_heads), seq = static_cast<int>(its / a.tokens), t = static_cast<int>(its - seq * a.tokens);
   const long long token = static_cast<long long>(seq) * a.n_tokens + a.token0 + t;
   int32_t *to = a.chosen + (token * a.n_kv_heads + kvh) * a.n_chosen;
   const int seen = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
   const int nb = (seen + a.block - 1) / a.block;
   if (nb <= a.n_chosen) {
-    for (int i = threadIdx.x; i < a.n_chosen; i += kChooseBlock) to[i] = i < nb ? i : -1;
+    for (int i = threadIdx.x; i < a.n_chosen; i += kBlock) to[i] = i < nb ? i : -1;
     return;
   }
   // candidates are the blocks first .. first + n - 1, of which `want` go
@@ -309,182 +335,284 @@ __global__ __launch_bounds__(kChooseBlock) void choose_kernel(const ChooseArgs a
   const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + kvh;
   const float *score = a.score + static_cast<size_t>(row) * a.scored + a.n_first, *peak = a.peak + unit * a.scored + a.n_first;
   const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + static_cast<long long>(kvh) * a.group) * D;
-  for (int i = threadIdx.x; i < a.n_first; i += kChooseBlock) to[i] = i;
-  for (int i = threadIdx.x; i < a.n_last; i += kChooseBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
+  for (int i = threadIdx.x; i < a.n_first; i += kBlock) to[i] = i;
+  for (int i = threadIdx.x; i < a.n_last; i += kBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
   if (want == 0) return;
 
-  // how far a score may be off
+  // the scores, their range, and how far one may be off
+  unsigned held[kHeld];
+  const int looks = kRegs > 0 ? kRegs : (n + kBlock - 1) / kBlock;
+  auto at_look = [&](int x) __attribute__((always_inline)) { return (x * kWaves + wave) * 64 + lane; };
+  auto each = [&](auto f) __attribute__((always_inline)) {   // f(candidate, its order or 0)
+    if constexpr (kRegs > 0) {
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) f(x, held[x]);
+    } else {
+      for (int x = 0; x < looks; ++x) f(x, at_look(x) < n ? order_of(score[min(at_look(x), n - 1)]) : 0u);
+    }
+  };
   float most = 0.f, size = 0.f;                    // largest bound; largest |q|_1
   bool odd = false;
-  for (int i = threadIdx.x; i < n; i += kChooseBlock) {
-    most = upper(most, peak[i]);
-    odd |= !(fabsf(score[i]) <= FLT_MAX);
-  }
-  for (int g = wave; g < a.group; g += kChooseWaves) {
-    float s = 0.f;
-    for (int e = lane; e < D; e += 64) {
-      float x;
-      if constexpr (kF32) x = q[g * D + e];
-      else x = __uint_as_float(static_cast<unsigned>(q[g * D + e]) << 16);
-      s += fabsf(x);
+  unsigned top = 0u, least = 0xFFFFFFFFu;
+  if constexpr (kRegs > 0) {
+    float s[kHeld], p[kHeld];
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) {
+      s[x] = p[x] = 0.f;
+      if (at_look(x) < n) {
+        s[x] = score[at_look(x)];
+        p[x] = peak[at_look(x)];
+      }
     }
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-    size = upper(size, s);
+    for (int x = 0; x < kRegs; ++x) {
+      const bool is = at_look(x) < n;
+      most = upper(most, p[x]);
+      odd |= !(fabsf(s[x]) <= FLT_MAX);
+      held[x] = is ? order_of(s[x]) : 0u;
+      top = max(top, held[x]);
+      least = min(least, is ? held[x] : 0xFFFFFFFFu);
+    }
+  } else {
+    for (int i = threadIdx.x; i < n; i += kBlock) {
+      const float s = score[i];
+      most = upper(most, peak[i]);
+      odd |= !(fabsf(s) <= FLT_MAX);
+      top = max(top, order_of(s));
+      least = min(least, order_of(s));
+    }
   }
+  for (int g0 = 0; g0 < a.group; g0 += kBlock / C) {
+    const int g = min(g0 + static_cast<int>(threadIdx.x) / C, a.group - 1);
+    const u32x4_t w = load_chunk(q + g * D + lane % C * kElems, a.wide);
+    float s = 0.f;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) most = upper(most, __shfl_xor(most, o));
-  if (lane == 0) {
-    wave_f[0][wave] = most;
-    wave_f[1][wave] = size;
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (kF32) s += fabsf(__uint_as_float(w[e]));
+      else s += fabsf(bf16_low(w[e])) + fabsf(bf16_high(w[e]));
+    }
+    size = upper(size, join_lanes<1, C / 2>(s, [](float x, float y) { return x + y; }));
   }
+  size = join_lanes<C, 32>(size, upper);
+  most = join_lanes<1, 32>(most, upper);
+  top = join_lanes<1, 32>(top, [](unsigned x, unsigned y) { return max(x, y); });
+  least = join_lanes<1, 32>(least, [](unsigned x, unsigned y) { return min(x, y); });
+  int turn_f = 0, turn_u = 0, turn_i = 0;
+  most = over_waves<kWaves>(most, room_f, turn_f, upper);
+  size = over_waves<kWaves>(size, room_f, turn_f, upper);
+  top = over_waves<kWaves>(top, room_u, turn_u, [](unsigned x, unsigned y) { return max(x, y); });
+  least = over_waves<kWaves>(least, room_u, turn_u, [](unsigned x, unsigned y) { return min(x, y); });
   odd = __syncthreads_or(odd);
-#pragma unroll
-  for (int w = 0; w < kChooseWaves; ++w) {
-    most = upper(most, wave_f[0][w]);
-    size = upper(size, wave_f[1][w]);
-  }
   // (2^-100: products too small for fp32; none of a row of zeros)
   const float off = size == 0.f && most <= FLT_MAX ? 0.f : size * most * 0x1p-14f + 0x1p-100f;
   const bool all_again = odd || !(size * most < 0x1p120f);
+  auto add = [](int x, int y) { return x + y; };
+  auto count_from = [&](unsigned cand) __attribute__((always_inline)) {
+    int have = 0;
+    each([&](int, unsigned k) __attribute__((always_inline)) { have += __popcll(__ballot(k >= cand)); });
+    return over_waves<kWaves>(have, room_i, turn_i, add);
+  };
 
   // the borders: surely taken from `sure` on, surely not below `out`
-  unsigned sure = 0xFFFFFFFFu, out = 0u;
+  unsigned sure = 0xFFFFFFFFu, out = 1u;
   if (!all_again) {
-    const unsigned kth = kth_largest<unsigned>(n, want, counts, [&](int i) { return order_of(score[i]); });
-    const float x = value_of(kth);
-    // (both borders are moved outwards by a step of their own rounding)
-    sure = order_of(x + 2.f * off) + (off > 0.f ? 1 : 0);
-    out = order_of(x - 2.f * off) - (off > 0.f ? 1 : 0);
-    if (!(off > 0.f)) sure += 1;                   // above T, surely; equal scores: by their numbers
+    // at least `want` are from `border` on, and fewer beyond border + span (or, found, just `want` from border on)
+    int bits = 32 - __clz(static_cast<int>(top ^ least));      // (__clz(0) = 32)
+    unsigned border = bits == 32 ? 0u : top >> bits << bits;
+    bool found = false;
+    while (bits > 0 && !found && !(value_of(border | (bits == 32 ? 0xFFFFFFFFu : (1u << bits) - 1)) - value_of(border) <= off)) {
+      --bits;
+      const unsigned cand = border | 1u << bits;
+      const int have = count_from(cand);
+      if (have >= want) border = cand;
+      found = have == want;
+    }
+    const float low = value_of(border), high = found ? low : value_of(border | ((1u << bits) - 1));
+    // (both are moved outwards by a step of their own rounding; no error at all: above T surely, and equal scores by their numbers)
+    sure = order_of(high + 2.f * off) + 1;
+    out = order_of(low - 2.f * off) - (off > 0.f ? 1 : 0);
   }
-  auto key = [&](int i) __attribute__((always_inline)) { return all_again ? 1u : order_of(score[i]); };
-  // their numbers, and the list of those between
-  if (threadIdx.x < 4) n_shared[threadIdx.x] = 0;
-  __syncthreads();
+  auto is_sure = [&](unsigned k) __attribute__((always_inline)) { return !all_again && k >= sure; };
+  auto between = [&](unsigned k) __attribute__((always_inline)) { return k != 0u && (all_again || (k < sure && k >= out)); };
   int n_sure = 0, n_between = 0;
-  for (int i0 = 0; i0 < n; i0 += kChooseBlock) {
-    const int i = i0 + static_cast<int>(threadIdx.x);
-    const unsigned k = i < n ? key(i) : 0u;
-    n_sure += __popcll(__ballot(i < n && !all_again && k >= sure));
-    n_between += __popcll(__ballot(i < n && (all_again || (k < sure && k >= out))));
-  }
-  if (lane == 0) {
-    atomicAdd(&n_shared[0], n_sure);
-    atomicAdd(&n_shared[1], n_between);
-  }
-  __syncthreads();
-  n_sure = n_shared[0];
-  n_between = n_shared[1];
-  const int rest = want - n_sure;                  // to take of those between, 1 .. n_between
-  auto between = [&](unsigned k) __attribute__((always_inline)) { return all_again || (k < sure && k >= out); };
+  each([&](int, unsigned k) __attribute__((always_inline)) {
+    n_sure += __popcll(__ballot(is_sure(k)));
+    n_between += __popcll(__ballot(between(k)));
+  });
+  n_sure = over_waves<kWaves>(n_sure, room_i, turn_i, add);
+  n_between = over_waves<kWaves>(n_between, room_i, turn_i, add);
+  const int rest = want - n_sure;                  // to take of those between, 0 .. n_between
+  const bool ask = (off > 0.f || all_again) && rest > 0 && rest < n_between;
 
   // exact score of a block, for all lanes: a lane has D / 8 elements of one of eight heads
   auto exact_score = [&](int i) __attribute__((always_inline)) {
-    constexpr int kPart = D / 8;
+    constexpr int kPart = D / 8, kLoads = kPart / kElems;
     const T *bounds = static_cast<const T *>(a.bounds) + (unit * a.n_blocks + a.n_first + i) * (2 * D) + lane % 8 * kPart;
+    u32x4_t lo[kLoads], hi[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      lo[j] = *reinterpret_cast<const u32x4_t *>(bounds + j * kElems);
+      hi[j] = *reinterpret_cast<const u32x4_t *>(bounds + D + j * kElems);
+    }
     double best = -INFINITY;
     for (int g0 = 0; g0 < a.group; g0 += 8) {
       const T *mine = q + min(g0 + lane / 8, a.group - 1) * D + lane % 8 * kPart;
       double s = 0.0;
-#pragma unroll 4
-      for (int e = 0; e < kPart; ++e) {
-        double x, l, u;
-        if constexpr (kF32) {
-          x = mine[e]; l = bounds[e]; u = bounds[D + e];
-        } else {
-          x = __uint_as_float(static_cast<unsigned>(mine[e]) << 16);
-          l = __uint_as_float(static_cast<unsigned>(bounds[e]) << 16);
-          u = __uint_as_float(static_cast<unsigned>(bounds[D + e]) << 16);
-        }
-        const double y = x > 0.0 ? x * u : x * l;  // (a NaN is a NaN)
-        s += x == 0.0 ? 0.0 : y;
-      }
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
+      for (int j = 0; j < kLoads; ++j) {
+        const u32x4_t w = load_chunk(mine + j * kElems, a.wide);
+#pragma unroll
+        for (int e = 0; e < kElems; ++e) {
+          auto of = [&](u32x4_t v) __attribute__((always_inline)) -> double {
+            if constexpr (kF32) return __uint_as_float(v[e]);
+            else return e % 2 ? bf16_high(v[e / 2]) : bf16_low(v[e / 2]);
+          };
+          const double x = of(w), y = x > 0.0 ? x * of(hi[j]) : x * of(lo[j]);   // (a NaN is a NaN)
+          s += x == 0.0 ? 0.0 : y;
+        }
+      }
+      s = join_lanes<1, 4>(s, [](double x, double y) { return x + y; });
       s = s != s ? INFINITY : s;
       best = s > best ? s : best;
     }
-#pragma unroll
-    for (int o = 8; o < 64; o <<= 1) {
-      const double x = __shfl_xor(best, o);
-      best = x > best ? x : best;
-    }
-    return best;
+    return join_lanes<8, 32>(best, [](double x, double y) { return x > y ? x : y; });
   };
 
-  unsigned long long border = 0;                   // of the exact scores of those between: taken above it, and `equal` of those at it
-  int equal = INT_MAX;
-  const bool few = n_between <= kAgain;
-  unsigned long long *wide = a.exact ? a.exact + static_cast<size_t>(row) * a.scored : nullptr;
-  const bool ask = off > 0.f || all_again;         // (without: rounded scores are the exact ones)
-  if (!ask) {
-    equal = rest;
-  } else if (rest == 0) {
-    border = ~0ull;
-    equal = 0;
-  } else if (rest < n_between) {
-    if (few) {                                     // the list, in the order of the blocks
-      if (wave == 0) {
-        int at = 0;
-        for (int i0 = 0; i0 < n; i0 += 64) {
-          const bool mine = i0 + lane < n && between(key(min(i0 + lane, n - 1)));
-          const unsigned long long m = __ballot(mine);
-          if (mine) again[at + __popcll(m & ((1ull << lane) - 1))] = i0 + lane;
-          at += __popcll(m);
+  if (kRegs == 0 || (ask && n_between > kAgain)) {
+    // many: numbers of 64 bits in memory, those surely taken the largest, and the list by one wave
+    unsigned long long *all = a.exact + static_cast<size_t>(row) * a.scored;
+    for (int x = 0; x < looks; ++x) {
+      const int i0 = (x * kWaves + wave) * 64, i = i0 + lane;
+      unsigned k = i < n ? order_of(score[min(i, n - 1)]) : 0u;
+      const unsigned long long mid = __ballot(between(k));
+      unsigned long long mine = is_sure(k) ? ~0ull : between(k) ? 1ull : 0ull;
+      if (ask)
+        for (unsigned long long m = mid; m; m &= m - 1) {
+          const int b = __builtin_ctzll(m);
+          const unsigned long long e = order_of(exact_score(i0 + b));
+          mine = lane == b ? e : mine;
         }
-      }
-      __syncthreads();
-      for (int x = wave; x < n_between; x += kChooseWaves) {
-        const double s = exact_score(again[x]);
-        if (lane == 0) exact[x] = s;
-      }
-      __syncthreads();
-      border = kth_largest<unsigned long long>(n_between, rest, counts, [&](int i) { return order_of(exact[i]); });
-    } else {
-      for (int i = wave; i < n; i += kChooseWaves) {
-        unsigned long long k = 0;
-        if (between(key(i))) k = order_of(exact_score(i));
-        if (lane == 0) wide[i] = k;
-      }
-      __syncthreads();
-      border = kth_largest<unsigned long long>(n, rest, counts, [&](int i) { return wide[i]; });
+      if (i < n) all[i] = mine;
+    }
+    __syncthreads();
+    unsigned long long border = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const unsigned long long cand = border | 1ull << bit;
+      int have = 0;
+      for (int i0 = wave * 64; i0 < n; i0 += kBlock) have += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] >= cand));
+      have = over_waves<kWaves>(have, room_i, turn_i, add);
+      if (have >= want) border = cand;
+      if (have == want) break;
     }
     int above = 0;
-    for (int i0 = 0; i0 < (few ? n_between : n); i0 += kChooseBlock) {
-      const int i = i0 + static_cast<int>(threadIdx.x);
-      above += __popcll(__ballot(i < (few ? n_between : n) && (few ? order_of(exact[min(i, n_between - 1)]) : wide[min(i, n - 1)]) > border));
+    for (int i0 = wave * 64; i0 < n; i0 += kBlock) above += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] > border));
+    above = over_waves<kWaves>(above, room_i, turn_i, add);
+    if (wave != 0) return;
+    int at = a.n_first, met = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      const unsigned long long k = i0 + lane < n ? all[i0 + lane] : 0ull, below = (1ull << lane) - 1;
+      const unsigned long long same = __ballot(i0 + lane < n && k == border);
+      const bool take = i0 + lane < n && (k > border || (k == border && met + __popcll(same & below) < want - above));
+      const unsigned long long m = __ballot(take);
+      if (take) to[at + __popcll(m & below)] = a.n_first + i0 + lane;
+      at += __popcll(m);
+      met += __popcll(same);
     }
-    if (lane == 0) atomicAdd(&n_shared[2], above);
-    __syncthreads();
-    equal = rest - n_shared[2];
+    return;
   }
-  // the list, by one wave
-  if (wave != 0) return;
-  int at = a.n_first, met = 0, seen_between = 0;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    const int i = i0 + lane;
-    const unsigned k = i < n ? key(i) : 0u;
-    bool take = i < n && !all_again && k >= sure;
-    const bool mid = i < n && between(k) && !take;
-    const unsigned long long m_mid = __ballot(mid), below = (1ull << lane) - 1;
-    bool same = false;
-    if (mid) {
-      if (!ask) same = true;
-      else if (rest >= n_between) take = true;
-      else {
-        const unsigned long long x = few ? order_of(exact[seen_between + __popcll(m_mid & below)]) : wide[i];
-        take = x > border;
-        same = x == border;
+  if constexpr (kRegs > 0) {
+    // numbers before a look of candidates with something: counts of all looks in LDS, added up by every wave
+    const unsigned long long below = (1ull << lane) - 1;
+    auto before_look = [&](const int (&mine)[kHeld], int (&before)[kHeld]) __attribute__((always_inline)) {
+      if constexpr (kWaves == 1) {
+        int sum = 0;
+#pragma unroll
+        for (int x = 0; x < kRegs; ++x) {
+          before[x] = sum;
+          sum += mine[x];
+        }
+      } else {
+        constexpr int kPer = (kLooks + 63) / 64;
+        __syncthreads();
+        if (lane == 0)
+#pragma unroll
+          for (int x = 0; x < kRegs; ++x) look_count[x * kWaves + wave] = mine[x];
+        __syncthreads();
+        int part[kPer], sum = 0;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) {
+          part[y] = sum;
+          sum += lane * kPer + y < kLooks ? look_count[lane * kPer + y] : 0;
+        }
+        int run = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int y = __shfl_up(run, o);
+          run += lane >= o ? y : 0;
+        }
+        run -= sum;
+#pragma unroll
+        for (int x = 0; x < kRegs; ++x) {
+          const int look = x * kWaves + wave;
+          int got = 0;
+#pragma unroll
+          for (int y = 0; y < kPer; ++y) {
+            const int z = __shfl(run + part[y], look / kPer);
+            got = look % kPer == y ? z : got;
+          }
+          before[x] = got;
+        }
       }
+    };
+    int mine[kHeld], before[kHeld];
+    unsigned taken = 0;                            // bit x: candidate x of this lane goes
+    if (rest > 0 && rest < n_between) {            // some of those between
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) mine[x] = __popcll(__ballot(between(held[x])));
+      before_look(mine, before);
+      if (!ask) {                                  // (equal, as exact as they are: the lowest)
+#pragma unroll
+        for (int x = 0; x < kRegs; ++x) {
+          const unsigned long long m = __ballot(between(held[x]));
+          if (between(held[x]) && before[x] + __popcll(m & below) < rest) taken |= 1u << x;
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < kRegs; ++x) {
+          const unsigned long long m = __ballot(between(held[x]));
+          if (between(held[x])) again[before[x] + __popcll(m & below)] = at_look(x);
+        }
+        __syncthreads();
+        for (int x = wave; x < n_between; x += kWaves) {
+          const double s = exact_score(again[x]);
+          if (lane == 0) exact[x] = s;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < kRegs; ++x) {
+          const unsigned long long m = __ballot(between(held[x]));
+          if (!between(held[x])) continue;
+          const int me = before[x] + __popcll(m & below);
+          const double s = exact[me];
+          int ahead = 0;
+          for (int y = 0; y < n_between; ++y) ahead += exact[y] > s || (exact[y] == s && y < me) ? 1 : 0;
+          if (ahead < rest) taken |= 1u << x;
+        }
+      }
+    } else if (rest > 0) {                         // all of them
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) taken |= between(held[x]) ? 1u << x : 0u;
     }
-    const unsigned long long m_same = __ballot(same);
-    if (same && met + __popcll(m_same & below) < equal) take = true;
-    const unsigned long long m = __ballot(take);
-    if (take) to[at + __popcll(m & below)] = a.n_first + i;
-    at += __popcll(m);
-    met += __popcll(m_same);
-    seen_between += __popcll(m_mid);
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) taken |= is_sure(held[x]) ? 1u << x : 0u;
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) mine[x] = __popcll(__ballot(taken >> x & 1u));
+    before_look(mine, before);
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) {
+      const unsigned long long m = __ballot(taken >> x & 1u);
+      if (taken >> x & 1u) to[a.n_first + before[x] + __popcll(m & below)] = a.n_first + at_look(x);
+    }
   }
 }
 
@@ -543,7 +671,12 @@ hipError_t launch(ChooseArgs a, hipStream_t stream) {
     }
     const long long blocks = static_cast<long long>(a.n_seqs) * a.tokens * a.n_kv_heads;
     if (blocks > (1ll << 23)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((choose_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kChooseBlock), 0, stream, a);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (a.scored <= 4 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 4>), grid, dim3(64), 0, stream, a);
+    else if (a.scored <= 16 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 16>), grid, dim3(64), 0, stream, a);
+    else if (a.scored <= 16 * 256) hipLaunchKernelGGL((choose_kernel<T, D, 4, 16>), grid, dim3(256), 0, stream, a);
+    else if (a.scored <= 16 * 1024) hipLaunchKernelGGL((choose_kernel<T, D, 16, 16>), grid, dim3(1024), 0, stream, a);
+    else hipLaunchKernelGGL((choose_kernel<T, D, 16, 0>), grid, dim3(1024), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
