@@ -181,7 +181,7 @@ int lazyev_pages_weigh(const lazyev_pages *pages, int32_t length, int32_t n_toke
   a.known = known; a.decay = decay;
   a.scale = scale_of(scale, pages->head_dim);
   a.visible = visible; a.q = q; a.lse = lse; a.old = old; a.weights = weights; a.stride = stride;
-  a.part = static_cast<float *>(workspace);
+  a.workspace = workspace;
   return done(lazyev::launch_weigh(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -324,8 +324,14 @@ struct WeighArgs {
   PageTable pages;
   float *weights;
   int64_t stride;                   // of old and weights, from unit to unit
-  float *part;                      // workspace: [n_split][units][length]
-  int32_t n_split, wide;            // filled in by the launch
+  void *workspace;
+  // filled in by the launch: blocks of a unit, stages of its rows, splits of them, rows at multiples of 16 bytes; and in the workspace what
+  // is known of rows and stages, and the sums [n_split][units][length]
+  int32_t across, stages, n_split, wide;
+  float *row_lse;
+  int32_t *row_sees;
+  int2 *stage_sees;
+  float *part;
 };
 size_t weigh_workspace(const WeighArgs &a);
 hipError_t launch_weigh(WeighArgs a, hipStream_t stream);

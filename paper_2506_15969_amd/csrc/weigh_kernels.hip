@@ -1,13 +1,16 @@
 // The attention weight that every entry of a cache received (lazyev_pages_weigh): w[i] = (old) + sum over the rows r that see entry i of
 // exp(scale q_r k_i - lse_r), rows being the tokens' heads of the entry's group.
 //
-// A wave keeps 32 entries' keys as the B operand of 32 x 32 products (32x32x16_bf16; fp32 rows: 32x32x2_f32) and goes over the rows, 32 at a time as A:
-// lane (c, h) = (l % 32, l / 32) holds, of entry c, the logits of the rows 8 i + 4 h + j (i, j < 4), so the sum over rows
-// is one in its register.  Rows that do not see all of the entries are masked, by the number of entries that they see; those past the last, and those
-// that saw nothing (lse of -inf), see none.
-//
-// Few entries: the rows are cut into splits too, every n-th tile of 32 to each (where tokens see their past, late rows are seen by
-// all entries, early ones by few), whose sums a second kernel adds in their order.
+// Both kernels have keys as the B operand of 32 x 32 products (32x32x16_bf16; fp32 rows: 32x32x2_f32) and rows as A: lane (c, h) = (l % 32, l / 32)
+// holds, of entry c, the logits of the rows 8 i + 4 h + j (i, j < 4), so the sum over rows is one in its register.  Rows
+// that do not see all of the entries are masked, by the number of entries that they see; those past the last, and those that saw nothing (lse of
+// -inf), see none.
+//   few   rows that fit one operand (a decode step): a wave keeps them and goes over tiles of 32 entries, one on its way while another is worked on
+//   many  the waves of a block keep 32 kSubs entries each and go over stages of 64 rows, fetched straight into LDS while the stage before
+//         is worked on.  A small kernel before it leaves, for every row, lse in units of log 2 and what it sees, and for every
+//         stage the least and the most that a row of it sees: a block goes over the stages that see some of its entries alone.
+// Few entries of many rows: the stages are also dealt out to splits in turn (where tokens see their past, late rows are seen by all entries,
+// early ones by few), whose sums a last kernel adds in their order.
 #include "kernels.h"
 #include "lazyev.h"
 
@@ -20,11 +23,23 @@ typedef unsigned short bf16_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kEntries = 128;           // of a block
+constexpr int kStageRows = 64;
 constexpr int kSplitMax = 64;
+
+template <typename T, int D>
+struct Rows {
+  static constexpr bool kF32 = sizeof(T) == 4;
+  static constexpr int kChunks = D * static_cast<int>(sizeof(T)) / 16;   // 16-byte chunks of a row
+  static constexpr int kOps = kChunks / 2;         // chunks of a row that a lane holds as an operand
+  static constexpr int kSubs = kF32 ? 1 : 2;       // (many) tiles of 32 entries that a wave keeps
+  static constexpr int kEntries = 4 * 32 * kSubs;  // of a block
+  // where chunk x of row r of a stage lies among the row's chunks: operands are read by 16 rows at a time, one chunk of each
+  __device__ static int slot(int r, int x) { return x ^ (kChunks == 8 ? (r >> 1) & 7 : r & 15); }
+};
 
 template <typename T>
 __device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
@@ -37,97 +52,295 @@ __device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
   return w;
 }
 
+// x / y for 0 <= x < 2^24, y > 0 (the rounded quotient is off by one at most).
+__device__ __forceinline__ int quotient(int x, int y) {
+  int q = static_cast<int>(static_cast<float>(x) * __builtin_amdgcn_rcpf(static_cast<float>(y)));
+  const int r = x - q * y;
+  q += r >= y ? 1 : 0;
+  return q - (r < 0 ? 1 : 0);
+}
+// The row r of a unit among all rows of q; its token.
+__device__ __forceinline__ long long row_of(const WeighArgs &a, int seq, int kvh, int r, long long &token) {
+  const int i = quotient(r, a.group);
+  token = static_cast<long long>(seq) * a.n_tokens + i;
+  return token * a.n_q_heads + static_cast<long long>(kvh) * a.group + (r - i * a.group);
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void logits(const u32x4_t (&q)[Rows<T, D>::kOps], const u32x4_t (&k)[Rows<T, D>::kOps], f32x16_t &s) {
+#pragma unroll
+  for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+  for (int j = 0; j < Rows<T, D>::kOps; ++j) {
+    if constexpr (Rows<T, D>::kF32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[j][e]), __uint_as_float(k[j][e]), s, 0, 0, 0);
+    } else {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, q[j]), __builtin_bit_cast(bf16x8_t, k[j]), s, 0, 0, 0);
+    }
+  }
+}
+
 // What an entry had before.
 __device__ __forceinline__ float before(const WeighArgs &a, long long at, int entry) { return entry < a.known ? a.decay * a.old[at] : 0.f; }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void weigh_kernel(const WeighArgs a) {
-  constexpr bool kF32 = sizeof(T) == 4;
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32;
-  __shared__ __align__(16) float row_lse[4][32];
-  __shared__ __align__(16) int row_sees[4][32];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = lane & 31, h = lane >> 5;
-  const int across = (a.length + kEntries - 1) / kEntries;
-  const int unit = static_cast<int>(blockIdx.x / across), split = static_cast<int>(blockIdx.y);
-  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
-  const int e0 = (static_cast<int>(blockIdx.x) - unit * across) * kEntries + wave * 32;
-  if (e0 >= a.length) return;
-  const int entry = min(e0 + c, a.length - 1), end = min(e0 + 32, a.length);
+// Where the keys of an entry lie (any: some entry's).
+__device__ __forceinline__ size_t key_row(const WeighArgs &a, int seq, int kvh, int entry, bool &there) {
   const int pg = page_of(a.pages, entry);
   const unsigned no = static_cast<unsigned>(a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg]);
-  const bool there = no < static_cast<unsigned>(a.pages.n_pages);
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
-  const unsigned k_row = (there ? no : 0u) * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
-  u32x4_t k[kOps];
+  there = no < static_cast<unsigned>(a.pages.n_pages);
+  return (there ? no : 0u) * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+}
+
+// ------------------------------------------------------------------------------------ few rows
+
+// Blocks of 256: wave w of block x of a unit has the tiles of 32 entries 4 x + w, and every 4 a.across further.  kEights: groups of eight rows.
+template <typename T, int D, int kEights>
+__global__ __launch_bounds__(256) void weigh_few_kernel(const WeighArgs a) {
+  using R = Rows<T, D>;
+  constexpr int kOps = R::kOps;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = lane & 31, h = lane >> 5;
+  const int unit = static_cast<int>(blockIdx.x) / a.across, x0 = static_cast<int>(blockIdx.x) - unit * a.across;
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  const int M = a.n_tokens * a.group, tiles = (a.length + 31) / 32, step = 4 * a.across;
+  int tile = 4 * x0 + wave;
+  if (tile >= tiles) return;
+  bool there[2];
+  u32x4_t k[2][kOps];
+  auto fetch = [&](int tl, int buf) __attribute__((always_inline)) {
+    const char *from = static_cast<const char *>(a.k_pages) + key_row(a, seq, kvh, min(tl * 32 + c, a.length - 1), there[buf]) * (D * sizeof(T)) + h * 16;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) k[buf][j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+  };
+  fetch(tile, 0);
+  u32x4_t q[kOps];
+  long long token;
   {
-    const char *from = static_cast<const char *>(a.k_pages) + static_cast<size_t>(k_row) * (D * sizeof(T)) + h * 16;
+    const T *from = static_cast<const T *>(a.q) + row_of(a, seq, kvh, min(c, M - 1), token) * D + h * (16 / sizeof(T));
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) k[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+    for (int j = 0; j < kOps; ++j) q[j] = load_chunk(from + j * (32 / sizeof(T)), a.wide);
   }
-  const int M = a.n_tokens * a.group, tiles = (M + 31) / 32;
-  const float c2 = a.scale * kLog2e;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int tile = split; tile < tiles; tile += a.n_split) {
-    const int r = tile * 32 + c, rr = min(r, M - 1), i = rr / a.group;
-    const long long token = static_cast<long long>(seq) * a.n_tokens + i;
-    const long long row = token * a.n_q_heads + static_cast<long long>(kvh) * a.group + (rr - i * a.group);
+  float ref[4 * kEights];
+  int sees[4 * kEights];
+  int least = INT_MAX;
+#pragma unroll
+  for (int x = 0; x < 4 * kEights; ++x) {
+    const int r = 8 * (x / 4) + 4 * h + x % 4;
+    const long long row = row_of(a, seq, kvh, min(r, M - 1), token);
     const float lse = a.lse[row];
-    int sees = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
-    if (r >= M || lse == -INFINITY) sees = 0;
-    int most = sees, least = sees;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      most = max(most, __shfl_xor(most, o));
-      least = min(least, __shfl_xor(least, o));
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
-    least = __builtin_amdgcn_readfirstlane(least);
-    if (most <= e0) continue;                      // (wave-uniform) nobody sees them
-    if (h == 0) {
-      row_lse[wave][c] = lse * kLog2e;
-      row_sees[wave][c] = sees;
-    }
-    const T *q = static_cast<const T *>(a.q) + row * D + h * (16 / sizeof(T));
+    sees[x] = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
+    if (r >= M || lse == -INFINITY) sees[x] = 0;
+    ref[x] = sees[x] > 0 ? lse * kLog2e : 0.f;
+    least = min(least, sees[x]);
+  }
+  const float c2 = a.scale * kLog2e;
+  auto work = [&](int tl, int buf) __attribute__((always_inline)) {
     f32x16_t s;
+    logits<T, D>(q, k[buf], s);
+    const int entry = tl * 32 + c;
+    float w = 0.f;
+    if (__builtin_amdgcn_ballot_w64(least < tl * 32 + 32) == 0) {       // (wave-uniform)
 #pragma unroll
-    for (int x = 0; x < 16; ++x) s[x] = 0.f;
+      for (int x = 0; x < 4 * kEights; ++x) w += __builtin_amdgcn_exp2f(fmaf(s[x], c2, -ref[x]));
+    } else {
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) {
-      const u32x4_t w = load_chunk(q + j * (32 / sizeof(T)), a.wide);
-      if constexpr (kF32) {
+      for (int x = 0; x < 4 * kEights; ++x) w += entry < sees[x] ? __builtin_amdgcn_exp2f(fmaf(s[x], c2, -ref[x])) : 0.f;
+    }
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+    w = there[buf] ? __uint_as_float(both[0]) + __uint_as_float(both[1]) : 0.f;
+    if (h == 0 && entry < a.length) {
+      const long long at = static_cast<long long>(unit) * a.stride + entry;
+      a.weights[at] = before(a, at, entry) + w;
+    }
+  };
+  while (true) {
+    if (tile + step < tiles) fetch(tile + step, 1);
+    work(tile, 0);
+    tile += step;
+    if (tile >= tiles) break;
+    if (tile + step < tiles) fetch(tile + step, 0);
+    work(tile, 1);
+    tile += step;
+    if (tile >= tiles) break;
+  }
+}
+
+// ------------------------------------------------------------------------------------ many rows
+
+// Rows [units][stages][64]: lse in units of log 2, entries that the row sees; of a stage the least and the most that one sees.
+__global__ __launch_bounds__(256) void weigh_rows_kernel(const WeighArgs a) {
+  const int M = a.n_tokens * a.group;
+  const long long at = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, stage = at / kStageRows;
+  const int unit = static_cast<int>(stage / a.stages);
+  if (unit >= a.n_seqs * a.n_kv_heads) return;
+  const int r = static_cast<int>(at - static_cast<long long>(unit) * a.stages * kStageRows);
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  long long token;
+  const long long row = row_of(a, seq, kvh, min(r, M - 1), token);
+  const float lse = a.lse[row];
+  int sees = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
+  if (r >= M || lse == -INFINITY) sees = 0;
+  a.row_lse[at] = sees > 0 ? lse * kLog2e : 0.f;
+  a.row_sees[at] = sees;
+  int least = sees, most = sees;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[e]), __uint_as_float(k[j][e]), s, 0, 0, 0);
+  for (int o = 1; o < 64; o <<= 1) {
+    least = min(least, __shfl_xor(least, o));
+    most = max(most, __shfl_xor(most, o));
+  }
+  if ((threadIdx.x & 63) == 0) a.stage_sees[stage] = make_int2(least, most);
+}
+
+constexpr int kList = 1024;             // stages of a block's turn
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void weigh_many_kernel(const WeighArgs a) {
+  using R = Rows<T, D>;
+  constexpr int kOps = R::kOps, C = R::kChunks, kSubs = R::kSubs;
+  constexpr int kStage = kStageRows * C * 16;      // bytes
+  constexpr int kPerLoad = 64 / C, kLoads = kStageRows / (kPerLoad * 4);   // rows of a wave's load of 1 KB, loads of a wave
+  __shared__ __align__(16) char stages[2 * kStage];
+  __shared__ __align__(16) float row_lse[2][kStageRows];
+  __shared__ __align__(16) int row_sees[2][kStageRows];
+  __shared__ int list[kList], list_least[kList], list_most[kList], counts[4][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, h = lane >> 5;
+  // early entries first: where tokens see their past, they have the most rows.  Units next: those of eight units share an XCD and its L2
+  const int units = a.n_seqs * a.n_kv_heads, x0 = static_cast<int>(blockIdx.x / units), unit = static_cast<int>(blockIdx.x) - x0 * units;
+  const int split = x0 % a.n_split, seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  const int block_e0 = x0 / a.n_split * R::kEntries, e0 = block_e0 + wave * 32 * kSubs;
+  const int M = a.n_tokens * a.group;
+  bool there[kSubs];
+  u32x4_t k[kSubs][kOps];
+#pragma unroll
+  for (int x = 0; x < kSubs; ++x) {
+    const char *from = static_cast<const char *>(a.k_pages) + key_row(a, seq, kvh, min(e0 + 32 * x + c, a.length - 1), there[x]) * (D * sizeof(T)) + h * 16;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) k[x][j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+  }
+  const unsigned stages_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)stages));
+  const unsigned lse_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)row_lse));
+  const unsigned sees_at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)row_sees));
+  // A stage's rows and what is known of them to LDS, straight from memory where the rows lie at multiples of 16 bytes.  (Written out, as the compiler
+  // has every read of LDS wait for all loads into it: they leave nothing in registers, and the waits for them are in `arrived`.)
+  const float *lse_from = a.row_lse + static_cast<size_t>(unit) * a.stages * kStageRows;
+  const int *sees_from = a.row_sees + static_cast<size_t>(unit) * a.stages * kStageRows;
+  auto fetch = [&](int stage, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int r = (u * 4 + wave) * kPerLoad + lane / C;
+      long long token;
+      const T *row = static_cast<const T *>(a.q) + row_of(a, seq, kvh, min(stage * kStageRows + r, M - 1), token) * D + R::slot(r, lane % C) * (16 / sizeof(T));
+      const unsigned at = buf * kStage + (u * 4 + wave) * 1024;
+      if (a.wide) {
+        __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(stages_at + at), "v"(row) : "memory", "m0");
       } else {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, k[j]), s, 0, 0, 0);
+        *reinterpret_cast<u32x4_t *>(stages + at + lane * 16) = load_chunk(row, false);
       }
     }
-    __builtin_amdgcn_wave_barrier();
-    const bool mask = least < end;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const f32x4_t ref = *reinterpret_cast<const f32x4_t *>(&row_lse[wave][8 * x + 4 * h]);
-      const int *limit = &row_sees[wave][8 * x + 4 * h];
-      float p[4];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        p[y] = __builtin_amdgcn_exp2f(fmaf(s[4 * x + y], c2, -ref[y]));
-        if (mask) p[y] = e0 + c < limit[y] ? p[y] : 0.f;
-      }
-      sum[x] += (p[0] + p[1]) + (p[2] + p[3]);
+    if (wave < 2) {
+      const void *from = wave == 0 ? static_cast<const void *>(lse_from + stage * kStageRows + lane) : sees_from + stage * kStageRows + lane;
+      const unsigned at = (wave == 0 ? lse_at : sees_at) + buf * (kStageRows * 4);
+      __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from) : "memory", "m0");
     }
-    __builtin_amdgcn_wave_barrier();
+  };
+  auto arrived = [&]() __attribute__((always_inline)) {
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4);            // vmcnt(0), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __asm__ volatile("" ::: "memory");
+  };
+  const float c2 = a.scale * kLog2e;
+  float sum[kSubs][2];
+#pragma unroll
+  for (int x = 0; x < kSubs; ++x) sum[x][0] = sum[x][1] = 0.f;
+  int q_at[kOps];
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) q_at[j] = (c * C + R::slot(c, 2 * j + h)) * 16;
+  auto work = [&](int buf, bool mask) __attribute__((always_inline)) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      u32x4_t q[kOps];
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) q[j] = *reinterpret_cast<const u32x4_t *>(stages + buf * kStage + half * 32 * C * 16 + q_at[j]);
+      f32x4_t ref[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) ref[x] = *reinterpret_cast<const f32x4_t *>(&row_lse[buf][half * 32 + 8 * x + 4 * h]);
+#pragma unroll
+      for (int x = 0; x < kSubs; ++x) {
+        f32x16_t s;
+        logits<T, D>(q, k[x], s);
+        if (mask) {
+          const int entry = e0 + 32 * x + c;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const i32x4_t limit = *reinterpret_cast<const i32x4_t *>(&row_sees[buf][half * 32 + 8 * y + 4 * h]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) s[4 * y + z] = entry < limit[z] ? s[4 * y + z] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 16; ++y) sum[x][y & 1] += __builtin_amdgcn_exp2f(fmaf(s[y], c2, -ref[y / 4][y % 4]));
+      }
+    }
+  };
+  const int mine = split < a.stages ? (a.stages - split + a.n_split - 1) / a.n_split : 0;   // stages of this split
+  const int2 *stage_sees = a.stage_sees + static_cast<size_t>(unit) * a.stages;
+#pragma unroll 1
+  for (int w0 = 0; w0 < mine; w0 += kList) {
+    // those of the next kList that see some of the block's entries, in their order
+    int at = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int x = 0; x < kList && w0 + x < mine; x += 256) {
+      const int i = w0 + x + static_cast<int>(threadIdx.x), stage = split + i * a.n_split;
+      const int2 s = i < mine ? stage_sees[stage] : make_int2(0, 0);
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(s.y > block_e0);
+      if (lane == 0) counts[x / 256][wave] = __popcll(m);
+      __syncthreads();
+      int before_wave = at;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        before_wave += w < wave ? counts[x / 256][w] : 0;
+        at += counts[x / 256][w];
+      }
+      if (s.y > block_e0) {
+        const int to = before_wave + __popcll(m & ((1ull << lane) - 1));
+        list[to] = stage;
+        list_least[to] = s.x;
+        list_most[to] = s.y;
+      }
+    }
+    __syncthreads();
+    const int n = __builtin_amdgcn_readfirstlane(at);
+    if (n > 0) fetch(__builtin_amdgcn_readfirstlane(list[0]), 0);
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const int least = __builtin_amdgcn_readfirstlane(list_least[i]), most = __builtin_amdgcn_readfirstlane(list_most[i]);
+      const int next = __builtin_amdgcn_readfirstlane(list[min(i + 1, n - 1)]);
+      arrived();
+      if (i + 1 < n) fetch(next, (i + 1) & 1);
+      if (most <= e0) continue;                    // (wave-uniform)
+      if (least >= e0 + 32 * kSubs) work(i & 1, false);
+      else work(i & 1, true);
+    }
   }
-  float w = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  w += __shfl_xor(w, 32);
-  if (h != 0 || e0 + c >= a.length) return;
-  if (!there) w = 0.f;
-  if (a.n_split > 1) {
-    a.part[(static_cast<size_t>(split) * a.n_seqs * a.n_kv_heads + unit) * a.length + e0 + c] = w;
-    return;
+#pragma unroll
+  for (int x = 0; x < kSubs; ++x) {
+    float w = sum[x][0] + sum[x][1];
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+    w = there[x] ? __uint_as_float(both[0]) + __uint_as_float(both[1]) : 0.f;
+    const int entry = e0 + 32 * x + c;
+    if (h != 0 || entry >= a.length) continue;
+    if (a.n_split > 1) {
+      a.part[(static_cast<size_t>(split) * a.n_seqs * a.n_kv_heads + unit) * a.length + entry] = w;
+    } else {
+      const long long at = static_cast<long long>(unit) * a.stride + entry;
+      a.weights[at] = before(a, at, entry) + w;
+    }
   }
-  const long long at = static_cast<long long>(unit) * a.stride + e0 + c;
-  a.weights[at] = before(a, at, e0 + c) + w;
 }
 
 __global__ __launch_bounds__(256) void weigh_join_kernel(const WeighArgs a) {
@@ -141,38 +354,90 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(const WeighArgs a) {
   a.weights[at] = before(a, at, entry) + w;
 }
 
-// Splits of the rows: a few blocks for every compute unit.
-int splits_of(const WeighArgs &a) {
-  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.length + kEntries - 1) / kEntries);
-  const int tiles = (a.n_tokens * a.group + 31) / 32;
-  long long n = blocks > 0 ? 1024 / blocks : 1;
-  if (n > tiles / 4) n = tiles / 4;
-  return static_cast<int>(n < 1 ? 1 : n > kSplitMax ? kSplitMax : n);
+// How a call is cut.
+struct Plan { int many, across, stages, n_split; };
+Plan plan_of(const WeighArgs &a) {
+  Plan p = {0, 0, 0, 1};
+  const int M = a.n_tokens * a.group, units = a.n_seqs * a.n_kv_heads;
+  p.many = M > 32;
+  if (!p.many) {                                   // (two blocks a compute unit, a few tiles a wave where there are so many)
+    const int blocks = ((a.length + 31) / 32 + 3) / 4, most = (1024 + units - 1) / units;
+    p.across = blocks < most ? blocks : most;
+    return p;
+  }
+  const int entries = a.dtype == LAZYEV_DTYPE_FP32 ? Rows<float, 64>::kEntries : Rows<bf16_t, 64>::kEntries;
+  p.across = (a.length + entries - 1) / entries;
+  p.stages = (M + kStageRows - 1) / kStageRows;
+  const long long blocks = static_cast<long long>(units) * p.across;
+  long long n = 1024 / blocks;                     // (late blocks have less to do where tokens see their past: four for a compute unit)
+  if (n > p.stages / 4) n = p.stages / 4;
+  p.n_split = static_cast<int>(n < 1 ? 1 : n > kSplitMax ? kSplitMax : n);
+  return p;
+}
+
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+size_t rows_of(const WeighArgs &a, const Plan &p) { return static_cast<size_t>(a.n_seqs) * a.n_kv_heads * p.stages * kStageRows; }
+size_t parts_of(const WeighArgs &a, const Plan &p) {
+  return p.n_split > 1 ? align_up(static_cast<size_t>(p.n_split) * a.n_seqs * a.n_kv_heads * a.length * 4) : 0;
 }
 
 template <typename T, int D>
-hipError_t launch(const WeighArgs &a, hipStream_t stream) {
-  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.length + kEntries - 1) / kEntries);
+hipError_t launch(const WeighArgs &a, const Plan &p, hipStream_t stream) {
+  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * p.across * p.n_split;
   if (blocks < 1 || blocks >= (1ll << 24)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((weigh_kernel<T, D>), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.n_split)), dim3(256), 0, stream, a);
+  const dim3 grid(static_cast<unsigned>(blocks));
+  if (p.many) {
+    hipLaunchKernelGGL((weigh_many_kernel<T, D>), grid, dim3(256), 0, stream, a);
+    return hipGetLastError();
+  }
+  switch ((a.n_tokens * a.group + 7) / 8) {
+    case 0:
+    case 1: hipLaunchKernelGGL((weigh_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((weigh_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, a); break;
+    default: hipLaunchKernelGGL((weigh_few_kernel<T, D, 4>), grid, dim3(256), 0, stream, a);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t weigh_workspace(const WeighArgs &a) {
-  const int n = splits_of(a);
-  return n > 1 ? (static_cast<size_t>(n) * a.n_seqs * a.n_kv_heads * a.length * 4 + 255) / 256 * 256 : 0;
+  const Plan p = plan_of(a);
+  if (!p.many) return 0;
+  return 2 * align_up(rows_of(a, p) * 4) + align_up(rows_of(a, p) / kStageRows * sizeof(int2)) + parts_of(a, p);
 }
 
 hipError_t launch_weigh(WeighArgs a, hipStream_t stream) {
-  a.n_split = splits_of(a);
+  const Plan p = plan_of(a);
+  a.across = p.across;
+  a.stages = p.stages;
+  a.n_split = p.n_split;
   a.wide = reinterpret_cast<uintptr_t>(a.q) % 16 == 0;
-  hipError_t e;
-  if (a.dtype == LAZYEV_DTYPE_FP32) e = a.head_dim == 64 ? launch<float, 64>(a, stream) : launch<float, 128>(a, stream);
-  else e = a.head_dim == 64 ? launch<bf16_t, 64>(a, stream) : launch<bf16_t, 128>(a, stream);
-  if (e != hipSuccess || a.n_split <= 1) return e;
   const long long n = static_cast<long long>(a.n_seqs) * a.n_kv_heads * a.length;
+  hipError_t e;
+  if (a.n_tokens == 0) {                           // what there was before, alone
+    a.n_split = 0;
+    hipLaunchKernelGGL(weigh_join_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+  }
+  if (p.many) {
+    const size_t rows = rows_of(a, p);
+    char *w = static_cast<char *>(a.workspace);
+    a.row_lse = reinterpret_cast<float *>(w);
+    w += align_up(rows * 4);
+    a.row_sees = reinterpret_cast<int32_t *>(w);
+    w += align_up(rows * 4);
+    a.stage_sees = reinterpret_cast<int2 *>(w);
+    w += align_up(rows / kStageRows * sizeof(int2));
+    a.part = reinterpret_cast<float *>(w);
+    if ((rows + 255) / 256 >= (1u << 24)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(weigh_rows_kernel, dim3(static_cast<unsigned>((rows + 255) / 256)), dim3(256), 0, stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dtype == LAZYEV_DTYPE_FP32) e = a.head_dim == 64 ? launch<float, 64>(a, p, stream) : launch<float, 128>(a, p, stream);
+  else e = a.head_dim == 64 ? launch<bf16_t, 64>(a, p, stream) : launch<bf16_t, 128>(a, p, stream);
+  if (e != hipSuccess || p.n_split <= 1) return e;
   hipLaunchKernelGGL(weigh_join_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
