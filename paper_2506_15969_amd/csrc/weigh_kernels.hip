@@ -84,10 +84,12 @@ __device__ __forceinline__ void logits(const u32x4_t (&q)[Rows<T, D>::kOps], con
 // What an entry had before.
 __device__ __forceinline__ float before(const WeighArgs &a, long long at, int entry) { return entry < a.known ? a.decay * a.old[at] : 0.f; }
 
-// Where the keys of an entry lie (any: some entry's).
-__device__ __forceinline__ size_t key_row(const WeighArgs &a, int seq, int kvh, int entry, bool &there) {
+// The number of an entry's page, and where its keys lie there (any: some entry's).
+__device__ __forceinline__ unsigned page_number(const WeighArgs &a, int seq, int entry) {
+  return static_cast<unsigned>(a.pages.table[static_cast<long long>(seq) * a.pages.stride + page_of(a.pages, entry)]);
+}
+__device__ __forceinline__ size_t key_row(const WeighArgs &a, int kvh, int entry, unsigned no, bool &there) {
   const int pg = page_of(a.pages, entry);
-  const unsigned no = static_cast<unsigned>(a.pages.table[static_cast<long long>(seq) * a.pages.stride + pg]);
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
   there = no < static_cast<unsigned>(a.pages.n_pages);
   return (there ? no : 0u) * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
@@ -95,71 +97,101 @@ __device__ __forceinline__ size_t key_row(const WeighArgs &a, int seq, int kvh, 
 
 // ------------------------------------------------------------------------------------ few rows
 
-// Blocks of 256: wave w of block x of a unit has the tiles of 32 entries 4 x + w, and every 4 a.across further.  kEights: groups of eight rows.
-template <typename T, int D, int kEights>
+// Blocks of 256: wave w of block x of a unit has the tiles of 32 entries 4 x + w, and every 4 a.across further, in halves of 16: 16x16x32_bf16 (fp32
+// rows: 16x16x4_f32), lane (c, g) = (l % 16, l / 16) holds the rows 4 g + j of each 16 for entry c, and a load of keys has 64 bytes
+// of each of 16 entries.  kTiles: tiles of 16 rows.
+template <typename T, int D, int kTiles>
 __global__ __launch_bounds__(256) void weigh_few_kernel(const WeighArgs a) {
   using R = Rows<T, D>;
-  constexpr int kOps = R::kOps;
+  constexpr int kOps = R::kChunks / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = lane & 31, h = lane >> 5;
+  const int c = lane & 15, g = lane >> 4;
   const int unit = static_cast<int>(blockIdx.x) / a.across, x0 = static_cast<int>(blockIdx.x) - unit * a.across;
   const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
   const int M = a.n_tokens * a.group, tiles = (a.length + 31) / 32, step = 4 * a.across;
   int tile = 4 * x0 + wave;
   if (tile >= tiles) return;
-  bool there[2];
-  u32x4_t k[2][kOps];
-  auto fetch = [&](int tl, int buf) __attribute__((always_inline)) {
-    const char *from = static_cast<const char *>(a.k_pages) + key_row(a, seq, kvh, min(tl * 32 + c, a.length - 1), there[buf]) * (D * sizeof(T)) + h * 16;
+  bool there[2][2];
+  u32x4_t k[2][2][kOps];
+  // (page numbers are asked for before the keys of the tile before: who waits for them does not wait for keys that are not needed yet.  32768
+  // entries of 128 units, 5 rows each: 228 -> 212 us.  What the entries had before, asked for like that too: 219)
+  unsigned no[2][2];
+  auto numbers = [&](int tl, int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) k[buf][j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+    for (int y = 0; y < 2; ++y) no[buf][y] = page_number(a, seq, min(tl * 32 + 16 * y + c, a.length - 1));
   };
+  auto fetch = [&](int tl, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const char *from = static_cast<const char *>(a.k_pages) + key_row(a, kvh, min(tl * 32 + 16 * y + c, a.length - 1), no[buf][y], there[buf][y]) * (D * sizeof(T)) + g * 16;
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) k[buf][y][j] = *reinterpret_cast<const u32x4_t *>(from + j * 64);
+    }
+  };
+  numbers(tile, 0);
+  numbers(min(tile + step, tiles - 1), 1);
   fetch(tile, 0);
-  u32x4_t q[kOps];
+  u32x4_t q[kTiles][kOps];
   long long token;
-  {
-    const T *from = static_cast<const T *>(a.q) + row_of(a, seq, kvh, min(c, M - 1), token) * D + h * (16 / sizeof(T));
+  float ref[kTiles][4];
+  int sees[kTiles][4], least = INT_MAX;
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) q[j] = load_chunk(from + j * (32 / sizeof(T)), a.wide);
-  }
-  float ref[4 * kEights];
-  int sees[4 * kEights];
-  int least = INT_MAX;
+  for (int t = 0; t < kTiles; ++t) {
+    const T *from = static_cast<const T *>(a.q) + row_of(a, seq, kvh, min(16 * t + c, M - 1), token) * D + g * (16 / sizeof(T));
 #pragma unroll
-  for (int x = 0; x < 4 * kEights; ++x) {
-    const int r = 8 * (x / 4) + 4 * h + x % 4;
-    const long long row = row_of(a, seq, kvh, min(r, M - 1), token);
-    const float lse = a.lse[row];
-    sees[x] = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
-    if (r >= M || lse == -INFINITY) sees[x] = 0;
-    ref[x] = sees[x] > 0 ? lse * kLog2e : 0.f;
-    least = min(least, sees[x]);
+    for (int j = 0; j < kOps; ++j) q[t][j] = load_chunk(from + j * (64 / sizeof(T)), a.wide);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int r = 16 * t + 4 * g + x;
+      const long long row = row_of(a, seq, kvh, min(r, M - 1), token);
+      const float lse = a.lse[row];
+      int n = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
+      if (r >= M || lse == -INFINITY) n = 0;
+      ref[t][x] = n > 0 ? lse * kLog2e : 0.f;
+      sees[t][x] = n;
+      least = min(least, r < M ? n : a.length);
+    }
   }
+  // (rows past the last do not add: the masks of a tile that all rows see leave out whole lanes)
   const float c2 = a.scale * kLog2e;
   auto work = [&](int tl, int buf) __attribute__((always_inline)) {
-    f32x16_t s;
-    logits<T, D>(q, k[buf], s);
-    const int entry = tl * 32 + c;
-    float w = 0.f;
-    if (__builtin_amdgcn_ballot_w64(least < tl * 32 + 32) == 0) {       // (wave-uniform)
+    const bool all = __builtin_amdgcn_ballot_w64(least < min(tl * 32 + 32, a.length)) == 0;   // (wave-uniform)
 #pragma unroll
-      for (int x = 0; x < 4 * kEights; ++x) w += __builtin_amdgcn_exp2f(fmaf(s[x], c2, -ref[x]));
-    } else {
+    for (int y = 0; y < 2; ++y) {
+      const int entry = tl * 32 + 16 * y + c;
+      float w = 0.f;
 #pragma unroll
-      for (int x = 0; x < 4 * kEights; ++x) w += entry < sees[x] ? __builtin_amdgcn_exp2f(fmaf(s[x], c2, -ref[x])) : 0.f;
-    }
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
-    w = there[buf] ? __uint_as_float(both[0]) + __uint_as_float(both[1]) : 0.f;
-    if (h == 0 && entry < a.length) {
-      const long long at = static_cast<long long>(unit) * a.stride + entry;
-      a.weights[at] = before(a, at, entry) + w;
+      for (int t = 0; t < kTiles; ++t) {
+        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kOps; ++j) {
+          if constexpr (R::kF32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[t][j][e]), __uint_as_float(k[buf][y][j][e]), s, 0, 0, 0);
+          } else {
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, q[t][j]), __builtin_bit_cast(bf16x8_t, k[buf][y][j]), s, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[x], c2, -ref[t][x]));
+          w += (all ? 16 * t + 4 * g + x < M : entry < sees[t][x]) ? p : 0.f;
+        }
+      }
+      const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+      w = __uint_as_float(r16[0]) + __uint_as_float(r16[1]);
+      const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+      w = there[buf][y] ? __uint_as_float(r32[0]) + __uint_as_float(r32[1]) : 0.f;
+      if (g == 0 && entry < a.length) a.weights[static_cast<long long>(unit) * a.stride + entry] = before(a, static_cast<long long>(unit) * a.stride + entry, entry) + w;
     }
   };
   while (true) {
+    numbers(min(tile + 2 * step, tiles - 1), 0);
     if (tile + step < tiles) fetch(tile + step, 1);
     work(tile, 0);
     tile += step;
     if (tile >= tiles) break;
+    numbers(min(tile + 2 * step, tiles - 1), 1);
     if (tile + step < tiles) fetch(tile + step, 0);
     work(tile, 1);
     tile += step;
@@ -216,7 +248,7 @@ __global__ __launch_bounds__(256, 2) void weigh_many_kernel(const WeighArgs a) {
   u32x4_t k[kSubs][kOps];
 #pragma unroll
   for (int x = 0; x < kSubs; ++x) {
-    const char *from = static_cast<const char *>(a.k_pages) + key_row(a, seq, kvh, min(e0 + 32 * x + c, a.length - 1), there[x]) * (D * sizeof(T)) + h * 16;
+    const char *from = static_cast<const char *>(a.k_pages) + key_row(a, kvh, min(e0 + 32 * x + c, a.length - 1), page_number(a, seq, min(e0 + 32 * x + c, a.length - 1)), there[x]) * (D * sizeof(T)) + h * 16;
 #pragma unroll
     for (int j = 0; j < kOps; ++j) k[x][j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
   }
@@ -390,12 +422,8 @@ hipError_t launch(const WeighArgs &a, const Plan &p, hipStream_t stream) {
     hipLaunchKernelGGL((weigh_many_kernel<T, D>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
   }
-  switch ((a.n_tokens * a.group + 7) / 8) {
-    case 0:
-    case 1: hipLaunchKernelGGL((weigh_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((weigh_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, a); break;
-    default: hipLaunchKernelGGL((weigh_few_kernel<T, D, 4>), grid, dim3(256), 0, stream, a);
-  }
+  if (a.n_tokens * a.group <= 16) hipLaunchKernelGGL((weigh_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((weigh_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
