@@ -252,6 +252,11 @@ struct ListArgs {
   int32_t tokens;                   // of a sequence: n_seqs of the arguments / tokens table rows
   int32_t entries;                  // of a table row: what `visible` goes up to
   int32_t run_shift;                // entries next to one another in a page and in a block: runs of 1 << run_shift
+  // filled in by the launch where tiles of tokens share their lists: tiles of a table row; of a tile and KV head the blocks that some of its tokens
+  // read with a bit for each that does, n_listed for every token at most, and their number
+  int32_t tiles;
+  int2 *pairs;
+  int32_t *counts;
 };
 // Attention over pages (see lazyev_pages_attend).
 struct AttendArgs {

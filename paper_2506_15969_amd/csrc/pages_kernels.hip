@@ -135,6 +135,18 @@ __device__ __forceinline__ RowPlace row_place(const AttendArgs &a, int unit, int
   return p;
 }
 
+// Rows of tiles of tokens (see kPerTile): a place that row_place gave by the tile made that among all tokens; rows of the tile, of which a
+// table row's last one may have fewer.
+__device__ __forceinline__ int tile_token0(const AttendArgs &a, int tile, int &table_row) {
+  table_row = tile / a.list.tiles;
+  return (tile - table_row * a.list.tiles) * a.n_tokens;
+}
+__device__ __forceinline__ int tile_rows(const AttendArgs &a, int token0) { return min(a.n_tokens, a.list.tokens - token0) * a.group; }
+__device__ __forceinline__ void place_in_tile(const AttendArgs &a, int tile, int table_row, int token0, RowPlace &p) {
+  p.token += table_row * a.list.tokens + token0 - tile * a.n_tokens;
+  p.row = static_cast<long long>(p.token) * a.n_q_heads + p.kvh * a.group + p.head;
+}
+
 // Four output elements of a row (columns e0 .. e0 + 3) joined with the other part and stored.
 template <typename T, int D>
 __device__ __forceinline__ void finish4(const AttendArgs &a, const RowPlace &p, int e0, f32x4_t o, const Joined &j) {
@@ -233,40 +245,60 @@ struct Shape {
   static constexpr int kLoads = kKeys / (kPerLoad * kWaves);   // of K and of V each, per wave and stage
   static_assert(kSub >= 1 && kLoads >= 1 && kLoads * kPerLoad * kWaves == kKeys, "whole loads");
   static constexpr int kPerSimd = D * sizeof(T) == 512 ? 1 : 2;   // (fp32 rows of 128: queries and output take 128 registers, the products' operands more)
+  static constexpr int kWindow = 512;              // page numbers that a block keeps in LDS
   static constexpr int kHalf = kKeys * D * static_cast<int>(sizeof(T)), kStage = 2 * kHalf;   // bytes of a stage: of K, then of V
 };
-constexpr int kWindow = 512;            // page numbers that a block keeps in LDS
 
-// Entries of listed blocks (kListed: a unit is a token of a sequence and a KV head): entry x of the list is entry x % block of block list[x / block].
-// What a table of pages says of the others, the window says of runs of 1 << run_shift entries, which lie next to one another in a block
-// and in a page: the row of the first one and how many of them the token sees; those beyond are holes, as pages that are none.
-template <typename T, int D, int kWR, int kWK, int kKeys, bool kListed = false>
+// Entries of listed blocks: entry x of the list is entry x % block of block list[x / block].  What a table of pages says of the others, the
+// window says of runs of 1 << run_shift entries, which lie next to one another in a block and in a page: the row of the first one, and
+//   kPerToken  (a unit is a token of a sequence and a KV head) how many of them the token sees; those beyond are holes, as pages that are none
+//   kPerTile   (a unit is a tile of tokens and a KV head, the list one of pairs: a block that some of them read, and a bit for each that does)
+//              the number of the first one in the table's row and the tokens' bits, by which every row is masked
+enum Lists { kNoList, kPerToken, kPerTile };
+constexpr int kNowhere = 1 << 30;       // beyond any entry that a token sees
+template <typename T, int D, int kWR, int kWK, int kKeys, int kLists = kNoList>
 __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPerSimd)) void attend_kernel(const AttendArgs a) {
   using R = Rows<T, D>;
   using S = Shape<T, D, kWR, kWK, kKeys>;
   constexpr int kSub = S::kSub, kOps = R::kOps, kTiles = R::kTiles, C = R::kChunks;
+  constexpr bool kListed = kLists != kNoList, kPairs = kLists == kPerTile;
+  constexpr int kWindow = kPairs ? S::kBlock : S::kWindow;   // (kPerTile: fewer registers on the way)
   __shared__ __align__(16) char stages[2 * S::kStage];
   __shared__ int window[kWindow];
   __shared__ float shared_ml[kWK][kWR][64];
   __shared__ int shared_most[S::kWaves], shared_least[S::kWaves], shared_hole[2], shared_odd;
-  __shared__ int window_seen[kListed ? kWindow : 1], stage_seen[2][kListed ? kKeys : 1];   // (kListed) entries of a run that the token sees
+  // of a run (kPerToken) entries that the token sees; (kPerTile) the first one's number, and the tokens' bits
+  __shared__ int window_seen[kListed ? kWindow : 1], stage_seen[2][kListed ? kKeys : 1];
+  __shared__ unsigned window_bits[kPairs ? kWindow : 1], stage_bits[2][kPairs ? kKeys : 1];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, h = lane >> 5;
   const int wr = wave % kWR, wk = wave / kWR;
-  const int M = a.n_tokens * a.group;
+  int M = a.n_tokens * a.group;
   // (blocks of one unit, split and so on are as far from one another as there are units: those of eight units, or four, share
   // an XCD and its L2.)  Late rows first: where a token sees its past only, they have the most to do
   const int unit = static_cast<int>(blockIdx.x), split = static_cast<int>(blockIdx.y), span = static_cast<int>(gridDim.z - 1 - blockIdx.z);
   const int seq = a.n_seqs == 1 ? 0 : unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
   const int r0 = (span * kWR + wr) * 32;           // this wave's rows
+  // (kPerTile: the table's row, the tile of its tokens, of which the last may be smaller, and the entries of the list)
+  int table_row = kLists == kPerToken ? seq / a.list.tokens : seq, token0 = 0;
+  if constexpr (kPairs) {
+    token0 = tile_token0(a, seq, table_row);
+    M = tile_rows(a, token0);
+  }
   const bool have = r0 < M;
-  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  const int my_token = place.token - seq * a.n_tokens;       // of the tile
+  if constexpr (kPairs) place_in_tile(a, seq, table_row, token0, place);
+  const int length = kPairs ? a.list.counts[unit] << a.list.block_shift : a.length;
 
   // entries of this block: first .. last - 1
-  const int first = split * a.split_keys, last = min(first + a.split_keys, a.length);
-  const int32_t *table = a.pages.table + static_cast<long long>(kListed ? seq / a.list.tokens : seq) * a.pages.stride;
-  const int32_t *list = kListed ? a.list.list + static_cast<long long>(unit) * a.list.n_listed : nullptr;
+  // (kPerTile: lists are of lengths of their own, each cut into a.n_split parts)
+  const int split_keys = kPairs ? ((length + kKeys - 1) / kKeys + a.n_split - 1) / a.n_split * kKeys : a.split_keys;
+  const int first = kPairs ? min(split * split_keys, length) : split * split_keys, last = min(first + split_keys, length);
+  const int32_t *table = a.pages.table + static_cast<long long>(table_row) * a.pages.stride;
+  const int32_t *list = kLists == kPerToken ? a.list.list + static_cast<long long>(unit) * a.list.n_listed : nullptr;
+  const int2 *pairs = kPairs ? a.list.pairs + static_cast<long long>(unit) * a.list.n_listed * a.n_tokens : nullptr;
   // (what the window goes by: a page, or a run)
   auto slot_of = [&](int entry) __attribute__((always_inline)) { return kListed ? entry >> a.list.run_shift : page_of(a.pages, entry); };
   // everything that is read before the first stage is worked on is asked for at once
@@ -286,10 +318,11 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       }
     }
   }
-  const float lse_other = lse_joined(a, place);
+  constexpr bool kLate = kPairs && kWK == 1;       // (nobody else of the block replaces it; fewer registers on the way)
+  float lse_other = kLate ? 0.f : lse_joined(a, place);
   int seen = a.visible ? min(max(a.visible[place.token], 0), kListed ? a.list.entries : a.length) : kListed ? a.list.entries : a.length;
-  const int reach = seen;                          // (kListed: entries of the table row that the unit's token sees)
-  if constexpr (kListed) seen = reach > 0 ? a.length : 0;
+  const int reach = seen;                          // (kListed: entries of the table row that the row's token sees)
+  if constexpr (kListed) seen = reach > 0 ? length : 0;
 
   // ---- stages on their way to LDS.  Loads go from memory to LDS, 1 KB a wave, in the order of the addresses there.  (Written out, as
   // the compiler has every read of LDS wait for all loads into it: they leave nothing in registers, and the waits for
@@ -301,18 +334,28 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     else __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
   };
   const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
-  // The row of the pools that a run begins with, and the entries of it that are there and that the token sees.
-  auto run_at = [&](int slot, int &n) __attribute__((always_inline)) {
-    const int shift = a.list.block_shift - a.list.run_shift, b = list[slot >> shift];
-    const int in_block = (slot & ((1 << shift) - 1)) << a.list.run_shift;
-    n = 0;
-    if (b < 0 || b > (reach - 1) >> a.list.block_shift) return 0u;
+  // The row of the pools that a run begins with, and of its entries those that are there and that the token sees, or (kPerTile) the first
+  // one's number, beyond any that a token sees where they are not there, and the tokens' bits.
+  auto run_at = [&](int slot, int &n, unsigned &bits) __attribute__((always_inline)) {
+    const int shift = a.list.block_shift - a.list.run_shift, in_block = (slot & ((1 << shift) - 1)) << a.list.run_shift;
+    const int limit = kPairs ? a.list.entries : reach;
+    int b;
+    if constexpr (kPairs) {
+      const int2 pair = pairs[slot >> shift];
+      b = pair.x;
+      bits = static_cast<unsigned>(pair.y);
+      n = kNowhere;
+    } else {
+      b = list[slot >> shift];
+      n = 0;
+    }
+    if (b < 0 || b > (limit - 1) >> a.list.block_shift) return 0u;
     const int entry = (b << a.list.block_shift) + in_block;
-    if (entry >= reach) return 0u;
+    if (entry >= limit) return 0u;
     const int pg = page_of(a.pages, entry);
     const unsigned no = static_cast<unsigned>(table[pg]);
     if (no >= static_cast<unsigned>(a.pages.n_pages)) return 0u;
-    n = min(1 << a.list.run_shift, reach - entry);
+    n = kPairs ? entry : min(1 << a.list.run_shift, limit - entry);
     return no * page_rows + kvh * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
   };
   int window_at = slot_of(first);
@@ -326,8 +369,12 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       unsigned no = static_cast<unsigned>(number(pg, u)), pool_row;
       if constexpr (kListed) {
         const int n = window_seen[pg - window_at], at = entry & ((1 << a.list.run_shift) - 1);
-        hole |= at >= n;
-        pool_row = no + static_cast<unsigned>(max(min(at, n - 1), 0));
+        if constexpr (kPairs) {                    // (every stage is masked; a run lies in one page as a whole)
+          pool_row = n == kNowhere ? 0u : no + static_cast<unsigned>(at);
+        } else {
+          hole |= at >= n;
+          pool_row = no + static_cast<unsigned>(max(min(at, n - 1), 0));
+        }
       } else {
         if (no >= static_cast<unsigned>(a.pages.n_pages)) {   // no page: any row; its entries are masked
           hole = true;
@@ -348,12 +395,14 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   const int page_last = last > first ? slot_of(last - 1) : 0;
   auto fill_window = [&]() __attribute__((always_inline)) {
     int no[kWindow / S::kBlock], runs[kListed ? kWindow / S::kBlock : 1];
+    unsigned bits[kListed ? kWindow / S::kBlock : 1];
 #pragma unroll
     for (int i = 0; i < kWindow / S::kBlock; ++i) {
       const int pg = window_at + i * S::kBlock + static_cast<int>(threadIdx.x);
       if constexpr (kListed) {
         no[i] = runs[i] = 0;
-        if (pg <= page_last) no[i] = static_cast<int>(run_at(pg, runs[i]));
+        bits[i] = 0;
+        if (pg <= page_last) no[i] = static_cast<int>(run_at(pg, runs[i], bits[i]));
       } else {
         no[i] = pg <= page_last ? table[pg] : 0;
       }
@@ -362,6 +411,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     for (int i = 0; i < kWindow / S::kBlock; ++i) {
       window[i * S::kBlock + threadIdx.x] = no[i];
       if constexpr (kListed) window_seen[i * S::kBlock + threadIdx.x] = runs[i];
+      if constexpr (kPairs) window_bits[i * S::kBlock + threadIdx.x] = bits[i];
     }
   };
   // (kListed) what the token sees of a stage's runs, for the masks: the window may have moved on by then
@@ -369,6 +419,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     if (static_cast<int>(threadIdx.x) < kKeys >> a.list.run_shift) {
       const int x = (e0 >> a.list.run_shift) + static_cast<int>(threadIdx.x) - window_at;
       stage_seen[buf][threadIdx.x] = x < kWindow ? window_seen[x] : 0;
+      if constexpr (kPairs) stage_bits[buf][threadIdx.x] = x < kWindow ? window_bits[x] : 0;
     }
   };
   bool hole_0 = false;
@@ -416,7 +467,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   const int n_stages = end > first ? (end - first + kKeys - 1) / kKeys : 0;
   // the first stage that some row does not see all of
   // (with weights in terms, of which the second may be negative or zero: as if it were the first of all)
-  const int mask_from = R::kTerms > 1 ? 0 : max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
+  const int mask_from = R::kTerms > 1 || kPairs ? 0 : max(__builtin_amdgcn_readfirstlane(min(block_least, last)) - first, 0) / kKeys;
   int masked = INT_MAX;                            // ... and the first one with anything masked
 
   auto fetch = [&](int st, int buf) __attribute__((always_inline)) {
@@ -429,7 +480,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
     const bool hole = load_stage(e0, end - 1, buf, [&](int pg, int) __attribute__((always_inline)) { return window[pg - window_at]; });
     if constexpr (kListed) keep_runs(e0, buf);
-    if (hole) shared_hole[buf] = st + 1;           // (by the barrier before the stage is worked on)
+    if (!kPairs && hole) shared_hole[buf] = st + 1;   // (by the barrier before the stage is worked on)
   };
   // Waits for this wave's loads and for the other waves.
   auto arrived = [&]() __attribute__((always_inline)) {
@@ -464,9 +515,11 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
   auto logits = [&](const char *ks, int e0, f32x16_t &s) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) s[x] = 0.f;
+    int k_0 = k_at[0];                             // (kPerTile: the places of the others worked out rather than kept, an exclusive or each)
+    if constexpr (kPairs) __asm__("" : "+v"(k_0));
 #pragma unroll
     for (int j = 0; j < kOps; ++j) {
-      const u32x4_t ka = *reinterpret_cast<const u32x4_t *>(ks + k_at[j] + e0 * kEntry);
+      const u32x4_t ka = *reinterpret_cast<const u32x4_t *>(ks + (kPairs ? k_0 ^ 32 * j : k_at[j]) + e0 * kEntry);
       if constexpr (R::kF32) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -539,30 +592,66 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     return sum;
   };
 
-  auto work = [&](const char *ks, const char *vs, int st, bool holes) __attribute__((always_inline)) {
+  auto work = [&](const char *ks, const char *vs, int st, int buf, bool holes) __attribute__((always_inline)) {
     const int key0 = first + st * kKeys + wk * (32 * kSub);   // this wave's entries
     ks += wk * (32 * kSub * kEntry);
     vs += wk * (32 * kSub * kEntry);
     if (key0 >= most) return;                      // (wave-uniform) nobody sees them
+    // (kPerTile) what the lane's row sees of the entries of a run from one on, `left` at most
+    const int shift = kPairs ? a.list.run_shift : 0, in_stage = wk * (32 * kSub) + 4 * h;
+    const bool whole_runs = shift >= 5;            // (uniform) 32 entries are always of one run
+    auto seen_of = [&](int key, int left) __attribute__((always_inline)) {
+      const int run = key >> shift;
+      const int n = (stage_bits[buf][kPairs ? run : 0] >> my_token & 1u) != 0 ? reach : 0;
+      return min(n - stage_seen[buf][kListed ? run : 0] - (key & ((1 << shift) - 1)), left);
+    };
+    if constexpr (kPairs) {
+      if (whole_runs) {
+        bool some = false;
+#pragma unroll
+        for (int x = 0; x < kSub; ++x) some |= seen_of(in_stage + 32 * x, last - key0 - 4 * h - 32 * x) > 0;
+        if (__builtin_amdgcn_ballot_w64(some) == 0) return;            // the wave's tokens read none of them
+      }
+    }
     f32x16_t s[kSub];
     Weights p[kSub];
 #pragma unroll
     for (int x = 0; x < kSub; ++x) logits(ks, 32 * x, s[x]);
-    ahead<kSub * kOps, R::kF32 ? 4 : 1, 1, R::kF32 ? 2 : 4>();
-    const bool mask = holes || key0 + 32 * kSub > min(least, last);
+    ahead<kSub * kOps, R::kF32 ? 4 : 1, 1, R::kF32 || kPairs ? 2 : 4>();
+    if constexpr (kPairs) {                        // each row by its token's bit and what it sees
+#pragma unroll
+      for (int x = 0; x < kSub; ++x) {
+        if (whole_runs) {
+          const int n = seen_of(in_stage + 32 * x, last - key0 - 4 * h - 32 * x);
+          if (__builtin_amdgcn_ballot_w64(n < 28) == 0) continue;      // all of them, for every row
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[x][i] = 8 * (i / 4) + i % 4 < n ? s[x][i] : -INFINITY;
+        } else {
+          unsigned there = 0;
+#pragma unroll 1
+          for (int i = 0; i < 16; ++i) {
+            const int key = 32 * x + 8 * (i / 4) + i % 4;
+            there |= seen_of(in_stage + key, last - key0 - 4 * h - key) > 0 ? 1u << i : 0u;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[x][i] = there >> i & 1u ? s[x][i] : -INFINITY;
+        }
+      }
+    }
+    const bool mask = !kPairs && (holes || key0 + 32 * kSub > min(least, last));
     if (mask) {
       const int limit = min(seen, last) - key0 - 4 * h;
       unsigned there[kSub];                        // bit i: the entry is on a page
 #pragma unroll
       for (int x = 0; x < kSub; ++x) there[x] = 0xFFFFu;
-      if (kListed && holes) {
+      if (kLists == kPerToken && holes) {
         const int shift = a.list.run_shift, in_stage = wk * (32 * kSub) + 4 * h;
 #pragma unroll
         for (int x = 0; x < kSub; ++x)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int key = in_stage + 32 * x + 8 * (i / 4) + i % 4;
-            if ((key & ((1 << shift) - 1)) >= stage_seen[st & 1][key >> shift]) there[x] &= ~(1u << i);
+            if ((key & ((1 << shift) - 1)) >= stage_seen[buf][key >> shift]) there[x] &= ~(1u << i);
           }
       }
       if (!kListed && holes) {
@@ -615,7 +704,7 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
       for (int g = 0; g < kProducts; ++g)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) product(values(vs, 32 * x, t, g), p[x], g, o[t]);
-    ahead<kSub * kProducts * kTiles, R::kF32 ? 1 : R::kTerms, R::kF32 ? 1 : 2, 4>();
+    ahead<kSub * kProducts * kTiles, R::kF32 ? 1 : R::kTerms, R::kF32 ? 1 : 2, kPairs ? 2 : 4>();
   };
   // (of a stage's values; the stage is complete and nobody's yet)
   auto take_out = [&](char *vs) __attribute__((always_inline)) {
@@ -640,12 +729,12 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     arrived();
     if (st + 1 < n_stages) fetch(st + 1, (st + 1) & 1);
     char *at = stages + (st & 1) * S::kStage;
-    const bool holes = __builtin_amdgcn_readfirstlane(shared_hole[st & 1]) == st + 1;
+    const bool holes = !kPairs && __builtin_amdgcn_readfirstlane(shared_hole[st & 1]) == st + 1;
     if (holes || st >= mask_from) {
       masked = min(masked, st);
       if (__builtin_expect(again, 0)) take_out(at + S::kHalf);
     }
-    work(at, at + S::kHalf, st, holes);
+    work(at, at + S::kHalf, st, st & 1, holes);
     if (st + 1 < n_stages || masked == INT_MAX || again) continue;
     // what the masks met.  (A look at the outputs, once a block, in place of one at the values of every such stage: tokens that see parts of
     // 701 entries, 99 of 32 heads, 64 x fp32 22.4 -> 20.8 us, 64 x bf16 16.0 -> 13.4, 128 x bf16 16.7 -> 16.2; the same where little is masked.)
@@ -724,16 +813,30 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
     }
   }
   if (!have) return;
+  if constexpr (kPairs) {                          // (worked out anew rather than kept)
+    int r = min(r0 + c, M - 1);
+    __asm__("" : "+v"(r));
+    place = row_place(a, unit, r);
+    place_in_tile(a, seq, table_row, token0, place);
+    if constexpr (kLate) lse_other = lse_joined(a, place);
+  }
 
   if (__builtin_expect(again, 0) && __builtin_amdgcn_readfirstlane(shared_odd) == 2) {
     // the infinities and NaN that were taken out and that a row sees (with a weight above zero, however small)
     for (int key = first + masked * kKeys; key < min(last, most); ++key) {
       unsigned pool_row;
+      bool sees = key < seen;
       if constexpr (kListed) {
         int n = 0;
+        unsigned bits = 0;
         const int at = key & ((1 << a.list.run_shift) - 1);
-        pool_row = run_at(key >> a.list.run_shift, n) + static_cast<unsigned>(at);
-        if (at >= n) continue;
+        pool_row = run_at(key >> a.list.run_shift, n, bits) + static_cast<unsigned>(at);
+        if constexpr (kPairs) {
+          if (n == kNowhere) continue;
+          sees = (bits >> my_token & 1u) != 0 && n + at < reach;
+        } else if (at >= n) {
+          continue;
+        }
       } else {
         const int pg = page_of(a.pages, key), no = __builtin_amdgcn_readfirstlane(table[pg]);
         if (static_cast<unsigned>(no) >= static_cast<unsigned>(a.pages.n_pages)) continue;
@@ -748,14 +851,14 @@ __global__ __launch_bounds__(64 * kWR * kWK, (Shape<T, D, kWR, kWK, kKeys>::kPer
           float f;
           if constexpr (R::kF32) f = y;
           else f = __uint_as_float(static_cast<unsigned>(y) << 16);
-          part[k][e] += key < seen && !(fabsf(f) <= FLT_MAX) ? f : 0.f;
+          part[k][e] += sees && !(fabsf(f) <= FLT_MAX) ? f : 0.f;
         }
     }
   }
 
   if (a.n_split > 1) {
     // for the second kernel: [unit][32 rows][split][group][lane] float4, and (m, l) of the rows
-    const int tiles = (M + 31) / 32;
+    const int tiles = (a.n_tokens * a.group + 31) / 32;
     const size_t p = (static_cast<size_t>(unit) * tiles + r0 / 32) * a.n_split + split;
     f32x4_t *to = reinterpret_cast<f32x4_t *>(a.part_o) + p * (4 * kTiles * 64) + lane;
 #pragma unroll
@@ -782,7 +885,8 @@ __global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const Atten
   __shared__ float lsums[kGroups][32];
   const int lane = threadIdx.x & 63, i = threadIdx.x >> 6 & 3, g = threadIdx.x >> 8;
   const int c = lane & 31, h = lane >> 5;
-  const int M = a.n_tokens * a.group, tiles = (M + 31) / 32, n = a.n_split;
+  int M = a.n_tokens * a.group;
+  const int tiles = (M + 31) / 32, n = a.n_split;
   const int t = static_cast<int>(blockIdx.y), ut = static_cast<int>(blockIdx.x);
   const size_t p0 = static_cast<size_t>(ut) * n;
   const f32x4_t *from = reinterpret_cast<const f32x4_t *>(a.part_o) + p0 * (4 * kTiles * 64) + (4 * t + i) * 64 + lane;
@@ -827,7 +931,14 @@ __global__ __launch_bounds__(256 * kGroups) void attend_merge_kernel(const Atten
     for (int k = 0; k < kGroups - 1; ++k) sum += sums[k][threadIdx.x];
   }
   const int unit = tiles == 1 ? ut : ut / tiles, r0 = (ut - unit * tiles) * 32;
-  const RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  RowPlace place = row_place(a, unit, min(r0 + c, M - 1));
+  if (a.list.tiles > 0) {                          // (uniform)
+    const int tile = unit / a.n_kv_heads;
+    int table_row;
+    const int token0 = tile_token0(a, tile, table_row);
+    M = tile_rows(a, token0);
+    place_in_tile(a, tile, table_row, token0, place);
+  }
   if (r0 + c >= M || !takes_part(a, place.token)) return;
   const Joined j = join(m, l, lse_other);
   finish4<T, D>(a, place, 32 * t + 8 * i + 4 * h, sum, j);
@@ -925,16 +1036,28 @@ size_t bytes_of(const AttendArgs &a, const Plan &p) {
   return align_up(parts * 32 * a.head_dim * sizeof(float)) + align_up(parts * 64 * sizeof(float)) + align_up(tiles_of(a) * 32 * sizeof(float));
 }
 
-template <typename T, int D, int kWR, int kWK, int kKeys, bool kListed = false>
+template <typename T, int D, int kWR, int kWK, int kKeys, int kLists = kNoList>
 hipError_t launch_shape(const AttendArgs &a, hipStream_t stream) {
   const long long M = static_cast<long long>(a.n_tokens) * a.group, spans = (M + 32 * kWR - 1) / (32 * kWR);
   if (spans > 65535) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(a.n_seqs * a.n_kv_heads), static_cast<unsigned>(a.n_split), static_cast<unsigned>(spans));
-  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kListed>), grid, dim3(64 * kWR * kWK), 0, stream, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, kWR, kWK, kKeys, kLists>), grid, dim3(64 * kWR * kWK), 0, stream, a);
   return hipGetLastError();
 }
 
-template <typename T, int D, bool kListed = false>
+template <typename T, int D>
+hipError_t launch_merge(const AttendArgs &a, hipStream_t stream) {
+  if (a.n_split <= 1) return hipSuccess;
+  const size_t blocks = tiles_of(a);
+  if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(blocks), D / 32);
+  if (a.n_split <= 4) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 4>), grid, dim3(256), 0, stream, a);
+  else if (a.n_split <= 16) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 16>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((attend_merge_kernel<T, D, 4, kSplitMax>), grid, dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D, int kLists = kNoList>
 hipError_t launch(AttendArgs a, hipStream_t stream) {
   constexpr bool kLong = D * sizeof(T) == 512;
   const Plan p = plan_of<T, D>(a);
@@ -952,10 +1075,10 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
     a.part_lse = reinterpret_cast<float *>(w);
   }
   hipError_t e = hipErrorInvalidValue;
-  if constexpr (kListed) {                         // (rows of one token: up to 64)
-    if constexpr (kLong) e = launch_shape<T, D, 2, 2, 64, true>(a, stream);
-    else if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128, true>(a, stream);
-    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128, true>(a, stream);
+  if constexpr (kLists == kPerToken) {             // (rows of one token: up to 64)
+    if constexpr (kLong) e = launch_shape<T, D, 2, 2, 64, kPerToken>(a, stream);
+    else if (p.wr == 1) e = launch_shape<T, D, 1, 4, 128, kPerToken>(a, stream);
+    else if (p.wr == 2) e = launch_shape<T, D, 2, 4, 128, kPerToken>(a, stream);
   } else if constexpr (kLong) {
     if (p.wr == 2) e = launch_shape<T, D, 2, 2, 64>(a, stream);
     else if (p.wr == 4) e = launch_shape<T, D, 4, 1, 64>(a, stream);
@@ -965,14 +1088,135 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
     else if (p.wr == 4) e = launch_shape<T, D, 4, 2, 128>(a, stream);
     else if (p.wr == 8) e = launch_shape<T, D, 8, 1, 64>(a, stream);
   }
-  if (e != hipSuccess || p.n_split <= 1) return e;
-  const size_t blocks = tiles_of(a);
-  if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
-  const dim3 grid(static_cast<unsigned>(blocks), D / 32);
-  if (p.n_split <= 4) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 4>), grid, dim3(256), 0, stream, a);
-  else if (p.n_split <= 16) hipLaunchKernelGGL((attend_merge_kernel<T, D, 1, 16>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((attend_merge_kernel<T, D, 4, kSplitMax>), grid, dim3(1024), 0, stream, a);
-  return hipGetLastError();
+  return e == hipSuccess ? launch_merge<T, D>(a, stream) : e;
+}
+
+// The lists of a tile's tokens as one: blocks that some token reads, ascending, with a bit for each token that does.  A number that a
+// token's list has twice is a pair of its own, behind the others.  One block per unit.
+constexpr int kListBlocks = 8192;       // of a table row, whose bits LDS holds
+__global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
+  __shared__ unsigned bits[kListBlocks];
+  __shared__ int counts[4], again;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int unit = static_cast<int>(blockIdx.x), tile = unit / a.n_kv_heads, kvh = unit - tile * a.n_kv_heads;
+  const int table_row = tile / a.list.tiles, token0 = (tile - table_row * a.list.tiles) * a.n_tokens;
+  const int tokens = min(a.n_tokens, a.list.tokens - token0), n = tokens * a.list.n_listed;
+  const int n_blocks = (a.list.entries + (1 << a.list.block_shift) - 1) >> a.list.block_shift;
+  int2 *to = a.list.pairs + static_cast<long long>(unit) * a.list.n_listed * a.n_tokens;
+  for (int b = threadIdx.x; b < n_blocks; b += 256) bits[b] = 0;
+  if (threadIdx.x == 0) again = 0;
+  __syncthreads();
+  // number x of the tokens' lists, -1 where it is no block that its token sees
+  auto number = [&](int x, int &i) __attribute__((always_inline)) {
+    i = x / a.list.n_listed;
+    const long long token = static_cast<long long>(table_row) * a.list.tokens + token0 + i;
+    const int b = a.list.list[(token * a.n_kv_heads + kvh) * a.list.n_listed + (x - i * a.list.n_listed)];
+    const int reach = a.visible ? min(max(a.visible[token], 0), a.list.entries) : a.list.entries;
+    return b >= 0 && b <= (reach - 1) >> a.list.block_shift ? b : -1;
+  };
+  bool twice = false;
+  for (int x = threadIdx.x; x < n; x += 256) {
+    int i;
+    const int b = number(x, i);
+    if (b >= 0) twice |= (atomicOr(&bits[b], 1u << i) >> i & 1u) != 0;
+  }
+  if (twice) again = 1;
+  __syncthreads();
+  int at = 0;
+  for (int b0 = 0; b0 < n_blocks; b0 += 256) {
+    const int b = b0 + static_cast<int>(threadIdx.x);
+    const unsigned mine = b < n_blocks ? bits[b] : 0u;
+    const unsigned long long m = __ballot(mine != 0);
+    if (lane == 0) counts[wave] = __popcll(m);
+    __syncthreads();
+    int before = at;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      before += w < wave ? counts[w] : 0;
+      at += counts[w];
+    }
+    if (mine) to[before + __popcll(m & ((1ull << lane) - 1))] = make_int2(b, static_cast<int>(mine));
+    __syncthreads();
+  }
+  if (again) {                                     // (uniform) one after the other, in the lists' order
+    for (int b = threadIdx.x; b < n_blocks; b += 256) bits[b] = 0;
+    __syncthreads();
+    if (threadIdx.x == 0)
+      for (int x = 0; x < n; ++x) {
+        int i;
+        const int b = number(x, i);
+        if (b < 0) continue;
+        if (bits[b] >> i & 1u) to[at++] = make_int2(b, static_cast<int>(1u << i));
+        bits[b] |= 1u << i;
+      }
+  }
+  if (threadIdx.x == 0) a.list.counts[unit] = at;
+}
+
+// Tokens that share a block's rows, by their lists as one (0: every token on its own), in tiles of a table row's; blocks of wr times 32 rows; splits of a tile's list.
+struct TilePlan { int tokens, tiles, wr, n_split; };
+TilePlan tile_plan_of(const AttendArgs &a) {
+  TilePlan p = {0, 0, 0, 1};
+  const int n = a.list.tokens, n_blocks = (a.list.entries + (1 << a.list.block_shift) - 1) >> a.list.block_shift;
+  if (n < 2 || n_blocks > kListBlocks || n_blocks < 1 || static_cast<long long>(a.n_seqs) * a.n_kv_heads <= 256) return p;
+  const bool long_rows = a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 128;
+  const int most = (long_rows ? 64 : 128) / a.group;
+  p.tokens = n < most ? n : most < 32 ? most : 32;
+  if (p.tokens < 2) return TilePlan{0, 0, 0, 1};
+  p.tiles = (n + p.tokens - 1) / p.tokens;
+  const int rows = p.tokens * a.group;
+  p.wr = rows <= 32 && !long_rows ? 1 : rows <= 64 ? 2 : 4;
+  const long long units = static_cast<long long>(a.n_seqs / n) * p.tiles * a.n_kv_heads;
+  const long long stages = static_cast<long long>(a.length) / (p.wr == 4 || long_rows ? 64 : 128);   // of one token's list
+  long long split = (p.wr == 4 ? 512 : 256) / units;
+  if (split > stages / 4) split = stages / 4;
+  p.n_split = static_cast<int>(split < 1 ? 1 : split > kSplitMax ? kSplitMax : split);
+  return p;
+}
+struct TileBytes { size_t pairs, counts, part_o, part_ml, part_lse; };
+TileBytes tile_bytes_of(const AttendArgs &a, const TilePlan &p) {
+  const size_t units = static_cast<size_t>(a.n_seqs) / a.list.tokens * p.tiles * a.n_kv_heads, tiles = units * ((p.tokens * a.group + 31) / 32);
+  TileBytes b = {align_up(units * p.tokens * a.list.n_listed * sizeof(int2)), align_up(units * sizeof(int32_t)), 0, 0, 0};
+  if (p.n_split > 1) {
+    b.part_o = align_up(tiles * p.n_split * 32 * a.head_dim * sizeof(float));
+    b.part_ml = align_up(tiles * p.n_split * 64 * sizeof(float));
+    b.part_lse = align_up(tiles * 32 * sizeof(float));
+  }
+  return b;
+}
+
+template <typename T, int D>
+hipError_t launch_tiles(AttendArgs a, const TilePlan &p, hipStream_t stream) {
+  const int rows = a.n_seqs / a.list.tokens;       // of the table
+  const size_t units = static_cast<size_t>(rows) * p.tiles * a.n_kv_heads;
+  const TileBytes bytes = tile_bytes_of(a, p);
+  char *w = static_cast<char *>(a.workspace);
+  if (!w) return hipErrorInvalidValue;
+  a.list.pairs = reinterpret_cast<int2 *>(w);
+  w += bytes.pairs;
+  a.list.counts = reinterpret_cast<int32_t *>(w);
+  w += bytes.counts;
+  a.part_o = reinterpret_cast<float *>(w);
+  w += bytes.part_o;
+  a.part_ml = reinterpret_cast<float *>(w);
+  w += bytes.part_ml;
+  a.part_lse = reinterpret_cast<float *>(w);
+  a.list.tiles = p.tiles;
+  a.n_seqs = rows * p.tiles;
+  a.n_tokens = p.tokens;
+  a.n_split = p.n_split;
+  a.split_keys = 0;
+  a.wide = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.joined_out)) % 16 == 0;
+  hipLaunchKernelGGL(join_lists_kernel, dim3(static_cast<unsigned>(units)), dim3(256), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if constexpr (D * sizeof(T) == 512) {
+    e = launch_shape<T, D, 2, 2, 64, kPerTile>(a, stream);
+  } else {
+    e = p.wr == 1 ? launch_shape<T, D, 1, 4, 128, kPerTile>(a, stream)
+        : p.wr == 2 ? launch_shape<T, D, 2, 4, 128, kPerTile>(a, stream) : launch_shape<T, D, 4, 1, 64, kPerTile>(a, stream);
+  }
+  return e == hipSuccess ? launch_merge<T, D>(a, stream) : e;
 }
 
 }  // namespace
@@ -982,16 +1226,22 @@ size_t attend_workspace(const AttendArgs &a) {
   return a.head_dim == 64 ? bytes_of(a, plan_of<bf16_t, 64>(a)) : bytes_of(a, plan_of<bf16_t, 128>(a));
 }
 
-size_t attend_list_workspace(const AttendArgs &a) { return attend_workspace(a); }
+size_t attend_list_workspace(const AttendArgs &a) {
+  const TilePlan p = tile_plan_of(a);
+  if (p.tokens == 0) return attend_workspace(a);
+  const TileBytes b = tile_bytes_of(a, p);
+  return b.pairs + b.counts + b.part_o + b.part_ml + b.part_lse;
+}
 
 hipError_t launch_attend_list(const AttendArgs &a, hipStream_t stream) {
   if (a.n_tokens != 1 || a.group < 1 || a.group > 64 || a.list.tokens < 1 || a.list.run_shift > a.list.block_shift || a.list.run_shift > 6 ||
       a.length != a.list.n_listed << a.list.block_shift)
     return hipErrorInvalidValue;
-  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 64) return launch<float, 64, true>(a, stream);
-  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 128) return launch<float, 128, true>(a, stream);
-  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 64) return launch<bf16_t, 64, true>(a, stream);
-  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 128) return launch<bf16_t, 128, true>(a, stream);
+  const TilePlan p = tile_plan_of(a);
+  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 64) return p.tokens ? launch_tiles<float, 64>(a, p, stream) : launch<float, 64, kPerToken>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 128) return p.tokens ? launch_tiles<float, 128>(a, p, stream) : launch<float, 128, kPerToken>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 64) return p.tokens ? launch_tiles<bf16_t, 64>(a, p, stream) : launch<bf16_t, 64, kPerToken>(a, stream);
+  if (a.dtype == LAZYEV_DTYPE_BF16 && a.head_dim == 128) return p.tokens ? launch_tiles<bf16_t, 128>(a, p, stream) : launch<bf16_t, 128, kPerToken>(a, stream);
   return hipErrorInvalidValue;
 }
 
