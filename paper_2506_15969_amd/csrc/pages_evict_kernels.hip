@@ -1,11 +1,11 @@
 // Eviction by the weights that entries received (lazyev_pages_evict): which entries of a unit (table row and KV head) stay, and their rows
 // moved together.
 //
-// select  one block per unit.  Every entry has a key of 32 bits: the order of its weight (a NaN above all), below it what is no
-//         entry, above it the newest and the first entries.  The key of the last entry that stays is found bit by bit from
-//         the top, from counts of the keys that reach a candidate; of those equal to it the lowest stay.  Entries that stay below
-//         `keep` keep their places; the places of the others there are free, and the n-th of them is the source's of the n-th
-//         entry that stays from `keep` on.  All of these numbers are prefix sums over the entries in their order.
+// select  one block per unit, whose waves have the entries in 16 stretches.  Every entry has a key of 32 bits: the order of its weight (a NaN above
+//         all), below it what is no entry, above it the newest and the first entries.  The key of the last entry that stays is
+//         found by counts of 1024 equal parts of the keys' range, then of the part that it is in, and so on; of those equal to it the lowest
+//         stay.  Entries that stay below `keep` keep their places; the places of the others there are free, and the n-th of them is the
+//         source's of the n-th entry that stays from `keep` on: numbers that a wave counts along its stretch, behind those of the waves before.
 // move    copies rows, weights and positions.  A row is read from `keep` on and written below it, so no two moves touch one another
 //         and their order does not matter; moves in the entries' order (which would keep it) are as many as entries behind the first
 //         one that goes: about `keep` of them where a window of 64 goes from 2112, instead of at most 64.
@@ -19,7 +19,8 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
 
-constexpr int kSelectBlock = 1024, kSelectWaves = kSelectBlock / 64;
+constexpr int kSelectBlock = 1024, kSelectWaves = kSelectBlock / 64, kBins = 1024;
+constexpr int kOwnMoves = 256;          // moves of a unit that the selecting block makes itself
 
 // The order of weights, above 0 (no entry) and below ~0 (stays whatever it weighs).
 __device__ __forceinline__ unsigned weight_key(float w) {
@@ -27,191 +28,28 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return w != w ? 0xFFFFFFFEu : u ^ (static_cast<unsigned>(static_cast<int>(u) >> 31) | 0x80000000u);
 }
 
-// kRegs: keys that a thread keeps (entry x * kSelectBlock + thread), 0: the keys are made anew from memory for every look.
-template <int kRegs>
-__global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictArgs a) {
-  __shared__ int counts[2][kSelectWaves];
-  __shared__ int wave_i[kSelectWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int unit = static_cast<int>(blockIdx.x), seq = unit / a.n_kv_heads;
-  const int len = a.lengths ? min(max(a.lengths[seq], 0), a.length) : a.length;
-  int32_t *sources = a.sources + static_cast<size_t>(unit) * a.keep;
-  if (len <= a.keep) {
-    for (int i = threadIdx.x; i < a.keep; i += kSelectBlock) sources[i] = i < len ? i : -1;
-    return;
-  }
-  const float *weights = a.weights + static_cast<long long>(unit) * a.stride;
-  const int32_t *positions = a.positions ? a.positions + static_cast<long long>(unit) * a.stride : nullptr;
-
-  // positions from here on are the newest
-  int newest = len - 1;
-  if (positions) {
-    newest = INT_MIN;
-    for (int i = threadIdx.x; i < len; i += kSelectBlock) newest = max(newest, positions[i]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) newest = max(newest, __shfl_xor(newest, o));
-    if (lane == 0) wave_i[wave] = newest;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) newest = max(newest, wave_i[w]);
-  }
-  const long long recent_from = static_cast<long long>(newest) - a.n_recent + 1;
-  auto make_key = [&](int i) __attribute__((always_inline)) {
-    if (i >= len) return 0u;
-    const int p = positions ? positions[i] : i;
-    return p >= recent_from || p < a.n_first ? 0xFFFFFFFFu : weight_key(weights[i]);
-  };
-  constexpr int kHeld = kRegs > 0 ? kRegs : 1;
-  unsigned held[kHeld];
-  const int looks = kRegs > 0 ? kRegs : (len + kSelectBlock - 1) / kSelectBlock;
-  if constexpr (kRegs > 0) {
-#pragma unroll
-    for (int x = 0; x < kRegs; ++x) held[x] = make_key(x * kSelectBlock + static_cast<int>(threadIdx.x));
-  }
-  auto each = [&](auto f) __attribute__((always_inline)) {
-    if constexpr (kRegs > 0) {
-#pragma unroll
-      for (int x = 0; x < kRegs; ++x) f(x, held[x]);
-    } else {
-      for (int x = 0; x < looks; ++x) f(x, make_key(x * kSelectBlock + static_cast<int>(threadIdx.x)));
-    }
-  };
-
-  // the largest key that at least `keep` keys reach
-  unsigned border = 0;
-  int reach = len;                                 // keys that reach it
-  for (int bit = 31; bit >= 0 && reach != a.keep; --bit) {
-    const unsigned cand = border | 1u << bit;
-    int have = 0;
-    each([&](int, unsigned k) __attribute__((always_inline)) { have += __popcll(__ballot(k >= cand)); });
-    if (lane == 0) counts[bit & 1][wave] = have;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) all += counts[bit & 1][w];
-    if (all >= a.keep) {
-      border = cand;
-      reach = all;
-    }
-  }
-  __syncthreads();
-  // of the keys equal to it this many stay, the lowest
-  int above = 0;
-  each([&](int, unsigned k) __attribute__((always_inline)) { above += __popcll(__ballot(k > border)); });
-  if (lane == 0) counts[0][wave] = above;
-  __syncthreads();
-  above = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) above += counts[0][w];
-  const int equal = a.keep - above;
-
-  // in the entries' order: those equal, free places, entries that stay from `keep` on.  Two sweeps, as the free places are to
-  // be met before the entries that fill them: the first writes the numbers of the free places where the second looks them up
-  auto sweep = [&](auto f) __attribute__((always_inline)) {
-    int met = 0, nth = 0;                          // of all entries before this look
-    for (int x = 0; x < looks; ++x) {
-      const int i = x * kSelectBlock + static_cast<int>(threadIdx.x);
-      unsigned k;
-      if constexpr (kRegs > 0) {
-        k = 0;
-#pragma unroll
-        for (int y = 0; y < kRegs; ++y) k = y == x ? held[y] : k;
-      } else {
-        k = make_key(i);
-      }
-      const unsigned long long below = (1ull << lane) - 1, eq = __ballot(k == border && i < len);
-      __syncthreads();
-      if (lane == 0) counts[0][wave] = __popcll(eq);
-      __syncthreads();
-      int before = met;
-#pragma unroll
-      for (int w = 0; w < kSelectWaves; ++w) {
-        before += w < wave ? counts[0][w] : 0;
-        met += counts[0][w];
-      }
-      const bool stays = i < len && (k > border || (k == border && before + __popcll(eq & below) < equal));
-      const bool mine = f(i, stays);
-      const unsigned long long m = __ballot(mine);
-      if (lane == 0) counts[1][wave] = __popcll(m);
-      __syncthreads();
-      int at = nth;
-#pragma unroll
-      for (int w = 0; w < kSelectWaves; ++w) {
-        at += w < wave ? counts[1][w] : 0;
-        nth += counts[1][w];
-      }
-      at += __popcll(m & below);
-      f.put(i, stays, mine, at);
-    }
-  };
-  struct Free {
-    int32_t *sources, *list;
-    int keep;
-    __device__ bool operator()(int i, bool stays) const { return i < keep && !stays; }
-    __device__ void put(int i, bool, bool mine, int at) const {
-      if (mine) list[at] = i;
-      else if (i < keep) sources[i] = i;
-    }
-  };
-  struct Late {
-    int32_t *sources, *list;
-    int keep;
-    __device__ bool operator()(int i, bool stays) const { return i >= keep && stays; }
-    __device__ void put(int i, bool, bool mine, int at) const {
-      if (mine) sources[list[at]] = i;
-    }
-  };
-  int32_t *list = a.free_places + static_cast<size_t>(unit) * a.keep;
-  sweep(Free{sources, list, a.keep});
-  __syncthreads();
-  __threadfence_block();
-  sweep(Late{sources, list, a.keep});
+// The row of an entry in the pools; false: it is in no page.
+__device__ __forceinline__ bool pool_row(const WeightEvictArgs &a, const int32_t *table, int kvh, int entry, unsigned &row) {
+  const int pg = page_of(a.pages, entry);
+  const unsigned no = static_cast<unsigned>(table[pg]), head_rows = static_cast<unsigned>(a.pages.page_size);
+  row = (no * static_cast<unsigned>(a.n_kv_heads) + kvh) * head_rows + static_cast<unsigned>(entry - pg * a.pages.page_size);
+  return no < static_cast<unsigned>(a.pages.n_pages);
 }
 
-constexpr int kMovePlaces = 64, kMoveBlock = 256;
+// Weight and position of a place, from its source.
+__device__ __forceinline__ void put_numbers(const WeightEvictArgs &a, int unit, int place, int source) {
+  const long long in = static_cast<long long>(unit) * a.stride, out = static_cast<long long>(unit) * a.to_stride + place;
+  const float w = source >= 0 ? a.weights[in + source] : 0.f;
+  const int p = source < 0 ? -1 : a.positions ? a.positions[in + source] : source;
+  if (a.weights_to) a.weights_to[out] = w;
+  if (a.positions_to) a.positions_to[out] = p;
+}
 
-// Places blockIdx.x * 64 .. of a unit; kChunks: 16-byte chunks of a row.
-template <int kChunks>
-__global__ __launch_bounds__(kMoveBlock) void move_kernel(const WeightEvictArgs a) {
-  __shared__ unsigned from_row[kMovePlaces], to_row[kMovePlaces];
-  const int per_unit = (a.keep + kMovePlaces - 1) / kMovePlaces;
-  const int unit = static_cast<int>(blockIdx.x / per_unit), place0 = (static_cast<int>(blockIdx.x) - unit * per_unit) * kMovePlaces;
-  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
-  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
-  const unsigned head_rows = static_cast<unsigned>(a.pages.page_size), page_rows = head_rows * static_cast<unsigned>(a.n_kv_heads);
-  __shared__ int n_moves;
-  if (threadIdx.x < 64) {
-    const int lane = threadIdx.x, place = place0 + lane;
-    int source = -1;
-    bool moves = false;
-    unsigned from = 0, to = 0;
-    if (place < a.keep) {
-      source = a.sources[static_cast<size_t>(unit) * a.keep + place];
-      const long long in = static_cast<long long>(unit) * a.stride, out = static_cast<long long>(unit) * a.to_stride + place;
-      const float w = source >= 0 ? a.weights[in + source] : 0.f;
-      const int p = source < 0 ? -1 : a.positions ? a.positions[in + source] : source;
-      if (a.weights_to) a.weights_to[out] = w;
-      if (a.positions_to) a.positions_to[out] = p;
-      if (source > place) {
-        const int pf = page_of(a.pages, source), pt = page_of(a.pages, place);
-        const unsigned nf = static_cast<unsigned>(table[pf]), nt = static_cast<unsigned>(table[pt]);
-        moves = nf < static_cast<unsigned>(a.pages.n_pages) && nt < static_cast<unsigned>(a.pages.n_pages);
-        from = nf * page_rows + kvh * head_rows + static_cast<unsigned>(source - pf * a.pages.page_size);
-        to = nt * page_rows + kvh * head_rows + static_cast<unsigned>(place - pt * a.pages.page_size);
-      }
-    }
-    const unsigned long long m = __ballot(moves);
-    if (moves) {
-      const int at = __popcll(m & ((1ull << lane) - 1));
-      from_row[at] = from;
-      to_row[at] = to;
-    }
-    if (lane == 0) n_moves = __popcll(m);
-  }
-  __syncthreads();
-  constexpr int kRows = kMoveBlock / kChunks;      // rows of the block's turn, of K and of V
-  const int n = n_moves, chunk = threadIdx.x % kChunks;
-  constexpr int kTurns = kMovePlaces / kRows < 4 ? kMovePlaces / kRows : 4;
+// n rows from_row -> to_row (of the pools, LDS; the same number twice: none is moved), by kThreads threads in groups of kChunks, kTurns of a group's rows on their way together.
+template <int kChunks, int kThreads, int kTurns>
+__device__ __forceinline__ void move_rows(const WeightEvictArgs &a, const unsigned *from_row, const unsigned *to_row, int n) {
+  constexpr int kRows = kThreads / kChunks;
+  const int chunk = threadIdx.x % kChunks;
   for (int m0 = threadIdx.x / kChunks; m0 < n; m0 += kRows * kTurns) {
     u32x4_t k[kTurns], v[kTurns];
 #pragma unroll
@@ -222,12 +60,278 @@ __global__ __launch_bounds__(kMoveBlock) void move_kernel(const WeightEvictArgs 
     }
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
-      if (m0 + u * kRows >= n) continue;
+      if (m0 + u * kRows >= n || from_row[m0 + u * kRows] == to_row[m0 + u * kRows]) continue;
       const size_t at = static_cast<size_t>(to_row[m0 + u * kRows]) * (kChunks * 16) + chunk * 16;
       *reinterpret_cast<u32x4_t *>(static_cast<char *>(a.k_pages) + at) = k[u];
       *reinterpret_cast<u32x4_t *>(static_cast<char *>(a.v_pages) + at) = v[u];
     }
   }
+}
+
+// kRegs: keys that a lane keeps (of a stretch of 64 kRegs entries), 0: they are made anew from memory for every look.  kChunks: the block moves the rows
+// too, of that many 16-byte chunks (at most kOwnMoves of them); 0: the next kernel does.
+template <int kRegs, int kChunks>
+__global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictArgs a) {
+  __shared__ int bins[kBins], waves_i[2][kSelectWaves];
+  __shared__ unsigned waves_u[2][kSelectWaves];
+  __shared__ int picked[3];                        // part of the range, keys of it, keys beyond it
+  constexpr int kOwn = kChunks > 0 ? kOwnMoves : 1;
+  __shared__ unsigned from_row[kOwn], to_row[kOwn];
+  __shared__ int free_place[kOwn];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int unit = static_cast<int>(blockIdx.x), seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  const int len = a.lengths ? min(max(a.lengths[seq], 0), a.length) : a.length;
+  int32_t *sources = a.sources + static_cast<size_t>(unit) * a.keep;
+  if (len <= a.keep) {
+    for (int i = threadIdx.x; i < a.keep; i += kSelectBlock) {
+      sources[i] = i < len ? i : -1;
+      if constexpr (kChunks > 0) put_numbers(a, unit, i, i < len ? i : -1);
+    }
+    return;
+  }
+  const float *weights = a.weights + static_cast<long long>(unit) * a.stride;
+  const int32_t *positions = a.positions ? a.positions + static_cast<long long>(unit) * a.stride : nullptr;
+  const int looks = kRegs > 0 ? kRegs : (len + kSelectBlock - 1) / kSelectBlock;
+  auto entry_of = [&](int x) __attribute__((always_inline)) { return (wave * looks + x) * 64 + lane; };
+
+  // numbers over all waves; the two rooms take turns, so that one barrier does
+  int turn = 0;
+  auto before_wave = [&](int mine, int &all) __attribute__((always_inline)) {
+    if (lane == 0) waves_i[turn][wave] = mine;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) {
+      const int n = waves_i[turn][w];
+      before += w < wave ? n : 0;
+      all += n;
+    }
+    turn ^= 1;
+    return before;
+  };
+
+  // positions from `recent_from` on are the newest
+  constexpr int kHeld = kRegs > 0 ? kRegs : 1;
+  unsigned held[kHeld];
+  int place[kHeld];
+  int newest = len - 1;
+  if (positions) {
+    newest = INT_MIN;
+    if constexpr (kRegs > 0) {
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) place[x] = entry_of(x) < len ? positions[entry_of(x)] : INT_MIN;
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) newest = max(newest, place[x]);
+    } else {
+      for (int x = 0; x < looks; ++x) newest = max(newest, entry_of(x) < len ? positions[entry_of(x)] : INT_MIN);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) newest = max(newest, __shfl_xor(newest, o));
+    if (lane == 0) waves_i[turn][wave] = newest;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) newest = max(newest, waves_i[turn][w]);
+    turn ^= 1;
+  }
+  const long long recent_from = static_cast<long long>(newest) - a.n_recent + 1;
+  auto key_of = [&](int i, int p, float w) __attribute__((always_inline)) {
+    return i >= len ? 0u : p >= recent_from || p < a.n_first ? 0xFFFFFFFFu : weight_key(w);
+  };
+  if constexpr (kRegs > 0) {
+    float w[kHeld];
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) w[x] = entry_of(x) < len ? weights[entry_of(x)] : 0.f;
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) held[x] = key_of(entry_of(x), positions ? place[x] : entry_of(x), w[x]);
+  }
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (kRegs > 0) {
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) f(entry_of(x), held[x]);
+    } else {
+      for (int x = 0; x < looks; ++x) {
+        const int i = entry_of(x), j = min(i, len - 1);
+        f(i, key_of(i, positions ? positions[j] : j, weights[j]));
+      }
+    }
+  };
+
+  // the `keep`-th largest key: it is among those from low to high, of which `want` are to stay
+  unsigned low = 0xFFFFFFFFu, high = 0u;
+  each([&](int i, unsigned k) __attribute__((always_inline)) {
+    low = i < len ? min(low, k) : low;
+    high = max(high, k);
+  });
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    low = min(low, static_cast<unsigned>(__shfl_xor(static_cast<int>(low), o)));
+    high = max(high, static_cast<unsigned>(__shfl_xor(static_cast<int>(high), o)));
+  }
+  if (lane == 0) {
+    waves_u[0][wave] = low;
+    waves_u[1][wave] = high;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelectWaves; ++w) {
+    low = min(low, waves_u[0][w]);
+    high = max(high, waves_u[1][w]);
+  }
+  int want = a.keep, have = len;                   // of the keys in the range
+  while (low < high && want < have) {
+    const int bits = 32 - __clz(static_cast<int>(high - low)), shift = bits > 10 ? bits - 10 : 0;
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+      const bool in = i < len && k >= low && k <= high;
+      const unsigned bin = in ? (k - low) >> shift : kBins;
+      // (many equal weights: those of the first lane's part in one addition)
+      const unsigned long long m = __ballot(in);
+      if (m == 0) return;
+      const unsigned one = __shfl(static_cast<int>(bin), __ffsll(static_cast<long long>(m)) - 1);
+      const unsigned long long same = __ballot(bin == one);
+      if (in && bin != one) atomicAdd(&bins[bin], 1);
+      if (lane == 0) atomicAdd(&bins[one], __popcll(same));
+    });
+    __syncthreads();
+    // parts from the top: thread t has part kBins - 1 - t
+    const int part = kBins - 1 - static_cast<int>(threadIdx.x), mine = bins[part];
+    int run = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(run, o);
+      run += lane >= o ? y : 0;
+    }
+    int all;
+    const int before = before_wave(__shfl(run, 63), all), above = before + run - mine;
+    if (above < want && above + mine >= want) {
+      picked[0] = part;
+      picked[1] = mine;
+      picked[2] = above;
+    }
+    __syncthreads();
+    const unsigned from = low + (static_cast<unsigned>(picked[0]) << shift);
+    have = picked[1];
+    want -= picked[2];
+    const unsigned to = from + ((1u << shift) - 1);
+    high = to < from || to > high ? high : to;
+    low = from;
+    __syncthreads();
+  }
+  // keys beyond the range stay, and of those in it (all of them, or equal ones) `want`, the lowest
+  int mine = 0, all;
+  each([&](int i, unsigned k) __attribute__((always_inline)) { mine += __popcll(__ballot(i < len && k >= low && k <= high)); });
+  int met = before_wave(mine, all);
+  const unsigned long long below = (1ull << lane) - 1;
+  unsigned kept = 0;                               // bit x: this lane's entry x stays
+  int n_free = 0, n_late = 0;
+  auto stays_of = [&](int i, unsigned k) __attribute__((always_inline)) {
+    const bool in = i < len && k >= low && k <= high;
+    const unsigned long long m = __ballot(in);
+    const bool stays = i < len && (k > high || (in && met + __popcll(m & below) < want));
+    met += __popcll(m);
+    return stays;
+  };
+  const int met_0 = met;
+  {
+    int x = 0;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+      const bool stays = stays_of(i, k);
+      if constexpr (kRegs > 0) kept |= stays ? 1u << x : 0u;
+      ++x;
+      n_free += __popcll(__ballot(i < a.keep && !stays));
+      n_late += __popcll(__ballot(i >= a.keep && stays));
+    });
+  }
+  int at_free = before_wave(n_free, all), at_late = before_wave(n_late, all);
+  int32_t *list = kChunks > 0 ? free_place : a.free_places + static_cast<size_t>(unit) * a.keep;
+  auto places = [&](auto f) __attribute__((always_inline)) {
+    met = met_0;
+    int x = 0;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+      bool stays;
+      if constexpr (kRegs > 0) stays = kept >> x & 1u;
+      else stays = stays_of(i, k);
+      ++x;
+      f(i, stays);
+    });
+  };
+  places([&](int i, bool stays) __attribute__((always_inline)) {
+    const bool free = i < a.keep && !stays;
+    const unsigned long long m = __ballot(free);
+    if (free) list[at_free + __popcll(m & below)] = i;
+    else if (i < a.keep) sources[i] = i;
+    at_free += __popcll(m);
+    if constexpr (kChunks > 0)
+      if (i < a.keep && stays) put_numbers(a, unit, i, i);
+  });
+  __threadfence_block();
+  __syncthreads();
+  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+  places([&](int i, bool stays) __attribute__((always_inline)) {
+    const bool late = i >= a.keep && stays;
+    const unsigned long long m = __ballot(late);
+    if (late) {
+      const int n = at_late + __popcll(m & below), to = list[n];
+      sources[to] = i;
+      if constexpr (kChunks > 0) {
+        put_numbers(a, unit, to, i);
+        unsigned rf, rt;
+        const bool both = pool_row(a, table, kvh, i, rf) & pool_row(a, table, kvh, to, rt);
+        from_row[n] = both ? rf : 0u;
+        to_row[n] = both ? rt : 0u;
+      }
+    }
+    at_late += __popcll(m);
+  });
+  if constexpr (kChunks > 0) {
+    __syncthreads();
+    move_rows<kChunks, kSelectBlock, 1>(a, from_row, to_row, all);
+  }
+}
+
+constexpr int kMovePlaces = 64, kMoveBlock = 256;
+
+// Places blockIdx.x * 64 .. of a unit; kChunks: 16-byte chunks of a row.
+template <int kChunks>
+__global__ __launch_bounds__(kMoveBlock) void move_kernel(const WeightEvictArgs a) {
+  __shared__ unsigned from_row[kMovePlaces], to_row[kMovePlaces];
+  __shared__ int n_moves;
+  const int per_unit = (a.keep + kMovePlaces - 1) / kMovePlaces;
+  const int unit = static_cast<int>(blockIdx.x / per_unit), place0 = (static_cast<int>(blockIdx.x) - unit * per_unit) * kMovePlaces;
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
+  if (threadIdx.x < 64) {
+    const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+    const int lane = threadIdx.x, place = place0 + lane;
+    bool moves = false;
+    unsigned from = 0, to = 0;
+    if (place < a.keep) {
+      const int source = a.sources[static_cast<size_t>(unit) * a.keep + place];
+      put_numbers(a, unit, place, source);
+      if (source > place) moves = pool_row(a, table, kvh, source, from) & pool_row(a, table, kvh, place, to);
+    }
+    const unsigned long long m = __ballot(moves);
+    if (moves) {
+      const int at = __popcll(m & ((1ull << lane) - 1));
+      from_row[at] = from;
+      to_row[at] = to;
+    }
+    if (lane == 0) n_moves = __popcll(m);
+  }
+  __syncthreads();
+  constexpr int kTurns = kMovePlaces / (kMoveBlock / kChunks);
+  move_rows<kChunks, kMoveBlock, kTurns < 4 ? kTurns : 4>(a, from_row, to_row, n_moves);
+}
+
+template <int kChunks>
+void launch_select(const WeightEvictArgs &a, const dim3 &grid, hipStream_t stream) {
+  const dim3 block(kSelectBlock);
+  const int regs = (a.length + kSelectBlock - 1) / kSelectBlock;
+  if (regs <= 3) hipLaunchKernelGGL((select_kernel<3, kChunks>), grid, block, 0, stream, a);
+  else if (regs <= 8) hipLaunchKernelGGL((select_kernel<8, kChunks>), grid, block, 0, stream, a);
+  else if (regs <= 32) hipLaunchKernelGGL((select_kernel<32, kChunks>), grid, block, 0, stream, a);
+  else if constexpr (kChunks == 0) hipLaunchKernelGGL((select_kernel<0, 0>), grid, block, 0, stream, a);
 }
 
 }  // namespace
@@ -238,19 +342,24 @@ size_t weight_evict_workspace(const WeightEvictArgs &a) {
 
 hipError_t launch_weight_evict(WeightEvictArgs a, hipStream_t stream) {
   const long long units = static_cast<long long>(a.n_seqs) * a.n_kv_heads, blocks = units * ((a.keep + kMovePlaces - 1) / kMovePlaces);
-  if (units > (1 << 22) || blocks > (1ll << 24) - 1) return hipErrorInvalidValue;
-  const dim3 grid(static_cast<unsigned>(units)), block(kSelectBlock);
-  const int regs = (a.length + kSelectBlock - 1) / kSelectBlock;
-  if (regs <= 4) hipLaunchKernelGGL((select_kernel<4>), grid, block, 0, stream, a);
-  else if (regs <= 32) hipLaunchKernelGGL((select_kernel<32>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((select_kernel<0>), grid, block, 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (units >= (1 << 22) || blocks > (1ll << 24) - 1) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(units));
   const int chunks = a.head_dim * (a.dtype == LAZYEV_DTYPE_FP32 ? 4 : 2) / 16;
-  const dim3 moves(static_cast<unsigned>(blocks));
-  if (chunks == 8) hipLaunchKernelGGL((move_kernel<8>), moves, dim3(kMoveBlock), 0, stream, a);
-  else if (chunks == 16) hipLaunchKernelGGL((move_kernel<16>), moves, dim3(kMoveBlock), 0, stream, a);
-  else hipLaunchKernelGGL((move_kernel<32>), moves, dim3(kMoveBlock), 0, stream, a);
+  const int moves = a.length - a.keep < a.keep ? a.length - a.keep : a.keep;   // of a unit, at most
+  // (a block that keeps no keys makes them anew, from numbers that its moves may be changing)
+  if (moves <= kOwnMoves && a.length <= 32 * kSelectBlock) {
+    if (chunks == 8) launch_select<8>(a, grid, stream);
+    else if (chunks == 16) launch_select<16>(a, grid, stream);
+    else launch_select<32>(a, grid, stream);
+    return hipGetLastError();
+  }
+  launch_select<0>(a, grid, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 all(static_cast<unsigned>(blocks));
+  if (chunks == 8) hipLaunchKernelGGL((move_kernel<8>), all, dim3(kMoveBlock), 0, stream, a);
+  else if (chunks == 16) hipLaunchKernelGGL((move_kernel<16>), all, dim3(kMoveBlock), 0, stream, a);
+  else hipLaunchKernelGGL((move_kernel<32>), all, dim3(kMoveBlock), 0, stream, a);
   return hipGetLastError();
 }
 
