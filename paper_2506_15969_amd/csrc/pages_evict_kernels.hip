@@ -157,43 +157,71 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
     }
   };
 
-  // the `keep`-th largest key: it is among those from low to high, of which `want` are to stay
-  unsigned low = 0xFFFFFFFFu, high = 0u;
-  each([&](int i, unsigned k) __attribute__((always_inline)) {
-    low = i < len ? min(low, k) : low;
-    high = max(high, k);
-  });
+  // the `keep`-th largest key: it is among those from low to high, of which `want` are to stay.  (The range is that of the keys in it: equal
+  // keys are found to be so at once)
+  unsigned low = 0u, high = 0xFFFFFFFFu;
+  auto tighten = [&]() __attribute__((always_inline)) {
+    unsigned least = 0xFFFFFFFFu, most = 0u;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+      const bool in = i < len && k >= low && k <= high;
+      least = min(least, in ? k : 0xFFFFFFFFu);
+      most = max(most, in ? k : 0u);
+    });
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    low = min(low, static_cast<unsigned>(__shfl_xor(static_cast<int>(low), o)));
-    high = max(high, static_cast<unsigned>(__shfl_xor(static_cast<int>(high), o)));
-  }
-  if (lane == 0) {
-    waves_u[0][wave] = low;
-    waves_u[1][wave] = high;
+    for (int o = 1; o < 64; o <<= 1) {
+      least = min(least, static_cast<unsigned>(__shfl_xor(static_cast<int>(least), o)));
+      most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), o)));
+    }
+    if (lane == 0) {
+      waves_u[0][wave] = least;
+      waves_u[1][wave] = most;
+    }
+    __syncthreads();
+    low = 0xFFFFFFFFu;
+    high = 0u;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) {
+      low = min(low, waves_u[0][w]);
+      high = max(high, waves_u[1][w]);
+    }
+  };
+  // Many weights may be alike: one such key, the most frequent of 64, is counted in registers, as additions to one place go one after the other.
+  if (wave == 0) {
+    unsigned k = 0;
+    if constexpr (kRegs > 0) k = held[kRegs / 2];
+    else k = key_of(lane, positions ? positions[lane] : lane, weights[lane]);
+    int times = 0;
+#pragma unroll 8
+    for (int y = 0; y < 64; ++y) times += static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(k), y)) == k ? 1 : 0;
+    int best = times << 6 | lane;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) best = max(best, __shfl_xor(best, o));
+    const unsigned mode = static_cast<unsigned>(__shfl(static_cast<int>(k), best & 63));
+    if (lane == 0) picked[0] = best >> 6 > 4 ? static_cast<int>(mode) : 0;
   }
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) {
-    low = min(low, waves_u[0][w]);
-    high = max(high, waves_u[1][w]);
-  }
+  const unsigned common = static_cast<unsigned>(picked[0]);
+  __syncthreads();
   int want = a.keep, have = len;                   // of the keys in the range
-  while (low < high && want < have) {
+  int had = 0;
+  while (true) {
+    if (have > had / 4) tighten();                 // (the first time, and where a part has much of the range: many equal ones)
+    had = have;
+    if (low == high || want == have) break;        // (uniform)
     const int bits = 32 - __clz(static_cast<int>(high - low)), shift = bits > 10 ? bits - 10 : 0;
     bins[threadIdx.x] = 0;
     __syncthreads();
-    each([&](int i, unsigned k) __attribute__((always_inline)) {
-      const bool in = i < len && k >= low && k <= high;
-      const unsigned bin = in ? (k - low) >> shift : kBins;
-      // (many equal weights: those of the first lane's part in one addition)
-      const unsigned long long m = __ballot(in);
-      if (m == 0) return;
-      const unsigned one = __shfl(static_cast<int>(bin), __ffsll(static_cast<long long>(m)) - 1);
-      const unsigned long long same = __ballot(bin == one);
-      if (in && bin != one) atomicAdd(&bins[bin], 1);
-      if (lane == 0) atomicAdd(&bins[one], __popcll(same));
+    int alike = 0;
+    each([&](int, unsigned k) __attribute__((always_inline)) {
+      if (k - low > high - low) return;            // (no entry: below all keys)
+      if (k == common) ++alike;
+      else atomicAdd(&bins[(k - low) >> shift], 1);
     });
+    if (common - low <= high - low) {              // (uniform)
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) alike += __shfl_xor(alike, o);
+      if (lane == 0) atomicAdd(&bins[(common - low) >> shift], alike);
+    }
     __syncthreads();
     // parts from the top: thread t has part kBins - 1 - t
     const int part = kBins - 1 - static_cast<int>(threadIdx.x), mine = bins[part];
