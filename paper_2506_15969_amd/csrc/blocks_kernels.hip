@@ -179,11 +179,94 @@ __device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
   return w;
 }
 
-// A wave has 32 blocks of a unit (x: the unit and 128 blocks of it) and goes over the tokens of its share (y) of the launch's, 32 / kPad of
-// them at a time; a token's group of up to 64 heads comes in passes of 32.
+// Scores of 32 rows (a token's heads filled up to kPad, 32 / kPad tokens) and 32 blocks: put(token, score of block c), for this lane's tokens.
+// A group of more than 32 heads comes in passes; operand(pass, j, pos, neg): chunk 2 j + h of row c.
+template <typename T, int D, int kPad, typename Q, typename P>
+__device__ __forceinline__ void tile_scores(const ChooseArgs &a, const u32x4_t *lo, const u32x4_t *hi, Q operand, P put) {
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
+  const int h = threadIdx.x >> 5 & 1;
+  float top = -INFINITY, out[16];
+  for (int pass = 0; pass < (kPad == 32 ? (a.group + 31) / 32 : 1); ++pass) {
+    f32x16_t s;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) {
+      u32x4_t pos, neg;
+      operand(pass, j, pos, neg);
+      if constexpr (kF32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[j][e]), s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[j][e]), s, 0, 0, 0);
+        }
+      } else {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi[j]), s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo[j]), s, 0, 0, 0);
+      }
+    }
+    // rows 8 i + 4 h + j in s[4 i + j]: the maxima of kPad rows next to one another
+    if constexpr (kPad == 1) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) out[x] = s[x];
+    } else if constexpr (kPad == 2) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) out[x] = upper(s[2 * x], s[2 * x + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        out[i] = upper(upper(s[4 * i], s[4 * i + 1]), upper(s[4 * i + 2], s[4 * i + 3]));
+        if constexpr (kPad > 4) out[i] = join_step<32>(out[i], upper);
+      }
+      if constexpr (kPad >= 16) {
+        out[0] = upper(out[0], out[1]);
+        out[1] = upper(out[2], out[3]);
+      }
+      if constexpr (kPad == 32) {
+        top = upper(top, upper(out[0], out[1]));
+        out[0] = top;
+      }
+    }
+  }
+  if constexpr (kPad == 1) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) put(8 * (x / 4) + 4 * h + x % 4, out[x]);
+  } else if constexpr (kPad == 2) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) put(4 * (x / 2) + 2 * h + x % 2, out[x]);
+  } else if constexpr (kPad == 4) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) put(2 * x + h, out[x]);
+  } else if (h == 0) {
+#pragma unroll
+    for (int x = 0; x < kTokens; ++x) put(x, out[x]);
+  }
+}
+
+// Bounds of block b as an operand; -> its largest one in size.
+template <typename T, int D>
+__device__ __forceinline__ void load_bounds(const ChooseArgs &a, int unit, int b, u32x4_t *lo, u32x4_t *hi) {
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32;
+  const char *from = static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + (threadIdx.x >> 5 & 1) * 16;
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+}
+template <typename T, int D>
+__device__ __forceinline__ float peak_of(const u32x4_t *lo, const u32x4_t *hi) {
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32;
+  float m = 0.f;
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) m = upper(upper(m, largest_of<sizeof(T) == 4>(lo[j])), largest_of<sizeof(T) == 4>(hi[j]));
+  return join_step<32>(m, upper);
+}
+
+// Scores for another kernel: a wave has 32 blocks of a unit (x: the unit and 128 blocks of it) and goes over the tokens of its share (y) of the
+// launch's, 32 / kPad of them at a time.
 template <typename T, int D, int kPad>
 __global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
-  constexpr bool kF32 = sizeof(T) == 4;
   constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = lane & 31, h = lane >> 5;
@@ -191,88 +274,26 @@ __global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
   const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
   const int b0 = (static_cast<int>(blockIdx.x) - unit * across) * 128 + wave * 32;
   if (b0 >= a.scored) return;
-  const int b = min(b0 + c, a.scored - 1);
   u32x4_t lo[kOps], hi[kOps];
-  const char *from = static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + h * 16;
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+  load_bounds<T, D>(a, unit, min(b0 + c, a.scored - 1), lo, hi);
   if (blockIdx.y == 0) {
-    float m = 0.f;
-#pragma unroll
-    for (int j = 0; j < kOps; ++j) m = upper(upper(m, largest_of<kF32>(lo[j])), largest_of<kF32>(hi[j]));
-    m = upper(m, __shfl_xor(m, 32));
+    const float m = peak_of<T, D>(lo, hi);
     if (h == 0 && b0 + c < a.scored) a.peak[static_cast<size_t>(unit) * a.scored + b0 + c] = m;
   }
   const int tiles = (a.tokens + kTokens - 1) / kTokens;
   const T *q = static_cast<const T *>(a.q) + static_cast<size_t>(kvh) * a.group * D + h * (16 / sizeof(T));
   for (int tile = static_cast<int>(blockIdx.y); tile < tiles; tile += static_cast<int>(gridDim.y)) {
-    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};        // (passes of 32 heads)
-    float out[16];
-    for (int pass = 0; pass < (kPad == 32 ? (a.group + 31) / 32 : 1); ++pass) {
-      const int token = a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1), head = min(pass * 32 + c % kPad, a.group - 1);
-      const T *row = q + ((static_cast<size_t>(seq) * a.n_tokens + token) * a.n_q_heads + head) * D;
-      f32x16_t s;
-#pragma unroll
-      for (int x = 0; x < 16; ++x) s[x] = 0.f;
-#pragma unroll
-      for (int j = 0; j < kOps; ++j) {
-        u32x4_t pos, neg;
-        by_sign<kF32>(load_chunk(row + j * (32 / sizeof(T)), a.wide), pos, neg);
-        if constexpr (kF32) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[j][e]), s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[j][e]), s, 0, 0, 0);
-          }
-        } else {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi[j]), s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo[j]), s, 0, 0, 0);
-        }
-      }
-      // rows 8 i + 4 h + j in s[4 i + j]: the maxima of kPad rows next to one another
-      if constexpr (kPad == 1) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) out[x] = s[x];
-      } else if constexpr (kPad == 2) {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) out[x] = upper(s[2 * x], s[2 * x + 1]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float m = upper(upper(s[4 * i], s[4 * i + 1]), upper(s[4 * i + 2], s[4 * i + 3]));
-          if constexpr (kPad > 4) m = upper(m, __shfl_xor(m, 32));
-          out[i] = m;
-        }
-        if constexpr (kPad >= 16) {
-          out[0] = upper(out[0], out[1]);
-          out[1] = upper(out[2], out[3]);
-        }
-        if constexpr (kPad == 32) {
-          top[0] = upper(top[0], upper(out[0], out[1]));
-          out[0] = top[0];
-        }
-      }
-    }
-    auto store = [&](int token, float x) __attribute__((always_inline)) {
-      const int t = tile * kTokens + token;
-      if (t < a.tokens && b0 + c < a.scored)
-        a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b0 + c] = x;
-    };
-    if constexpr (kPad == 1) {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) store(8 * (x / 4) + 4 * h + x % 4, out[x]);
-    } else if constexpr (kPad == 2) {
-#pragma unroll
-      for (int x = 0; x < 8; ++x) store(4 * (x / 2) + 2 * h + x % 2, out[x]);
-    } else if constexpr (kPad == 4) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) store(2 * x + h, out[x]);
-    } else if (h == 0) {
-#pragma unroll
-      for (int x = 0; x < kTokens; ++x) store(x, out[x]);
-    }
+    const int token = a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1);
+    tile_scores<T, D, kPad>(
+        a, lo, hi,
+        [&](int pass, int j, u32x4_t &pos, u32x4_t &neg) __attribute__((always_inline)) {
+          const T *row = q + ((static_cast<size_t>(seq) * a.n_tokens + token) * a.n_q_heads + min(pass * 32 + c % kPad, a.group - 1)) * D;
+          by_sign<sizeof(T) == 4>(load_chunk(row + j * (32 / sizeof(T)), a.wide), pos, neg);
+        },
+        [&](int t, float x) __attribute__((always_inline)) {
+          t += tile * kTokens;
+          if (t < a.tokens && b0 + c < a.scored) a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b0 + c] = x;
+        });
   }
 }
 
@@ -289,7 +310,26 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
   return x != x ? ~0ull : u ^ (static_cast<unsigned long long>(static_cast<long long>(u) >> 63) | 1ull << 63);
 }
 
-constexpr int kAgain = 512;             // blocks between the borders whose exact scores LDS holds
+// What a row's waves share; kAgain: blocks between the borders whose exact scores it holds.
+template <int kWaves, int kRegs, int kAgain>
+struct Room {
+  int i[2][kWaves];
+  unsigned u[2][kWaves];
+  float f[2][kWaves];
+  double exact[kAgain];
+  int again[kAgain], look_count[kRegs > 0 ? kRegs * kWaves : 1];
+};
+// What the waves of a row have written is there for all of them.
+template <int kWaves>
+__device__ __forceinline__ void together() {
+  if constexpr (kWaves > 1) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
 
 // x of all waves, by `join`; LDS of one number a wave, of which two take turns.
 template <int kWaves, typename V, typename F>
@@ -305,38 +345,34 @@ __device__ __forceinline__ V over_waves(V x, V (&room)[2][kWaves], int &turn, F 
   return x;
 }
 
-// One block of kWaves waves for a token and KV head.  Its candidates' scores stay in registers, kRegs for a thread (candidate 64 (x kWaves + wave) + lane is x
-// of a lane); 0: there are more of them, and they are read anew for every look.
+// The choice of a token and KV head (row: of the launch's), by kWaves waves.  Its candidates' scores stay in registers, kRegs for a thread (candidate
+// 64 (x kWaves + wave) + lane is x of a lane); 0: there are more of them, and they are read anew for every look.
 // T is not needed to its last bit: an interval of T no wider than E does, so the bits of its order are settled from the first one in which candidates
 // differ to about the fourteenth behind, by counts of the candidates from a number on.
-template <typename T, int D, int kWaves, int kRegs>
-__global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a) {
+template <typename T, int D, int kWaves, int kRegs, int kAgain, typename F>
+__device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Room<kWaves, kRegs, kAgain> &room, F numbers) {
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int kBlock = 64 * kWaves, C = D * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
   constexpr int kLooks = kRegs * kWaves, kHeld = kRegs > 0 ? kRegs : 1;
-  __shared__ int room_i[2][kWaves];
-  __shared__ unsigned room_u[2][kWaves];
-  __shared__ float room_f[2][kWaves];
-  __shared__ double exact[kAgain];
-  __shared__ int again[kAgain], look_count[kLooks > 0 ? kLooks : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const unsigned row = blockIdx.x, its = row / a.n_kv_heads;          // (sequence, token of the launch, KV head)
+  const int lane = threadIdx.x & 63, wave = kWaves > 1 ? threadIdx.x >> 6 : 0, thread = wave * 64 + lane;
+  const unsigned its = row / a.n_kv_heads;         // (sequence, token of the launch)
   const int kvh = static_cast<int>(row - its * a.n_kv_heads), seq = static_cast<int>(its / a.tokens), t = static_cast<int>(its - seq * a.tokens);
   const long long token = static_cast<long long>(seq) * a.n_tokens + a.token0 + t;
   int32_t *to = a.chosen + (token * a.n_kv_heads + kvh) * a.n_chosen;
   const int seen = a.visible ? min(max(a.visible[token], 0), a.length) : a.length;
   const int nb = (seen + a.block - 1) / a.block;
   if (nb <= a.n_chosen) {
-    for (int i = threadIdx.x; i < a.n_chosen; i += kBlock) to[i] = i < nb ? i : -1;
+    for (int i = thread; i < a.n_chosen; i += kBlock) to[i] = i < nb ? i : -1;
     return;
   }
   // candidates are the blocks first .. first + n - 1, of which `want` go
   const int n = nb - a.n_last - a.n_first, want = a.n_chosen - a.n_last - a.n_first;
   const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + kvh;
-  const float *score = a.score + static_cast<size_t>(row) * a.scored + a.n_first, *peak = a.peak + unit * a.scored + a.n_first;
+  const auto score = [&](int i) __attribute__((always_inline)) { return numbers.score(i + a.n_first); };
+  const auto peak = [&](int i) __attribute__((always_inline)) { return numbers.peak(i + a.n_first); };
   const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + static_cast<long long>(kvh) * a.group) * D;
-  for (int i = threadIdx.x; i < a.n_first; i += kBlock) to[i] = i;
-  for (int i = threadIdx.x; i < a.n_last; i += kBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
+  for (int i = thread; i < a.n_first; i += kBlock) to[i] = i;
+  for (int i = thread; i < a.n_last; i += kBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
   if (want == 0) return;
 
   // the scores, their range, and how far one may be off
@@ -348,7 +384,7 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
 #pragma unroll
       for (int x = 0; x < kRegs; ++x) f(x, held[x]);
     } else {
-      for (int x = 0; x < looks; ++x) f(x, at_look(x) < n ? order_of(score[min(at_look(x), n - 1)]) : 0u);
+      for (int x = 0; x < looks; ++x) f(x, at_look(x) < n ? order_of(score(min(at_look(x), n - 1))) : 0u);
     }
   };
   float most = 0.f, size = 0.f;                    // largest bound; largest |q|_1
@@ -360,8 +396,8 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
     for (int x = 0; x < kRegs; ++x) {
       s[x] = p[x] = 0.f;
       if (at_look(x) < n) {
-        s[x] = score[at_look(x)];
-        p[x] = peak[at_look(x)];
+        s[x] = score(at_look(x));
+        p[x] = peak(at_look(x));
       }
     }
 #pragma unroll
@@ -374,16 +410,16 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
       least = min(least, is ? held[x] : 0xFFFFFFFFu);
     }
   } else {
-    for (int i = threadIdx.x; i < n; i += kBlock) {
-      const float s = score[i];
-      most = upper(most, peak[i]);
+    for (int i = thread; i < n; i += kBlock) {
+      const float s = score(i);
+      most = upper(most, peak(i));
       odd |= !(fabsf(s) <= FLT_MAX);
       top = max(top, order_of(s));
       least = min(least, order_of(s));
     }
   }
   for (int g0 = 0; g0 < a.group; g0 += kBlock / C) {
-    const int g = min(g0 + static_cast<int>(threadIdx.x) / C, a.group - 1);
+    const int g = min(g0 + thread / C, a.group - 1);
     const u32x4_t w = load_chunk(q + g * D + lane % C * kElems, a.wide);
     float s = 0.f;
 #pragma unroll
@@ -398,11 +434,12 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
   top = join_lanes<1, 32>(top, [](unsigned x, unsigned y) { return max(x, y); });
   least = join_lanes<1, 32>(least, [](unsigned x, unsigned y) { return min(x, y); });
   int turn_f = 0, turn_u = 0, turn_i = 0;
-  most = over_waves<kWaves>(most, room_f, turn_f, upper);
-  size = over_waves<kWaves>(size, room_f, turn_f, upper);
-  top = over_waves<kWaves>(top, room_u, turn_u, [](unsigned x, unsigned y) { return max(x, y); });
-  least = over_waves<kWaves>(least, room_u, turn_u, [](unsigned x, unsigned y) { return min(x, y); });
-  odd = __syncthreads_or(odd);
+  most = over_waves<kWaves>(most, room.f, turn_f, upper);
+  size = over_waves<kWaves>(size, room.f, turn_f, upper);
+  top = over_waves<kWaves>(top, room.u, turn_u, [](unsigned x, unsigned y) { return max(x, y); });
+  least = over_waves<kWaves>(least, room.u, turn_u, [](unsigned x, unsigned y) { return min(x, y); });
+  if constexpr (kWaves > 1) odd = __syncthreads_or(odd);
+  else odd = __ballot(odd) != 0;
   // (2^-100: products too small for fp32; none of a row of zeros)
   const float off = size == 0.f && most <= FLT_MAX ? 0.f : size * most * 0x1p-14f + 0x1p-100f;
   const bool all_again = odd || !(size * most < 0x1p120f);
@@ -410,7 +447,7 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
   auto count_from = [&](unsigned cand) __attribute__((always_inline)) {
     int have = 0;
     each([&](int, unsigned k) __attribute__((always_inline)) { have += __popcll(__ballot(k >= cand)); });
-    return over_waves<kWaves>(have, room_i, turn_i, add);
+    return over_waves<kWaves>(have, room.i, turn_i, add);
   };
 
   // the borders: surely taken from `sure` on, surely not below `out`
@@ -439,8 +476,8 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
     n_sure += __popcll(__ballot(is_sure(k)));
     n_between += __popcll(__ballot(between(k)));
   });
-  n_sure = over_waves<kWaves>(n_sure, room_i, turn_i, add);
-  n_between = over_waves<kWaves>(n_between, room_i, turn_i, add);
+  n_sure = over_waves<kWaves>(n_sure, room.i, turn_i, add);
+  n_between = over_waves<kWaves>(n_between, room.i, turn_i, add);
   const int rest = want - n_sure;                  // to take of those between, 0 .. n_between
   const bool ask = (off > 0.f || all_again) && rest > 0 && rest < n_between;
 
@@ -483,7 +520,7 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
     unsigned long long *all = a.exact + static_cast<size_t>(row) * a.scored;
     for (int x = 0; x < looks; ++x) {
       const int i0 = (x * kWaves + wave) * 64, i = i0 + lane;
-      unsigned k = i < n ? order_of(score[min(i, n - 1)]) : 0u;
+      unsigned k = i < n ? order_of(score(min(i, n - 1))) : 0u;
       const unsigned long long mid = __ballot(between(k));
       unsigned long long mine = is_sure(k) ? ~0ull : between(k) ? 1ull : 0ull;
       if (ask)
@@ -494,19 +531,19 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
         }
       if (i < n) all[i] = mine;
     }
-    __syncthreads();
+    together<kWaves>();
     unsigned long long border = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const unsigned long long cand = border | 1ull << bit;
       int have = 0;
       for (int i0 = wave * 64; i0 < n; i0 += kBlock) have += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] >= cand));
-      have = over_waves<kWaves>(have, room_i, turn_i, add);
+      have = over_waves<kWaves>(have, room.i, turn_i, add);
       if (have >= want) border = cand;
       if (have == want) break;
     }
     int above = 0;
     for (int i0 = wave * 64; i0 < n; i0 += kBlock) above += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] > border));
-    above = over_waves<kWaves>(above, room_i, turn_i, add);
+    above = over_waves<kWaves>(above, room.i, turn_i, add);
     if (wave != 0) return;
     int at = a.n_first, met = 0;
     for (int i0 = 0; i0 < n; i0 += 64) {
@@ -533,16 +570,16 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
         }
       } else {
         constexpr int kPer = (kLooks + 63) / 64;
-        __syncthreads();
+        together<kWaves>();
         if (lane == 0)
 #pragma unroll
-          for (int x = 0; x < kRegs; ++x) look_count[x * kWaves + wave] = mine[x];
-        __syncthreads();
+          for (int x = 0; x < kRegs; ++x) room.look_count[x * kWaves + wave] = mine[x];
+        together<kWaves>();
         int part[kPer], sum = 0;
 #pragma unroll
         for (int y = 0; y < kPer; ++y) {
           part[y] = sum;
-          sum += lane * kPer + y < kLooks ? look_count[lane * kPer + y] : 0;
+          sum += lane * kPer + y < kLooks ? room.look_count[lane * kPer + y] : 0;
         }
         int run = sum;
 #pragma unroll
@@ -580,22 +617,22 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
 #pragma unroll
         for (int x = 0; x < kRegs; ++x) {
           const unsigned long long m = __ballot(between(held[x]));
-          if (between(held[x])) again[before[x] + __popcll(m & below)] = at_look(x);
+          if (between(held[x])) room.again[before[x] + __popcll(m & below)] = at_look(x);
         }
-        __syncthreads();
+        together<kWaves>();
         for (int x = wave; x < n_between; x += kWaves) {
-          const double s = exact_score(again[x]);
-          if (lane == 0) exact[x] = s;
+          const double s = exact_score(room.again[x]);
+          if (lane == 0) room.exact[x] = s;
         }
-        __syncthreads();
+        together<kWaves>();
 #pragma unroll
         for (int x = 0; x < kRegs; ++x) {
           const unsigned long long m = __ballot(between(held[x]));
           if (!between(held[x])) continue;
           const int me = before[x] + __popcll(m & below);
-          const double s = exact[me];
+          const double s = room.exact[me];
           int ahead = 0;
-          for (int y = 0; y < n_between; ++y) ahead += exact[y] > s || (exact[y] == s && y < me) ? 1 : 0;
+          for (int y = 0; y < n_between; ++y) ahead += room.exact[y] > s || (room.exact[y] == s && y < me) ? 1 : 0;
           if (ahead < rest) taken |= 1u << x;
         }
       }
@@ -614,6 +651,75 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
       if (taken >> x & 1u) to[a.n_first + before[x] + __popcll(m & below)] = a.n_first + at_look(x);
     }
   }
+}
+
+// Scores from memory, one block for a row.
+struct ScoresFrom {
+  const float *s, *p;
+  __device__ float score(int b) const { return s[b]; }
+  __device__ float peak(int b) const { return p[b]; }
+};
+template <typename T, int D, int kWaves, int kRegs>
+__global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a) {
+  __shared__ Room<kWaves, kRegs, 512> room;
+  const unsigned row = blockIdx.x, its = row / a.n_kv_heads, seq = its / a.tokens;
+  const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + (row - its * a.n_kv_heads);
+  choose_row<T, D, kWaves, kRegs, 512>(a, row, room, ScoresFrom{a.score + static_cast<size_t>(row) * a.scored, a.peak + unit * a.scored});
+}
+
+// Both for a tile of 32 / kPad tokens of a unit, whose scores stay in LDS: four waves, which take turns at the blocks and then at the tokens.  kRegs: of
+// the candidates, for a lane.
+constexpr int kTileRegs = 16;
+constexpr int kTileBytes = 60 << 10;    // of scores
+template <typename T, int D, int kPad>
+__global__ __launch_bounds__(256) void choose_tile_kernel(const ChooseArgs a) {
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
+  __shared__ Room<1, kTileRegs, 64> room[4];
+  extern __shared__ float scores[];                // [kTokens][scored], largest bounds [scored]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = lane & 31, h = lane >> 5;
+  // (late tokens first: where tokens see their past, they have the most blocks.  Units next: those of eight share an XCD and its L2)
+  const int units = a.n_seqs * a.n_kv_heads, tiles = (a.tokens + kTokens - 1) / kTokens;
+  const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / units, unit = static_cast<int>(blockIdx.x) % units;
+  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads, first = tile * kTokens, n = min(kTokens, a.tokens - first);
+  float *peaks = scores + kTokens * a.scored;
+  // blocks that some token of the tile ranks
+  int most = 0;
+  {
+    const long long token = static_cast<long long>(seq) * a.n_tokens + a.token0 + first;
+    for (int t = 0; t < n; ++t) most = max(most, a.visible ? min(max(a.visible[token + t], 0), a.length) : a.length);
+    most = min((most + a.block - 1) / a.block - a.n_last, a.scored);
+  }
+  u32x4_t pos[kOps], neg[kOps];
+  {
+    const size_t token = static_cast<size_t>(seq) * a.n_tokens + a.token0 + first + min(c / kPad, n - 1);
+    const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + kvh * a.group + min(c % kPad, a.group - 1)) * D + h * (16 / sizeof(T));
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) by_sign<sizeof(T) == 4>(load_chunk(q + j * (32 / sizeof(T)), a.wide), pos[j], neg[j]);
+  }
+  for (int b0 = wave * 32; b0 < most; b0 += 128) {
+    u32x4_t lo[kOps], hi[kOps];
+    load_bounds<T, D>(a, unit, min(b0 + c, most - 1), lo, hi);
+    const float m = peak_of<T, D>(lo, hi);
+    if (h == 0 && b0 + c < most) peaks[b0 + c] = m;
+    tile_scores<T, D, kPad>(
+        a, lo, hi,
+        [&](int, int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
+          x = pos[j];
+          y = neg[j];
+        },
+        [&](int t, float x) __attribute__((always_inline)) {
+          if (b0 + c < most) scores[t * a.scored + b0 + c] = x;
+        });
+  }
+  __syncthreads();
+  struct InLds {
+    const float *s, *p;
+    __device__ float score(int b) const { return s[b]; }
+    __device__ float peak(int b) const { return p[b]; }
+  };
+  for (int t = wave; t < n; t += 4)
+    choose_row<T, D, 1, kTileRegs, 64>(a, static_cast<unsigned>((seq * a.tokens + first + t) * a.n_kv_heads + kvh), room[wave], InLds{scores + t * a.scored, peaks});
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -648,6 +754,27 @@ hipError_t launch_scores(const ChooseArgs &a, int pad, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// One kernel for both: where a tile's scores fit LDS and tiles are as many as half the compute units.
+bool tiles_fit(const ChooseArgs &a, int pad) {
+  const int per = 32 / pad;
+  return a.scored > 0 && a.scored <= 64 * kTileRegs && a.group <= 32 && (per + 1) * a.scored * 4 <= kTileBytes &&
+         static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.tokens + per - 1) / per) >= 128;
+}
+template <typename T, int D>
+hipError_t launch_tiles(const ChooseArgs &a, int pad, hipStream_t stream) {
+  const int per = 32 / pad, bytes = (per + 1) * a.scored * 4;
+  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.tokens + per - 1) / per)));
+  switch (pad) {
+    case 1: hipLaunchKernelGGL((choose_tile_kernel<T, D, 1>), grid, dim3(256), bytes, stream, a); break;
+    case 2: hipLaunchKernelGGL((choose_tile_kernel<T, D, 2>), grid, dim3(256), bytes, stream, a); break;
+    case 4: hipLaunchKernelGGL((choose_tile_kernel<T, D, 4>), grid, dim3(256), bytes, stream, a); break;
+    case 8: hipLaunchKernelGGL((choose_tile_kernel<T, D, 8>), grid, dim3(256), bytes, stream, a); break;
+    case 16: hipLaunchKernelGGL((choose_tile_kernel<T, D, 16>), grid, dim3(256), bytes, stream, a); break;
+    default: hipLaunchKernelGGL((choose_tile_kernel<T, D, 32>), grid, dim3(256), bytes, stream, a);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch(ChooseArgs a, hipStream_t stream) {
   int pad = 1;
@@ -665,6 +792,11 @@ hipError_t launch(ChooseArgs a, hipStream_t stream) {
   }
   for (a.token0 = 0; a.token0 < a.n_tokens; a.token0 += each) {
     a.tokens = a.n_tokens - a.token0 < each ? a.n_tokens - a.token0 : each;
+    if (tiles_fit(a, pad)) {
+      const hipError_t e = launch_tiles<T, D>(a, pad, stream);
+      if (e != hipSuccess) return e;
+      continue;
+    }
     if (a.scored > 0) {
       const hipError_t e = launch_scores<T, D>(a, pad, stream);
       if (e != hipSuccess) return e;
