@@ -11,7 +11,8 @@
 // Rows are heads, every token's filled up to a power of two of them with copies of its last, so that the maximum over a group is one of registers.
 // Numbers that rank are to be the exact ones, whatever order a sum is taken in, and these sums are rounded: each of at most 128 terms that are not zero
 // (the products of bf16 elements are exact) comes with an addition, off by at most 2^-22 of what is added up so far whichever way the
-// matrix instruction rounds, fp32 products with another rounding: a score is within E = 2^-14 max_g |q_g|_1 max_b,e |bound_be| of the exact one.
+// matrix instruction rounds, fp32 products with another rounding: a score is within E = 2^-15 max_g |q_g| max_b |bound_b| (fp32 rows: 2^-14; Euclidean
+// norms, of the larger bound of each element in size) of the exact one.
 // With T the largest but k - 1 of the rounded scores, the exact score of a block
 //   beyond T + 2 E is among the k best: it is above T + E, and so are only blocks whose rounded score is above T, at most k - 1
 //   below T - 2 E is not: it is below T - E, and the k blocks from T on are not
@@ -156,16 +157,23 @@ __device__ __forceinline__ void by_sign(u32x4_t w, u32x4_t &pos, u32x4_t &neg) {
   }
 }
 
+// Squares of the larger one of each pair of elements, in size.  (A NaN does not show here: it does in the score.)
 template <bool kF32>
-__device__ __forceinline__ float largest_of(u32x4_t w) {                // in size; a NaN, if there is one
-  float m = 0.f;
+__device__ __forceinline__ float squares_of(u32x4_t lo, u32x4_t hi, float sum) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    if constexpr (kF32) m = upper(m, fabsf(__uint_as_float(w[e])));
-    else m = upper(upper(m, fabsf(bf16_low(w[e]))), fabsf(bf16_high(w[e])));
+    if constexpr (kF32) {
+      const float x = fmaxf(fabsf(__uint_as_float(lo[e])), fabsf(__uint_as_float(hi[e])));
+      sum = fmaf(x, x, sum);
+    } else {
+      const float x = fmaxf(fabsf(bf16_low(lo[e])), fabsf(bf16_low(hi[e]))), y = fmaxf(fabsf(bf16_high(lo[e])), fabsf(bf16_high(hi[e])));
+      sum = fmaf(y, y, fmaf(x, x, sum));
+    }
   }
-  return m;
+  return sum;
 }
+// Not below the norm whose squares sum up to this: 128 roundings and the root's, and elements too small to have a square in fp32.
+__device__ __forceinline__ float norm_of(float squares) { return sqrtf(squares) * (1.f + 0x1p-10f) + 0x1p-50f; }
 
 // Elements at any address of their own type.
 template <typename T>
@@ -180,9 +188,10 @@ __device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
 }
 
 // Scores of 32 rows (a token's heads filled up to kPad, 32 / kPad tokens) and 32 blocks: put(token, score of block c), for this lane's tokens.
-// A group of more than 32 heads comes in passes; operand(pass, j, pos, neg): chunk 2 j + h of row c.
-template <typename T, int D, int kPad, typename Q, typename P>
-__device__ __forceinline__ void tile_scores(const ChooseArgs &a, const u32x4_t *lo, const u32x4_t *hi, Q operand, P put) {
+// A group of more than 32 heads comes in passes; operand(pass, j, pos, neg): chunk 2 j + h of row c; bounds(j, lo, hi): of block c, after whose products
+// used(j) is called.
+template <typename T, int D, int kPad, typename Q, typename B, typename U, typename P>
+__device__ __forceinline__ void tile_scores(const ChooseArgs &a, Q operand, B bounds, U used, P put) {
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
   const int h = threadIdx.x >> 5 & 1;
@@ -193,18 +202,20 @@ __device__ __forceinline__ void tile_scores(const ChooseArgs &a, const u32x4_t *
     for (int x = 0; x < 16; ++x) s[x] = 0.f;
 #pragma unroll
     for (int j = 0; j < kOps; ++j) {
-      u32x4_t pos, neg;
+      u32x4_t pos, neg, lo, hi;
       operand(pass, j, pos, neg);
+      bounds(j, lo, hi);
       if constexpr (kF32) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[j][e]), s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[j][e]), s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[e]), s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[e]), s, 0, 0, 0);
         }
       } else {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi[j]), s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo[j]), s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi), s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo), s, 0, 0, 0);
       }
+      used(j);
     }
     // rows 8 i + 4 h + j in s[4 i + j]: the maxima of kPad rows next to one another
     if constexpr (kPad == 1) {
@@ -244,24 +255,12 @@ __device__ __forceinline__ void tile_scores(const ChooseArgs &a, const u32x4_t *
   }
 }
 
-// Bounds of block b as an operand; -> its largest one in size.
+// Where this lane's chunks of the bounds of block b lie: 32 bytes apart, the largest elements D behind the smallest.
 template <typename T, int D>
-__device__ __forceinline__ void load_bounds(const ChooseArgs &a, int unit, int b, u32x4_t *lo, u32x4_t *hi) {
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32;
-  const char *from = static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + (threadIdx.x >> 5 & 1) * 16;
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+__device__ __forceinline__ const char *bounds_at(const ChooseArgs &a, int unit, int b) {
+  return static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + (threadIdx.x >> 5 & 1) * 16;
 }
-template <typename T, int D>
-__device__ __forceinline__ float peak_of(const u32x4_t *lo, const u32x4_t *hi) {
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32;
-  float m = 0.f;
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) m = upper(upper(m, largest_of<sizeof(T) == 4>(lo[j])), largest_of<sizeof(T) == 4>(hi[j]));
-  return join_step<32>(m, upper);
-}
+__device__ __forceinline__ float add(float x, float y) { return x + y; }
 
 // Scores for another kernel: a wave has 32 blocks of a unit (x: the unit and 128 blocks of it) and goes over the tokens of its share (y) of the
 // launch's, 32 / kPad of them at a time.
@@ -275,9 +274,17 @@ __global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
   const int b0 = (static_cast<int>(blockIdx.x) - unit * across) * 128 + wave * 32;
   if (b0 >= a.scored) return;
   u32x4_t lo[kOps], hi[kOps];
-  load_bounds<T, D>(a, unit, min(b0 + c, a.scored - 1), lo, hi);
+  const char *from = bounds_at<T, D>(a, unit, min(b0 + c, a.scored - 1));
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) {
+    lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+    hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
+  }
   if (blockIdx.y == 0) {
-    const float m = peak_of<T, D>(lo, hi);
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) m = squares_of<sizeof(T) == 4>(lo[j], hi[j], m);
+    m = norm_of(join_step<32>(m, add));
     if (h == 0 && b0 + c < a.scored) a.peak[static_cast<size_t>(unit) * a.scored + b0 + c] = m;
   }
   const int tiles = (a.tokens + kTokens - 1) / kTokens;
@@ -285,11 +292,16 @@ __global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
   for (int tile = static_cast<int>(blockIdx.y); tile < tiles; tile += static_cast<int>(gridDim.y)) {
     const int token = a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1);
     tile_scores<T, D, kPad>(
-        a, lo, hi,
+        a,
         [&](int pass, int j, u32x4_t &pos, u32x4_t &neg) __attribute__((always_inline)) {
           const T *row = q + ((static_cast<size_t>(seq) * a.n_tokens + token) * a.n_q_heads + min(pass * 32 + c % kPad, a.group - 1)) * D;
           by_sign<sizeof(T) == 4>(load_chunk(row + j * (32 / sizeof(T)), a.wide), pos, neg);
         },
+        [&](int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
+          x = lo[j];
+          y = hi[j];
+        },
+        [](int) {},
         [&](int t, float x) __attribute__((always_inline)) {
           t += tile * kTokens;
           if (t < a.tokens && b0 + c < a.scored) a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b0 + c] = x;
@@ -387,8 +399,8 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
       for (int x = 0; x < looks; ++x) f(x, at_look(x) < n ? order_of(score(min(at_look(x), n - 1))) : 0u);
     }
   };
-  float most = 0.f, size = 0.f;                    // largest bound; largest |q|_1
-  bool odd = false;
+  float most = 0.f, size = 0.f;                    // largest norm of a block's bounds, and of a query
+  bool odd = false, none = true;                   // a score that is no finite number; no element of a query but zeros
   unsigned top = 0u, least = 0xFFFFFFFFu;
   if constexpr (kRegs > 0) {
     float s[kHeld], p[kHeld];
@@ -421,13 +433,8 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   for (int g0 = 0; g0 < a.group; g0 += kBlock / C) {
     const int g = min(g0 + thread / C, a.group - 1);
     const u32x4_t w = load_chunk(q + g * D + lane % C * kElems, a.wide);
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if constexpr (kF32) s += fabsf(__uint_as_float(w[e]));
-      else s += fabsf(bf16_low(w[e])) + fabsf(bf16_high(w[e]));
-    }
-    size = upper(size, join_lanes<1, C / 2>(s, [](float x, float y) { return x + y; }));
+    none &= ((w[0] | w[1] | w[2] | w[3]) & (kF32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0;
+    size = upper(size, norm_of(join_lanes<1, C / 2>(squares_of<kF32>(w, w, 0.f), add)));
   }
   size = join_lanes<C, 32>(size, upper);
   most = join_lanes<1, 32>(most, upper);
@@ -438,16 +445,20 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   size = over_waves<kWaves>(size, room.f, turn_f, upper);
   top = over_waves<kWaves>(top, room.u, turn_u, [](unsigned x, unsigned y) { return max(x, y); });
   least = over_waves<kWaves>(least, room.u, turn_u, [](unsigned x, unsigned y) { return min(x, y); });
-  if constexpr (kWaves > 1) odd = __syncthreads_or(odd);
-  else odd = __ballot(odd) != 0;
+  if constexpr (kWaves > 1) {
+    odd = __syncthreads_or(odd);
+    none = __syncthreads_and(none);
+  } else {
+    odd = __ballot(odd) != 0;
+    none = __ballot(!none) == 0;
+  }
   // (2^-100: products too small for fp32; none of a row of zeros)
-  const float off = size == 0.f && most <= FLT_MAX ? 0.f : size * most * 0x1p-14f + 0x1p-100f;
+  const float off = none && most <= FLT_MAX ? 0.f : size * most * (kF32 ? 0x1p-14f : 0x1p-15f) + 0x1p-100f;
   const bool all_again = odd || !(size * most < 0x1p120f);
-  auto add = [](int x, int y) { return x + y; };
   auto count_from = [&](unsigned cand) __attribute__((always_inline)) {
     int have = 0;
     each([&](int, unsigned k) __attribute__((always_inline)) { have += __popcll(__ballot(k >= cand)); });
-    return over_waves<kWaves>(have, room.i, turn_i, add);
+    return over_waves<kWaves>(have, room.i, turn_i, [](int x, int y) { return x + y; });
   };
 
   // the borders: surely taken from `sure` on, surely not below `out`
@@ -476,8 +487,8 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
     n_sure += __popcll(__ballot(is_sure(k)));
     n_between += __popcll(__ballot(between(k)));
   });
-  n_sure = over_waves<kWaves>(n_sure, room.i, turn_i, add);
-  n_between = over_waves<kWaves>(n_between, room.i, turn_i, add);
+  n_sure = over_waves<kWaves>(n_sure, room.i, turn_i, [](int x, int y) { return x + y; });
+  n_between = over_waves<kWaves>(n_between, room.i, turn_i, [](int x, int y) { return x + y; });
   const int rest = want - n_sure;                  // to take of those between, 0 .. n_between
   const bool ask = (off > 0.f || all_again) && rest > 0 && rest < n_between;
 
@@ -537,13 +548,13 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
       const unsigned long long cand = border | 1ull << bit;
       int have = 0;
       for (int i0 = wave * 64; i0 < n; i0 += kBlock) have += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] >= cand));
-      have = over_waves<kWaves>(have, room.i, turn_i, add);
+      have = over_waves<kWaves>(have, room.i, turn_i, [](int x, int y) { return x + y; });
       if (have >= want) border = cand;
       if (have == want) break;
     }
     int above = 0;
     for (int i0 = wave * 64; i0 < n; i0 += kBlock) above += __popcll(__ballot(i0 + lane < n && all[min(i0 + lane, n - 1)] > border));
-    above = over_waves<kWaves>(above, room.i, turn_i, add);
+    above = over_waves<kWaves>(above, room.i, turn_i, [](int x, int y) { return x + y; });
     if (wave != 0) return;
     int at = a.n_first, met = 0;
     for (int i0 = 0; i0 < n; i0 += 64) {
@@ -690,27 +701,37 @@ __global__ __launch_bounds__(256) void choose_tile_kernel(const ChooseArgs a) {
     for (int t = 0; t < n; ++t) most = max(most, a.visible ? min(max(a.visible[token + t], 0), a.length) : a.length);
     most = min((most + a.block - 1) / a.block - a.n_last, a.scored);
   }
-  u32x4_t pos[kOps], neg[kOps];
+  u32x4_t q[kOps], lo[kOps], hi[kOps];
+  // the bounds of a block are asked for as those of the one before have been used
+  const char *from = bounds_at<T, D>(a, unit, max(min(wave * 32 + c, most - 1), 0));
+  auto fetch = [&](int j) __attribute__((always_inline)) {
+    lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
+    hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
+  };
+#pragma unroll
+  for (int j = 0; j < kOps; ++j) fetch(j);
   {
     const size_t token = static_cast<size_t>(seq) * a.n_tokens + a.token0 + first + min(c / kPad, n - 1);
-    const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + kvh * a.group + min(c % kPad, a.group - 1)) * D + h * (16 / sizeof(T));
+    const T *at = static_cast<const T *>(a.q) + (token * a.n_q_heads + kvh * a.group + min(c % kPad, a.group - 1)) * D + h * (16 / sizeof(T));
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) by_sign<sizeof(T) == 4>(load_chunk(q + j * (32 / sizeof(T)), a.wide), pos[j], neg[j]);
+    for (int j = 0; j < kOps; ++j) q[j] = load_chunk(at + j * (32 / sizeof(T)), a.wide);
   }
   for (int b0 = wave * 32; b0 < most; b0 += 128) {
-    u32x4_t lo[kOps], hi[kOps];
-    load_bounds<T, D>(a, unit, min(b0 + c, most - 1), lo, hi);
-    const float m = peak_of<T, D>(lo, hi);
-    if (h == 0 && b0 + c < most) peaks[b0 + c] = m;
+    from = bounds_at<T, D>(a, unit, min(b0 + 128 + c, most - 1));
+    float m = 0.f;
     tile_scores<T, D, kPad>(
-        a, lo, hi,
-        [&](int, int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
-          x = pos[j];
-          y = neg[j];
+        a, [&](int, int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) { by_sign<sizeof(T) == 4>(q[j], x, y); },
+        [&](int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
+          x = lo[j];
+          y = hi[j];
+          m = squares_of<sizeof(T) == 4>(x, y, m);
         },
+        fetch,
         [&](int t, float x) __attribute__((always_inline)) {
           if (b0 + c < most) scores[t * a.scored + b0 + c] = x;
         });
+    m = norm_of(join_step<32>(m, add));
+    if (h == 0 && b0 + c < most) peaks[b0 + c] = m;
   }
   __syncthreads();
   struct InLds {
