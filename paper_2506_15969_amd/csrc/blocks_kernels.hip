@@ -6,8 +6,8 @@
 // Choice.  score(b) = max over the heads g of the group of sum_e max(q_ge lo_be, q_ge hi_be): of the keys between the bounds none has a
 // larger product with any of the queries.  The larger of the two terms is the one with hi where q_ge > 0 and with lo where q_ge < 0, so
 // the sums are products of matrices, [q+ | q-] [hi | lo]^T with twice the length, on matrix instructions:
-//   32x32x16_bf16 (fp32 rows: 32x32x2_f32), rows of q as A, blocks as B: lane (c, h) = (l % 32, l / 32) holds, of block c,
-//   the sums of the rows 8 i + 4 h + j (i, j < 4)
+//   16x16x32_bf16 (fp32 rows: 16x16x4_f32), rows of q as A, blocks as B: lane (c, g) = (l % 16, l / 16) holds, of block c,
+//   the sums of the rows 4 g + i (i < 4)
 // Rows are heads, every token's filled up to a power of two of them with copies of its last, so that the maximum over a group is one of registers.
 // Numbers that rank are to be the exact ones, whatever order a sum is taken in, and these sums are rounded: each of at most 128 terms that are not zero
 // (the products of bf16 elements are exact) comes with an addition, off by at most 2^-22 of what is added up so far whichever way the
@@ -28,7 +28,7 @@ namespace {
 
 typedef unsigned short bf16_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
 
 __device__ __forceinline__ float bf16_low(unsigned w) { return __uint_as_float(w << 16); }
@@ -150,8 +150,9 @@ __device__ __forceinline__ void by_sign(u32x4_t w, u32x4_t &pos, u32x4_t &neg) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     unsigned minus;
-    if constexpr (kF32) minus = static_cast<unsigned>(static_cast<int>(w[e]) >> 31);
-    else minus = ((w[e] >> 15) & 0x00010001u) * 0xFFFFu;
+    const unsigned high = static_cast<unsigned>(static_cast<int>(w[e]) >> 31), low = static_cast<unsigned>(static_cast<int>(w[e] << 16) >> 31);
+    if constexpr (kF32) minus = high;
+    else minus = (high & 0xFFFF0000u) | (low & 0xFFFFu);
     pos[e] = w[e] & ~minus;
     neg[e] = w[e] & minus;
   }
@@ -187,125 +188,125 @@ __device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
   return w;
 }
 
-// Scores of 32 rows (a token's heads filled up to kPad, 32 / kPad tokens) and 32 blocks: put(token, score of block c), for this lane's tokens.
-// A group of more than 32 heads comes in passes; operand(pass, j, pos, neg): chunk 2 j + h of row c; bounds(j, lo, hi): of block c, after whose products
-// used(j) is called.
-template <typename T, int D, int kPad, typename Q, typename B, typename U, typename P>
-__device__ __forceinline__ void tile_scores(const ChooseArgs &a, Q operand, B bounds, U used, P put) {
-  constexpr bool kF32 = sizeof(T) == 4;
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
-  const int h = threadIdx.x >> 5 & 1;
-  float top = -INFINITY, out[16];
-  for (int pass = 0; pass < (kPad == 32 ? (a.group + 31) / 32 : 1); ++pass) {
-    f32x16_t s;
-#pragma unroll
-    for (int x = 0; x < 16; ++x) s[x] = 0.f;
-#pragma unroll
-    for (int j = 0; j < kOps; ++j) {
-      u32x4_t pos, neg, lo, hi;
-      operand(pass, j, pos, neg);
-      bounds(j, lo, hi);
-      if constexpr (kF32) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(pos[e]), __uint_as_float(hi[e]), s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(neg[e]), __uint_as_float(lo[e]), s, 0, 0, 0);
-        }
-      } else {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi), s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo), s, 0, 0, 0);
-      }
-      used(j);
-    }
-    // rows 8 i + 4 h + j in s[4 i + j]: the maxima of kPad rows next to one another
-    if constexpr (kPad == 1) {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) out[x] = s[x];
-    } else if constexpr (kPad == 2) {
-#pragma unroll
-      for (int x = 0; x < 8; ++x) out[x] = upper(s[2 * x], s[2 * x + 1]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        out[i] = upper(upper(s[4 * i], s[4 * i + 1]), upper(s[4 * i + 2], s[4 * i + 3]));
-        if constexpr (kPad > 4) out[i] = join_step<32>(out[i], upper);
-      }
-      if constexpr (kPad >= 16) {
-        out[0] = upper(out[0], out[1]);
-        out[1] = upper(out[2], out[3]);
-      }
-      if constexpr (kPad == 32) {
-        top = upper(top, upper(out[0], out[1]));
-        out[0] = top;
-      }
-    }
-  }
-  if constexpr (kPad == 1) {
-#pragma unroll
-    for (int x = 0; x < 16; ++x) put(8 * (x / 4) + 4 * h + x % 4, out[x]);
-  } else if constexpr (kPad == 2) {
-#pragma unroll
-    for (int x = 0; x < 8; ++x) put(4 * (x / 2) + 2 * h + x % 2, out[x]);
-  } else if constexpr (kPad == 4) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x) put(2 * x + h, out[x]);
-  } else if (h == 0) {
-#pragma unroll
-    for (int x = 0; x < kTokens; ++x) put(x, out[x]);
-  }
-}
-
-// Where this lane's chunks of the bounds of block b lie: 32 bytes apart, the largest elements D behind the smallest.
-template <typename T, int D>
-__device__ __forceinline__ const char *bounds_at(const ChooseArgs &a, int unit, int b) {
-  return static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + b) * (2 * D * sizeof(T)) + (threadIdx.x >> 5 & 1) * 16;
-}
 __device__ __forceinline__ float add(float x, float y) { return x + y; }
 
-// Scores for another kernel: a wave has 32 blocks of a unit (x: the unit and 128 blocks of it) and goes over the tokens of its share (y) of the
-// launch's, 32 / kPad of them at a time.
-template <typename T, int D, int kPad>
+// A wave has 16 kCols blocks of a unit (x: the unit and 64 kCols blocks of it) and goes over the tokens of its share (y) of the launch's, 16 / kPad of
+// them at a time, the next ones' queries on their way; a token's group of more than 16 heads comes in passes of 16.  (A load brings 64 bytes of each of 16
+// rows: 32 rows to an operand, and 32 bytes of each, take the address units twice as long, which was what bound it.)
+template <typename T, int D, int kPad, int kCols>
 __global__ __launch_bounds__(256) void score_kernel(const ChooseArgs a) {
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
+  constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 64, kTokens = 16 / kPad, kBlocks = 16 * kCols;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = lane & 31, h = lane >> 5;
-  const int across = (a.scored + 127) / 128, unit = static_cast<int>(blockIdx.x) / across;
+  const int c = lane & 15, g = lane >> 4;
+  const int across = (a.scored + 4 * kBlocks - 1) / (4 * kBlocks), unit = static_cast<int>(blockIdx.x) / across;
   const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
-  const int b0 = (static_cast<int>(blockIdx.x) - unit * across) * 128 + wave * 32;
+  const int b0 = (static_cast<int>(blockIdx.x) - unit * across) * (4 * kBlocks) + wave * kBlocks;
   if (b0 >= a.scored) return;
-  u32x4_t lo[kOps], hi[kOps];
-  const char *from = bounds_at<T, D>(a, unit, min(b0 + c, a.scored - 1));
+  const int tiles = (a.tokens + kTokens - 1) / kTokens, passes = kPad == 16 ? (a.group + 15) / 16 : 1;
+  const T *queries = static_cast<const T *>(a.q) + static_cast<size_t>(kvh) * a.group * D + g * (16 / sizeof(T));
+  // (asked for together, before one is used)
+  auto load_row = [&](int tile, int pass, u32x4_t (&w)[kOps]) __attribute__((always_inline)) {
+    const size_t token = static_cast<size_t>(seq) * a.n_tokens + a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1);
+    const T *p = queries + (token * a.n_q_heads + min(pass * 16 + c % kPad, a.group - 1)) * D;
+    if (a.wide) {
 #pragma unroll
-  for (int j = 0; j < kOps; ++j) {
-    lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
-    hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
+      for (int j = 0; j < kOps; ++j) w[j] = *reinterpret_cast<const u32x4_t *>(p + j * (64 / sizeof(T)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) w[j] = load_chunk(p + j * (64 / sizeof(T)), false);
+    }
+  };
+  u32x4_t lo[kCols][kOps], hi[kCols][kOps], q[kOps];
+#pragma unroll
+  for (int x = 0; x < kCols; ++x) {
+    const char *from = static_cast<const char *>(a.bounds) + (static_cast<size_t>(unit) * a.n_blocks + min(b0 + 16 * x + c, a.scored - 1)) * (2 * D * sizeof(T)) + g * 16;
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) lo[x][j] = *reinterpret_cast<const u32x4_t *>(from + j * 64);
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) hi[x][j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 64);
   }
+  int tile = static_cast<int>(blockIdx.y);
+  if (tile < tiles) load_row(tile, 0, q);
   if (blockIdx.y == 0) {
-    float m = 0.f;
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) m = squares_of<sizeof(T) == 4>(lo[j], hi[j], m);
-    m = norm_of(join_step<32>(m, add));
-    if (h == 0 && b0 + c < a.scored) a.peak[static_cast<size_t>(unit) * a.scored + b0 + c] = m;
+    for (int x = 0; x < kCols; ++x) {
+      float m = 0.f;
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) m = squares_of<kF32>(lo[x][j], hi[x][j], m);
+      m = norm_of(join_lanes<16, 32>(m, add));
+      if (g == 0 && b0 + 16 * x + c < a.scored) a.peak[static_cast<size_t>(unit) * a.scored + b0 + 16 * x + c] = m;
+    }
   }
-  const int tiles = (a.tokens + kTokens - 1) / kTokens;
-  const T *q = static_cast<const T *>(a.q) + static_cast<size_t>(kvh) * a.group * D + h * (16 / sizeof(T));
-  for (int tile = static_cast<int>(blockIdx.y); tile < tiles; tile += static_cast<int>(gridDim.y)) {
-    const int token = a.token0 + min(tile * kTokens + c / kPad, a.tokens - 1);
-    tile_scores<T, D, kPad>(
-        a,
-        [&](int pass, int j, u32x4_t &pos, u32x4_t &neg) __attribute__((always_inline)) {
-          const T *row = q + ((static_cast<size_t>(seq) * a.n_tokens + token) * a.n_q_heads + min(pass * 32 + c % kPad, a.group - 1)) * D;
-          by_sign<sizeof(T) == 4>(load_chunk(row + j * (32 / sizeof(T)), a.wide), pos, neg);
-        },
-        [&](int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
-          x = lo[j];
-          y = hi[j];
-        },
-        [](int) {},
-        [&](int t, float x) __attribute__((always_inline)) {
-          t += tile * kTokens;
-          if (t < a.tokens && b0 + c < a.scored) a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b0 + c] = x;
-        });
+  for (; tile < tiles; tile += static_cast<int>(gridDim.y)) {
+    float top[kCols], out[kCols][4];
+#pragma unroll
+    for (int x = 0; x < kCols; ++x) top[x] = -INFINITY;
+    for (int pass = 0; pass < passes; ++pass) {
+      const bool last = pass + 1 == passes;
+      u32x4_t next[kOps];
+      load_row(last ? min(tile + static_cast<int>(gridDim.y), tiles - 1) : tile, last ? 0 : pass + 1, next);
+      f32x4_t s[kCols];
+#pragma unroll
+      for (int x = 0; x < kCols; ++x) s[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        u32x4_t pos, neg;
+        by_sign<kF32>(q[j], pos, neg);
+#pragma unroll
+        for (int x = 0; x < kCols; ++x) {
+          if constexpr (kF32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pos[e]), __uint_as_float(hi[x][j][e]), s[x], 0, 0, 0);
+              s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(neg[e]), __uint_as_float(lo[x][j][e]), s[x], 0, 0, 0);
+            }
+          } else {
+            s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pos), __builtin_bit_cast(bf16x8_t, hi[x][j]), s[x], 0, 0, 0);
+            s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, neg), __builtin_bit_cast(bf16x8_t, lo[x][j]), s[x], 0, 0, 0);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) q[j] = next[j];
+      // rows 4 g + i in s[i]: the maxima of kPad rows next to one another
+#pragma unroll
+      for (int x = 0; x < kCols; ++x) {
+        if constexpr (kPad == 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) out[x][i] = s[x][i];
+        } else if constexpr (kPad == 2) {
+          out[x][0] = upper(s[x][0], s[x][1]);
+          out[x][1] = upper(s[x][2], s[x][3]);
+        } else {
+          float m = upper(upper(s[x][0], s[x][1]), upper(s[x][2], s[x][3]));
+          if constexpr (kPad > 4) m = join_step<16>(m, upper);
+          if constexpr (kPad > 8) m = join_step<32>(m, upper);
+          out[x][0] = top[x] = upper(top[x], m);
+        }
+      }
+    }
+    auto put = [&](int t, int x, float y) __attribute__((always_inline)) {
+      const int b = b0 + 16 * x + c;
+      t += tile * kTokens;
+      if (t < a.tokens && b < a.scored) a.score[((static_cast<size_t>(seq) * a.tokens + t) * a.n_kv_heads + kvh) * a.scored + b] = y;
+    };
+#pragma unroll
+    for (int x = 0; x < kCols; ++x) {
+      if constexpr (kPad == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(4 * g + i, x, out[x][i]);
+      } else if constexpr (kPad == 2) {
+        put(2 * g, x, out[x][0]);
+        put(2 * g + 1, x, out[x][1]);
+      } else if constexpr (kPad == 4) {
+        put(g, x, out[x][0]);
+      } else if constexpr (kPad == 8) {
+        if ((g & 1) == 0) put(g / 2, x, out[x][0]);
+      } else {
+        if (g == 0) put(0, x, out[x][0]);
+      }
+    }
   }
 }
 
@@ -678,71 +679,6 @@ __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a)
   choose_row<T, D, kWaves, kRegs, 512>(a, row, room, ScoresFrom{a.score + static_cast<size_t>(row) * a.scored, a.peak + unit * a.scored});
 }
 
-// Both for a tile of 32 / kPad tokens of a unit, whose scores stay in LDS: four waves, which take turns at the blocks and then at the tokens.  kRegs: of
-// the candidates, for a lane.
-constexpr int kTileRegs = 16;
-constexpr int kTileBytes = 60 << 10;    // of scores
-template <typename T, int D, int kPad>
-__global__ __launch_bounds__(256) void choose_tile_kernel(const ChooseArgs a) {
-  constexpr int kOps = D * static_cast<int>(sizeof(T)) / 32, kTokens = 32 / kPad;
-  __shared__ Room<1, kTileRegs, 64> room[4];
-  extern __shared__ float scores[];                // [kTokens][scored], largest bounds [scored]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = lane & 31, h = lane >> 5;
-  // (late tokens first: where tokens see their past, they have the most blocks.  Units next: those of eight share an XCD and its L2)
-  const int units = a.n_seqs * a.n_kv_heads, tiles = (a.tokens + kTokens - 1) / kTokens;
-  const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / units, unit = static_cast<int>(blockIdx.x) % units;
-  const int seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads, first = tile * kTokens, n = min(kTokens, a.tokens - first);
-  float *peaks = scores + kTokens * a.scored;
-  // blocks that some token of the tile ranks
-  int most = 0;
-  {
-    const long long token = static_cast<long long>(seq) * a.n_tokens + a.token0 + first;
-    for (int t = 0; t < n; ++t) most = max(most, a.visible ? min(max(a.visible[token + t], 0), a.length) : a.length);
-    most = min((most + a.block - 1) / a.block - a.n_last, a.scored);
-  }
-  u32x4_t q[kOps], lo[kOps], hi[kOps];
-  // the bounds of a block are asked for as those of the one before have been used
-  const char *from = bounds_at<T, D>(a, unit, max(min(wave * 32 + c, most - 1), 0));
-  auto fetch = [&](int j) __attribute__((always_inline)) {
-    lo[j] = *reinterpret_cast<const u32x4_t *>(from + j * 32);
-    hi[j] = *reinterpret_cast<const u32x4_t *>(from + D * sizeof(T) + j * 32);
-  };
-#pragma unroll
-  for (int j = 0; j < kOps; ++j) fetch(j);
-  {
-    const size_t token = static_cast<size_t>(seq) * a.n_tokens + a.token0 + first + min(c / kPad, n - 1);
-    const T *at = static_cast<const T *>(a.q) + (token * a.n_q_heads + kvh * a.group + min(c % kPad, a.group - 1)) * D + h * (16 / sizeof(T));
-#pragma unroll
-    for (int j = 0; j < kOps; ++j) q[j] = load_chunk(at + j * (32 / sizeof(T)), a.wide);
-  }
-  for (int b0 = wave * 32; b0 < most; b0 += 128) {
-    from = bounds_at<T, D>(a, unit, min(b0 + 128 + c, most - 1));
-    float m = 0.f;
-    tile_scores<T, D, kPad>(
-        a, [&](int, int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) { by_sign<sizeof(T) == 4>(q[j], x, y); },
-        [&](int j, u32x4_t &x, u32x4_t &y) __attribute__((always_inline)) {
-          x = lo[j];
-          y = hi[j];
-          m = squares_of<sizeof(T) == 4>(x, y, m);
-        },
-        fetch,
-        [&](int t, float x) __attribute__((always_inline)) {
-          if (b0 + c < most) scores[t * a.scored + b0 + c] = x;
-        });
-    m = norm_of(join_step<32>(m, add));
-    if (h == 0 && b0 + c < most) peaks[b0 + c] = m;
-  }
-  __syncthreads();
-  struct InLds {
-    const float *s, *p;
-    __device__ float score(int b) const { return s[b]; }
-    __device__ float peak(int b) const { return p[b]; }
-  };
-  for (int t = wave; t < n; t += 4)
-    choose_row<T, D, 1, kTileRegs, 64>(a, static_cast<unsigned>((seq * a.tokens + first + t) * a.n_kv_heads + kvh), room[wave], InLds{scores + t * a.scored, peaks});
-}
-
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Tokens of a launch: the scores of all of them stay in the on-chip cache (256 MB).
@@ -755,51 +691,23 @@ int tokens_of(const ChooseArgs &a) {
   return static_cast<int>(n < 1 ? 1 : n < static_cast<size_t>(a.n_tokens) ? n : a.n_tokens);
 }
 
-template <typename T, int D>
-hipError_t launch_scores(const ChooseArgs &a, int pad, hipStream_t stream) {
-  const int tiles = (a.tokens + 32 / pad - 1) / (32 / pad);
-  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.scored + 127) / 128);
+template <typename T, int D, int kPad>
+hipError_t launch_scores(const ChooseArgs &a, hipStream_t stream) {
+  constexpr int kCols = 2;                         // (one or four: 43 and 47 instead of 40 us for a token each of 128 units over 3126 blocks)
+  const int tiles = (a.tokens + 16 / kPad - 1) / (16 / kPad);
+  const long long blocks = static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.scored + 64 * kCols - 1) / (64 * kCols));
   if (blocks > (1 << 22)) return hipErrorInvalidValue;
-  int shares = 1;                                  // of the tokens: a few blocks for every compute unit
-  while (shares < tiles && shares * blocks < 1024) shares *= 2;
+  int shares = 1;                                  // of the tokens: two blocks for a compute unit (one, four, eight: 26, 21, 33 instead of 17 us for 640 tokens)
+  while (shares < tiles && shares * blocks < 512) shares *= 2;
   if (shares > tiles) shares = tiles;
-  const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(shares));
-  switch (pad) {
-    case 1: hipLaunchKernelGGL((score_kernel<T, D, 1>), grid, dim3(256), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((score_kernel<T, D, 2>), grid, dim3(256), 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((score_kernel<T, D, 4>), grid, dim3(256), 0, stream, a); break;
-    case 8: hipLaunchKernelGGL((score_kernel<T, D, 8>), grid, dim3(256), 0, stream, a); break;
-    case 16: hipLaunchKernelGGL((score_kernel<T, D, 16>), grid, dim3(256), 0, stream, a); break;
-    default: hipLaunchKernelGGL((score_kernel<T, D, 32>), grid, dim3(256), 0, stream, a);
-  }
-  return hipGetLastError();
-}
-
-// One kernel for both: where a tile's scores fit LDS and tiles are as many as half the compute units.
-bool tiles_fit(const ChooseArgs &a, int pad) {
-  const int per = 32 / pad;
-  return a.scored > 0 && a.scored <= 64 * kTileRegs && a.group <= 32 && (per + 1) * a.scored * 4 <= kTileBytes &&
-         static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.tokens + per - 1) / per) >= 128;
-}
-template <typename T, int D>
-hipError_t launch_tiles(const ChooseArgs &a, int pad, hipStream_t stream) {
-  const int per = 32 / pad, bytes = (per + 1) * a.scored * 4;
-  const dim3 grid(static_cast<unsigned>(static_cast<long long>(a.n_seqs) * a.n_kv_heads * ((a.tokens + per - 1) / per)));
-  switch (pad) {
-    case 1: hipLaunchKernelGGL((choose_tile_kernel<T, D, 1>), grid, dim3(256), bytes, stream, a); break;
-    case 2: hipLaunchKernelGGL((choose_tile_kernel<T, D, 2>), grid, dim3(256), bytes, stream, a); break;
-    case 4: hipLaunchKernelGGL((choose_tile_kernel<T, D, 4>), grid, dim3(256), bytes, stream, a); break;
-    case 8: hipLaunchKernelGGL((choose_tile_kernel<T, D, 8>), grid, dim3(256), bytes, stream, a); break;
-    case 16: hipLaunchKernelGGL((choose_tile_kernel<T, D, 16>), grid, dim3(256), bytes, stream, a); break;
-    default: hipLaunchKernelGGL((choose_tile_kernel<T, D, 32>), grid, dim3(256), bytes, stream, a);
-  }
+  hipLaunchKernelGGL((score_kernel<T, D, kPad, kCols>), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(shares)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch(ChooseArgs a, hipStream_t stream) {
   int pad = 1;
-  while (pad < a.group && pad < 32) pad *= 2;
+  while (pad < a.group && pad < 16) pad *= 2;
   a.wide = reinterpret_cast<uintptr_t>(a.q) % 16 == 0;
   const int each = tokens_of(a);
   const size_t rows = static_cast<size_t>(a.n_seqs) * each * a.n_kv_heads;
@@ -813,13 +721,9 @@ hipError_t launch(ChooseArgs a, hipStream_t stream) {
   }
   for (a.token0 = 0; a.token0 < a.n_tokens; a.token0 += each) {
     a.tokens = a.n_tokens - a.token0 < each ? a.n_tokens - a.token0 : each;
-    if (tiles_fit(a, pad)) {
-      const hipError_t e = launch_tiles<T, D>(a, pad, stream);
-      if (e != hipSuccess) return e;
-      continue;
-    }
     if (a.scored > 0) {
-      const hipError_t e = launch_scores<T, D>(a, pad, stream);
+      const hipError_t e = pad == 1 ? launch_scores<T, D, 1>(a, stream) : pad == 2 ? launch_scores<T, D, 2>(a, stream) : pad == 4 ? launch_scores<T, D, 4>(a, stream)
+                           : pad == 8 ? launch_scores<T, D, 8>(a, stream) : launch_scores<T, D, 16>(a, stream);
       if (e != hipSuccess) return e;
     }
     const long long blocks = static_cast<long long>(a.n_seqs) * a.tokens * a.n_kv_heads;
