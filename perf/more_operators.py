@@ -410,7 +410,7 @@ def run(state):
         return {"out": out, "lse": lse}
     if kind == "weigh":
         if own:
-            weights = state["pages"].weigh(case["length"], state["q"], state["lse"], visible=state["visible"], old=state["old"],
+            weights = state["pages"].weigh(case["length"], state["q"], state["lse"].contiguous(), visible=state["visible"], old=state["old"],
                                            known=case["known"], decay=case["decay"], weights=state["weights"])
         else:
             weights = _plain_weigh(state["q"], state["lse"], state["k_pages"], state["table"], case["length"], state["visible"],
