@@ -1160,8 +1160,9 @@ TilePlan tile_plan_of(const AttendArgs &a) {
   const int n = a.list.tokens, n_blocks = (a.list.entries + (1 << a.list.block_shift) - 1) >> a.list.block_shift;
   if (n < 2 || n_blocks > kListBlocks || n_blocks < 1 || static_cast<long long>(a.n_seqs) * a.n_kv_heads <= 256) return p;
   const bool long_rows = a.dtype == LAZYEV_DTYPE_FP32 && a.head_dim == 128;
-  const int most = (long_rows ? 64 : 128) / a.group;
-  p.tokens = n < most ? n : most < 32 ? most : 32;
+  int most = (long_rows ? 64 : 128) / a.group;
+  most = most < 32 ? most : 32;                    // (a bit each)
+  p.tokens = n < most ? n : most;
   if (p.tokens < 2) return TilePlan{0, 0, 0, 1};
   p.tiles = (n + p.tokens - 1) / p.tokens;
   const int rows = p.tokens * a.group;

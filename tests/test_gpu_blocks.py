@@ -218,8 +218,9 @@ def _attend(c, length, q, blocks, block, visible=None, joined=None, scale=0.0, t
     k, v = c.rows(c.k_pages), c.rows(c.v_pages)
     S, n, Hq, d = q.shape
     G = Hq // c.H
+    # (of many tokens the first and the last ones, and every eleventh)
     for s in range(S):
-        for i in range(n):
+        for i in range(n) if n <= 60 else sorted({*range(12), *range(n - 12, n), *range(0, n, 11)}):
             end = length if visible is None else min(max(int(visible[s, i]), 0), length)
             for h in range(c.H):
                 at = [torch.arange(x * block, min(x * block + block, end), device="cuda") for x in blocks[s, i, h].tolist() if 0 <= x and x * block < end]
@@ -246,7 +247,10 @@ def _some_blocks(c, n, length, block, m):
 
 SHAPES = [  # tables, tokens, query and KV heads, page, length, block, chosen
     (1, 1, 1, 1, 16, 1, 16, 1), (2, 1, 28, 4, 16, 333, 16, 5), (1, 1, 7, 1, 24, 1000, 32, 9), (3, 5, 8, 8, 1, 77, 16, 4), (1, 4, 64, 1, 64, 600, 64, 3),
-    (2, 3, 33, 1, 48, 500, 16, 12), (1, 2, 6, 2, 4096, 3000, 128, 20), (1, 33, 10, 2, 32, 900, 64, 6), (1, 1, 8, 1, 128, 9000, 16, 300), (1, 2, 5, 1, 100, 2000, 128, 3)]
+    (2, 3, 33, 1, 48, 500, 16, 12), (1, 2, 6, 2, 4096, 3000, 128, 20), (1, 33, 10, 2, 32, 900, 64, 6), (1, 1, 8, 1, 128, 9000, 16, 300), (1, 2, 5, 1, 100, 2000, 128, 3),
+    # many units: tiles of tokens share their lists; tiles that the tokens do not fill, pages that end inside blocks, groups of 1 to 64 heads
+    (1, 259, 7, 1, 64, 700, 64, 4), (2, 71, 6, 2, 32, 900, 32, 9), (3, 5, 160, 20, 16, 500, 16, 6), (1, 300, 1, 1, 24, 333, 16, 7), (1, 131, 32, 2, 1, 130, 16, 3),
+    (1, 270, 64, 1, 128, 600, 128, 2), (4, 2, 99, 33, 48, 1000, 64, 12), (1, 33, 40, 8, 64, 5000, 32, 50), (1, 257, 4, 1, 256, 2100, 128, 17)]
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
@@ -269,42 +273,54 @@ def test_attention(lazyev_lib, dtype, d, S, n, Hq, H, page, length, block, m):
     assert all(torch.equal(x, y) for x, y in zip(c.cache.attend_blocks(length, q, blocks, block), plain))
 
 
+# (one token's lists on their own; 40 tokens of 7 KV heads and so on: tiles of tokens)
 @pytest.mark.parametrize("dtype,d", TYPES)
-def test_numbers_that_are_no_block_and_numbers_twice(lazyev_lib, dtype, d):
-    c = Cache(lazyev_lib, dtype, d, 2, 2, 16, 300, seed=3)
-    q = c.randn(2, 4, 14, d).to(c.dt)
-    blocks = _some_blocks(c, 4, 300, 16, 11)
+@pytest.mark.parametrize("n,H", [(4, 2), (40, 7)])
+def test_numbers_that_are_no_block_and_numbers_twice(lazyev_lib, dtype, d, n, H):
+    c = Cache(lazyev_lib, dtype, d, 2, H, 16, 300, seed=3)
+    q = c.randn(2, n, 3 * H, d).to(c.dt)
+    blocks = _some_blocks(c, n, 300, 16, 11)
     blocks[:, 0] = -1                              # no block at all
     blocks[:, 1, :, ::2] = torch.tensor([19, 2 ** 31 - 1, -2 ** 31, 10 ** 6, -7, 1 << 27], device="cuda").int()     # 0 .. 18 are blocks
     blocks[:, 2, :, 3] = blocks[:, 2, :, 4]        # twice
     blocks[:, 3] = blocks[:, 3].flip(-1)           # in another order
-    _attend(c, 300, q, blocks, 16)
-    _attend(c, 295, q, blocks, 16, visible=torch.tensor([[295, 200, 290, 17], [1, 16, 289, 0]], device="cuda").int())
+    if n > 20:
+        blocks[:, 20, :, :] = 5                    # eleven times
+    first = _attend(c, 300, q, blocks, 16)
+    again = c.cache.attend_blocks(300, q, blocks, 16)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    vis = c.randint(0, 300, 2, n).int()
+    vis[0, :4], vis[1, :4] = torch.tensor([295, 200, 290, 17], device="cuda").int(), torch.tensor([1, 16, 289, 0], device="cuda").int()
+    _attend(c, 295, q, blocks, 16, visible=vis)
     _attend(c, 0, q, blocks, 16)
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n,H", [(3, 2), (50, 6)])
 @pytest.mark.parametrize("block,page", [(16, 16), (64, 24), (32, 64)])
-def test_entries_of_no_page(lazyev_lib, dtype, d, block, page):
-    c = Cache(lazyev_lib, dtype, d, 1, 2, page, 700, seed=4)
+def test_entries_of_no_page(lazyev_lib, dtype, d, block, page, n, H):
+    c = Cache(lazyev_lib, dtype, d, 1, H, page, 700, seed=4)
     dense = c.rows(c.k_pages), c.rows(c.v_pages)
     c.table[0, 1], c.table[0, -2] = -1, 10 ** 6
     there = [(torch.arange(700, device="cuda") // page != 1) & (torch.arange(700, device="cuda") // page != c.table.shape[1] - 2)]
     c.rows = lambda pages: dense[0] if pages is c.k_pages else dense[1]
-    q = c.randn(1, 3, 12, d).to(c.dt)
-    blocks = _some_blocks(c, 3, 700, block, 8)
+    q = c.randn(1, n, 3 * H, d).to(c.dt)
+    blocks = _some_blocks(c, n, 700, block, 8)
     blocks[:, :, :, 0] = page // block
     _attend(c, 700, q, blocks, block, there=there)
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("many", [1, 30])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
-def test_what_a_token_does_not_see_has_no_influence(lazyev_lib, dtype, d, value):
+def test_what_a_token_does_not_see_has_no_influence(lazyev_lib, dtype, d, value, many):
     """Entries of other blocks, those of a listed block behind what the token sees, and those behind the length."""
     c = Cache(lazyev_lib, dtype, d, 1, 2, 24, 500, seed=5)
-    q = c.randn(1, 6, 14, d).to(c.dt)
-    blocks = torch.tensor([0, 3, 7, 12, -1], device="cuda").int().expand(1, 6, 2, 5).contiguous()
-    vis = torch.tensor([[500, 402, 385, 120, 7, 397]], device="cuda").int()
+    n = 6 * many                                   # (30: tiles of tokens)
+    q = c.randn(1, n, 14, d).to(c.dt)
+    blocks = torch.tensor([0, 3, 7, 12, -1], device="cuda").int().expand(1, n, 2, 5).contiguous()
+    blocks[:, ::2, :, 4] = 10
+    vis = torch.tensor([[500, 402, 385, 120, 7, 397]], device="cuda").int().repeat(1, many)
     clean = c.cache.attend_blocks(450, q, blocks, 32, visible=vis)
     for at in list(range(32, 96)) + list(range(416, 500)) + list(range(402, 416)):
         if at >= 416 or at < 402:
@@ -316,6 +332,29 @@ def test_what_a_token_does_not_see_has_no_influence(lazyev_lib, dtype, d, value)
     assert bool((~torch.isfinite(got[0][:, ~low])).all())
     only = c.cache.attend_blocks(450, q, blocks[..., :3].contiguous(), 32)       # (none of them listed)
     assert bool(torch.isfinite(only[0]).all())
+    # a value that some tokens of a tile read, in a column of its own: theirs and nobody else's
+    c.v_pages[c.table[0, 321 // 24].long(), :, 321 % 24, 5] = value               # (of block 10)
+    got = c.cache.attend_blocks(400, q, blocks, 32)
+    assert bool((~torch.isfinite(got[0][:, ::2, :, 5])).all()) and bool(torch.isfinite(got[0][:, 1::2]).all())
+    others = torch.arange(d, device="cuda") != 5
+    assert bool(torch.isfinite(got[0][..., others]).all())
+
+
+def test_tokens_that_share_a_tile_do_not_see_one_another(lazyev_lib):
+    """A token's bits depend on its own list and queries alone: other tokens' lists, values and order in the tile change nothing."""
+    for dtype, d in TYPES:
+        c = Cache(lazyev_lib, dtype, d, 1, 4, 32, 2000, seed=20)
+        n = 90
+        q = c.randn(1, n, 28, d).to(c.dt)
+        blocks = _some_blocks(c, n, 2000, 32, 12)
+        vis = c.randint(1500, 2001, 1, n).int()
+        want = c.cache.attend_blocks(2000, q, blocks, 32, visible=vis)
+        other_q, other_b = c.randn(1, n, 28, d).to(c.dt) * 3, blocks.clone()
+        keep = torch.arange(n, device="cuda") % 3 == 1
+        other_q[:, keep] = q[:, keep]
+        mine = other_b[:, keep].clone()
+        got = c.cache.attend_blocks(2000, other_q, other_b, 32, visible=vis)
+        assert torch.equal(got[0][:, keep], want[0][:, keep]) and torch.equal(got[1][:, keep], want[1][:, keep]) and torch.equal(mine, blocks[:, keep])
 
 
 def test_the_binding_refuses(lazyev_lib):
