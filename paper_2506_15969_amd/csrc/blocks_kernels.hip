@@ -457,8 +457,9 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   const float off = none && most <= FLT_MAX ? 0.f : size * most * (kF32 ? 0x1p-14f : 0x1p-15f) + 0x1p-100f;
   const bool all_again = odd || !(size * most < 0x1p120f);
   auto count_from = [&](unsigned cand) __attribute__((always_inline)) {
-    int have = 0;
-    each([&](int, unsigned k) __attribute__((always_inline)) { have += __popcll(__ballot(k >= cand)); });
+    int have = 0;                                  // (of the lane: counts of ballots take scalar registers that there are too few of)
+    each([&](int, unsigned k) __attribute__((always_inline)) { have += k >= cand ? 1 : 0; });
+    have = join_lanes<1, 32>(have, [](int x, int y) { return x + y; });
     return over_waves<kWaves>(have, room.i, turn_i, [](int x, int y) { return x + y; });
   };
 
@@ -485,9 +486,11 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   auto between = [&](unsigned k) __attribute__((always_inline)) { return k != 0u && (all_again || (k < sure && k >= out)); };
   int n_sure = 0, n_between = 0;
   each([&](int, unsigned k) __attribute__((always_inline)) {
-    n_sure += __popcll(__ballot(is_sure(k)));
-    n_between += __popcll(__ballot(between(k)));
+    n_sure += is_sure(k) ? 1 : 0;
+    n_between += between(k) ? 1 : 0;
   });
+  n_sure = join_lanes<1, 32>(n_sure, [](int x, int y) { return x + y; });
+  n_between = join_lanes<1, 32>(n_between, [](int x, int y) { return x + y; });
   n_sure = over_waves<kWaves>(n_sure, room.i, turn_i, [](int x, int y) { return x + y; });
   n_between = over_waves<kWaves>(n_between, room.i, turn_i, [](int x, int y) { return x + y; });
   const int rest = want - n_sure;                  // to take of those between, 0 .. n_between
