@@ -34,9 +34,9 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
 __device__ __forceinline__ float bf16_low(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// (a NaN stays)
-__device__ __forceinline__ float lower(float m, float x) { return x < m || x != x ? x : m; }
-__device__ __forceinline__ float upper(float m, float x) { return x > m || x != x ? x : m; }
+// (a NaN stays: v_minimum3_f32, v_maximum3_f32)
+__device__ __forceinline__ float lower(float m, float x) { return __builtin_elementwise_minimum(m, x); }
+__device__ __forceinline__ float upper(float m, float x) { return __builtin_elementwise_maximum(m, x); }
 
 // x of the lanes whose numbers differ in the bits kFrom .. kTo (powers of two) joined; a step of 4 takes the steps of 1 and 2 to be done.
 template <int kStep>

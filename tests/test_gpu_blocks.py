@@ -165,6 +165,24 @@ def test_equal_scores_go_by_their_numbers(lazyev_lib, dtype, d, n_blocks):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_choice_of_very_many_blocks(lazyev_lib, dtype):
+    """More blocks than a row's registers hold; then many tokens, whose scores come in several turns."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    dt = _dt(dtype)
+    bounds = _bounds(gen, 1, 2, 17000, 64, dt)
+    bounds[:, :, 5000:5300] = bounds[:, :, 100:400]
+    q = torch.randn((1, 3, 4, 64), generator=gen, device="cuda").to(dt)
+    q[:, 2] = 0
+    for chosen in (7, 900):
+        _choose(lazyev_lib, bounds, 16, 16 * 17000, q, chosen, first=2, last=2)
+    bounds = _bounds(gen, 1, 8, 4100, 64, dt)
+    q = torch.randn((1, 300, 8, 64), generator=gen, device="cuda").to(dt)
+    size = lazyev_lib.lib.lazyev_blocks_choose_workspace(lazyev_lib.KeyBounds(bounds, 16).blocks, 16 * 4100, 300, 8, 1, 33)
+    assert size < 300 * 8 * 4098 * 12              # (not for all of them at once)
+    _choose(lazyev_lib, bounds, 16, 16 * 4100, q, 33)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_choice_by_odd_numbers(lazyev_lib, dtype):
     """Infinities, NaN, blocks of nothing, sums that leave the range of 32 bits, elements too small for a product of 32 bits."""
     gen = torch.Generator(device="cuda").manual_seed(6)
@@ -250,7 +268,9 @@ SHAPES = [  # tables, tokens, query and KV heads, page, length, block, chosen
     (2, 3, 33, 1, 48, 500, 16, 12), (1, 2, 6, 2, 4096, 3000, 128, 20), (1, 33, 10, 2, 32, 900, 64, 6), (1, 1, 8, 1, 128, 9000, 16, 300), (1, 2, 5, 1, 100, 2000, 128, 3),
     # many units: tiles of tokens share their lists; tiles that the tokens do not fill, pages that end inside blocks, groups of 1 to 64 heads
     (1, 259, 7, 1, 64, 700, 64, 4), (2, 71, 6, 2, 32, 900, 32, 9), (3, 5, 160, 20, 16, 500, 16, 6), (1, 300, 1, 1, 24, 333, 16, 7), (1, 131, 32, 2, 1, 130, 16, 3),
-    (1, 270, 64, 1, 128, 600, 128, 2), (4, 2, 99, 33, 48, 1000, 64, 12), (1, 33, 40, 8, 64, 5000, 32, 50), (1, 257, 4, 1, 256, 2100, 128, 17)]
+    (1, 270, 64, 1, 128, 600, 128, 2), (4, 2, 99, 33, 48, 1000, 64, 12), (1, 33, 40, 8, 64, 5000, 32, 50), (1, 257, 4, 1, 256, 2100, 128, 17),
+    # runs of single entries: more of them than a block looks up at once
+    (1, 2, 4, 1, 5, 4000, 16, 100), (1, 200, 8, 2, 3, 3000, 16, 10)]
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)

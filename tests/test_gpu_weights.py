@@ -127,6 +127,19 @@ def test_weights_of_nothing(lazyev_lib):
     assert bool((c.cache.weigh(100, q, torch.full_like(lse, math.inf)) == 0).all())
 
 
+def test_weights_from_very_many_rows(lazyev_lib):
+    """66400 rows of a KV head (more stages than a block lists at once), which see the first 300 of 32768 entries at most."""
+    c = Cache(lazyev_lib, "bf16", 64, 1, 8, 256, 32768, seed=15)
+    q = c.randn(1, 8300, 64, 64).bfloat16()
+    vis = c.randint(0, 301, 1, 8300).int()
+    vis[0, 100:5000] = 0
+    lse = _lse(c, 300, q, vis)
+    got = c.cache.weigh(32768, q, lse, visible=vis)
+    assert bool((got[:, :, 300:] == 0).all())
+    want, bound = long64.weigh(q[0], lse[0], c.rows(c.k_pages)[0, :300], vis[0].long(), 0.125)
+    assert bool(((got[0, :, :300].double() - want).abs() <= bound + U * want.abs() + 1e-30).all())
+
+
 # ------------------------------------------------------------------------------------ eviction
 
 def _evict(c, length, weights, keep, recent=0, first=0, positions=None, lengths=None, in_place=False, no_page=()):
