@@ -354,7 +354,7 @@ struct WeightEvictArgs {
   int32_t *positions_to;
   void *k_pages, *v_pages;
   PageTable pages;
-  int32_t *free_places;             // workspace: [units][keep]
+  int32_t *free_places;             // workspace: [2][units][keep] free places, entries that come to them
 };
 size_t weight_evict_workspace(const WeightEvictArgs &a);
 hipError_t launch_weight_evict(WeightEvictArgs a, hipStream_t stream);

@@ -10,6 +10,7 @@
 //         and their order does not matter; moves in the entries' order (which would keep it) are as many as entries behind the first
 //         one that goes: about `keep` of them where a window of 64 goes from 2112, instead of at most 64.
 #include "kernels.h"
+#include "lanes.h"
 #include "lazyev.h"
 
 #include <climits>
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
   __shared__ int picked[3];                        // part of the range, keys of it, keys beyond it
   constexpr int kOwn = kChunks > 0 ? kOwnMoves : 1;
   __shared__ unsigned from_row[kOwn], to_row[kOwn];
-  __shared__ int free_place[kOwn];
+  __shared__ int free_place[kOwn], late_entry[kOwn];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int unit = static_cast<int>(blockIdx.x), seq = unit / a.n_kv_heads, kvh = unit - seq * a.n_kv_heads;
   const int len = a.lengths ? min(max(a.lengths[seq], 0), a.length) : a.length;
@@ -126,8 +127,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
     } else {
       for (int x = 0; x < looks; ++x) newest = max(newest, entry_of(x) < len ? positions[entry_of(x)] : INT_MIN);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) newest = max(newest, __shfl_xor(newest, o));
+    newest = join_lanes<1, 32>(newest, [](int x, int y) { return max(x, y); });
     if (lane == 0) waves_i[turn][wave] = newest;
     __syncthreads();
 #pragma unroll
@@ -167,11 +167,8 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
       least = min(least, in ? k : 0xFFFFFFFFu);
       most = max(most, in ? k : 0u);
     });
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      least = min(least, static_cast<unsigned>(__shfl_xor(static_cast<int>(least), o)));
-      most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), o)));
-    }
+    least = join_lanes<1, 32>(least, [](unsigned x, unsigned y) { return min(x, y); });
+    most = join_lanes<1, 32>(most, [](unsigned x, unsigned y) { return max(x, y); });
     if (lane == 0) {
       waves_u[0][wave] = least;
       waves_u[1][wave] = most;
@@ -194,8 +191,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
 #pragma unroll 8
     for (int y = 0; y < 64; ++y) times += static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(k), y)) == k ? 1 : 0;
     int best = times << 6 | lane;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) best = max(best, __shfl_xor(best, o));
+    best = join_lanes<1, 32>(best, [](int x, int y) { return max(x, y); });
     const unsigned mode = static_cast<unsigned>(__shfl(static_cast<int>(k), best & 63));
     if (lane == 0) picked[0] = best >> 6 > 4 ? static_cast<int>(mode) : 0;
   }
@@ -204,7 +200,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
   __syncthreads();
   int want = a.keep, have = len;                   // of the keys in the range
   int had = 0;
-  while (true) {
+  for (int pass = 0; pass < 8; ++pass) {           // (four do: 10 bits each)
     if (have > had / 4) tighten();                 // (the first time, and where a part has much of the range: many equal ones)
     had = have;
     if (low == high || want == have) break;        // (uniform)
@@ -218,8 +214,7 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
       else atomicAdd(&bins[(k - low) >> shift], 1);
     });
     if (common - low <= high - low) {              // (uniform)
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) alike += __shfl_xor(alike, o);
+      alike = join_lanes<1, 32>(alike, [](int x, int y) { return x + y; });
       if (lane == 0) atomicAdd(&bins[(common - low) >> shift], alike);
     }
     __syncthreads();
@@ -248,71 +243,114 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
     __syncthreads();
   }
   // keys beyond the range stay, and of those in it (all of them, or equal ones) `want`, the lowest
-  int mine = 0, all;
-  each([&](int i, unsigned k) __attribute__((always_inline)) { mine += __popcll(__ballot(i < len && k >= low && k <= high)); });
-  int met = before_wave(mine, all);
   const unsigned long long below = (1ull << lane) - 1;
-  unsigned kept = 0;                               // bit x: this lane's entry x stays
-  int n_free = 0, n_late = 0;
-  auto stays_of = [&](int i, unsigned k) __attribute__((always_inline)) {
-    const bool in = i < len && k >= low && k <= high;
-    const unsigned long long m = __ballot(in);
-    const bool stays = i < len && (k > high || (in && met + __popcll(m & below) < want));
-    met += __popcll(m);
-    return stays;
+  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
+  int32_t *list = kChunks > 0 ? free_place : a.free_places + static_cast<size_t>(unit) * a.keep;
+  int all = 0;
+  auto comes = [&](int i, int n, int place) __attribute__((always_inline)) {   // entry i to the n-th free place
+    sources[place] = i;
+    if constexpr (kChunks > 0) {
+      put_numbers(a, unit, place, i);
+      unsigned rf, rt;
+      const bool both = pool_row(a, table, kvh, i, rf) & pool_row(a, table, kvh, place, rt);
+      from_row[n] = both ? rf : 0u;
+      to_row[n] = both ? rt : 0u;
+    }
   };
-  const int met_0 = met;
-  {
-    int x = 0;
+  if constexpr (kRegs > 0) {
+    // as bits, a word of 32 entries for a thread
+    __shared__ unsigned beyond_bits[32 * kRegs], in_bits[32 * kRegs];
+#pragma unroll
+    for (int x = 0; x < kRegs; ++x) {
+      const unsigned long long beyond = __ballot(held[x] > high), in = __ballot(held[x] - low <= high - low);
+      if (lane < 2) {
+        beyond_bits[(wave * kRegs + x) * 2 + lane] = static_cast<unsigned>(beyond >> (32 * lane));
+        in_bits[(wave * kRegs + x) * 2 + lane] = static_cast<unsigned>(in >> (32 * lane));
+      }
+    }
+    __syncthreads();
+    const int word = static_cast<int>(threadIdx.x);
+    auto before_word = [&](int mine, int &total) __attribute__((always_inline)) {
+      int run = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(run, o);
+        run += lane >= o ? y : 0;
+      }
+      return before_wave(__builtin_amdgcn_readlane(run, 63), total) + run - mine;
+    };
+    unsigned kept = word < 32 * kRegs ? beyond_bits[word] : 0u, in = word < 32 * kRegs ? in_bits[word] : 0u;
+    const int n_in = static_cast<int>(__popc(in)), room = want - before_word(n_in, all);   // (of no sign: __popc; room may be negative)
+    if (room >= n_in) {
+      kept |= in;
+    } else {
+      unsigned rest = in;
+      for (int x = 0; x < room; ++x) rest &= rest - 1;
+      kept |= in & ~rest;
+    }
+    const int left = a.keep - 32 * word;           // entries of the word below `keep`
+    const unsigned low_places = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+    unsigned free = word < 32 * kRegs ? ~kept & low_places : 0u, late = kept & ~low_places;
+    // (numbers of 16 bits: at most 32768 of each)
+    int both = 0;
+    const int before = before_word(static_cast<int>(__popc(free) | __popc(late) << 16), both);
+    all = static_cast<int>(static_cast<unsigned>(both) >> 16);
+    if (word < 32 * kRegs) beyond_bits[word] = kept;
+    // (numbers alone: what has to be looked up for an entry is left to a thread of its own)
+    int32_t *lates = kChunks > 0 ? late_entry : list + static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.keep;
+    for (int n = before & 0xFFFF; free; free &= free - 1) list[n++] = 32 * word + __builtin_ctz(free);
+    for (int n = static_cast<int>(static_cast<unsigned>(before) >> 16); late; late &= late - 1) lates[n++] = 32 * word + __builtin_ctz(late);
+    __threadfence_block();
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.keep; i += kSelectBlock)
+      if (beyond_bits[i / 32] >> (i % 32) & 1u) {
+        sources[i] = i;
+        if constexpr (kChunks > 0) put_numbers(a, unit, i, i);
+      }
+    for (int n = threadIdx.x; n < all; n += kSelectBlock) comes(lates[n], n, list[n]);
+  } else {
+    // along each wave's stretch.  (Numbers that change meanwhile, which no caller may do, find no place out of range)
+    int mine = 0;
+    each([&](int i, unsigned k) __attribute__((always_inline)) { mine += __popcll(__ballot(i < len && k >= low && k <= high)); });
+    const int met_0 = before_wave(mine, all);
+    int met = met_0;
+    auto stays_of = [&](int i, unsigned k) __attribute__((always_inline)) {
+      const bool in = i < len && k >= low && k <= high;
+      const unsigned long long m = __ballot(in);
+      const bool stays = i < len && (k > high || (in && met + __popcll(m & below) < want));
+      met += __popcll(m);
+      return stays;
+    };
+    int n_free = 0, n_late = 0;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
       const bool stays = stays_of(i, k);
-      if constexpr (kRegs > 0) kept |= stays ? 1u << x : 0u;
-      ++x;
       n_free += __popcll(__ballot(i < a.keep && !stays));
       n_late += __popcll(__ballot(i >= a.keep && stays));
     });
-  }
-  int at_free = before_wave(n_free, all), at_late = before_wave(n_late, all);
-  int32_t *list = kChunks > 0 ? free_place : a.free_places + static_cast<size_t>(unit) * a.keep;
-  auto places = [&](auto f) __attribute__((always_inline)) {
+    int at_free = before_wave(n_free, all), at_late = before_wave(n_late, all);
     met = met_0;
-    int x = 0;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
-      bool stays;
-      if constexpr (kRegs > 0) stays = kept >> x & 1u;
-      else stays = stays_of(i, k);
-      ++x;
-      f(i, stays);
+      const bool stays = stays_of(i, k), free = i < a.keep && !stays;
+      const unsigned long long m = __ballot(free);
+      const int n = at_free + __popcll(m & below);
+      if (free && n < a.keep) list[n] = i;
+      else if (i < a.keep) sources[i] = i;
+      at_free += __popcll(m);
     });
-  };
-  places([&](int i, bool stays) __attribute__((always_inline)) {
-    const bool free = i < a.keep && !stays;
-    const unsigned long long m = __ballot(free);
-    if (free) list[at_free + __popcll(m & below)] = i;
-    else if (i < a.keep) sources[i] = i;
-    at_free += __popcll(m);
-    if constexpr (kChunks > 0)
-      if (i < a.keep && stays) put_numbers(a, unit, i, i);
-  });
-  __threadfence_block();
-  __syncthreads();
-  const int32_t *table = a.pages.table + static_cast<long long>(seq) * a.pages.stride;
-  places([&](int i, bool stays) __attribute__((always_inline)) {
-    const bool late = i >= a.keep && stays;
-    const unsigned long long m = __ballot(late);
-    if (late) {
-      const int n = at_late + __popcll(m & below), to = list[n];
-      sources[to] = i;
-      if constexpr (kChunks > 0) {
-        put_numbers(a, unit, to, i);
-        unsigned rf, rt;
-        const bool both = pool_row(a, table, kvh, i, rf) & pool_row(a, table, kvh, to, rt);
-        from_row[n] = both ? rf : 0u;
-        to_row[n] = both ? rt : 0u;
+    __threadfence_block();
+    __syncthreads();
+    met = met_0;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+      const bool stays = stays_of(i, k), late = i >= a.keep && stays;
+      const unsigned long long m = __ballot(late);
+      const int n = at_late + __popcll(m & below);
+      if (late && n < a.keep) {
+        const int place = list[n];
+        if (place >= 0 && place < a.keep) comes(i, n, place);
       }
-    }
-    at_late += __popcll(m);
-  });
+      at_late += __popcll(m);
+    });
+  }
   if constexpr (kChunks > 0) {
     __syncthreads();
     move_rows<kChunks, kSelectBlock, 1>(a, from_row, to_row, all);
@@ -365,7 +403,7 @@ void launch_select(const WeightEvictArgs &a, const dim3 &grid, hipStream_t strea
 }  // namespace
 
 size_t weight_evict_workspace(const WeightEvictArgs &a) {
-  return (static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.keep * 4 + 255) / 256 * 256;
+  return (2 * static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.keep * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_weight_evict(WeightEvictArgs a, hipStream_t stream) {
