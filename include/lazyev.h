@@ -447,7 +447,7 @@ size_t lazyev_blocks_attend_workspace(const lazyev_pages *pages /*host*/, int32_
                                       int32_t n_tokens, int32_t n_q_heads);
 
 /* The attention weight that every entry received, over the tokens that see it and the heads of its group:
- *   weights[s][kvh][e] = (e < known ? decay * old[s][kvh][e] : 0) + sum of exp(scale * q k - lse),  e < length
+ *   weights[s][kvh][e] = (e < known and decay is not 0 ? decay * old[s][kvh][e] : 0) + sum of exp(scale * q k - lse),  e < length
  * with the lse that lazyev_pages_attend (or lazyev_blocks_attend) gave these queries; one over more than the row's entries, a joined one, gives
  * the weights beside those.  Called for a prompt and then for every step, with decay 1, it keeps the sum of all weights; with decay 0 those of
  * the call alone.  A token whose lse is -inf adds nothing, nor does any token to an entry that it does not see or that lies in no page.
@@ -471,7 +471,7 @@ size_t lazyev_pages_weigh_workspace(const lazyev_pages *pages /*host*/, int32_t 
  * their keys and values.  So no more rows are moved than entries go; the order of entries is not that of positions any more, which
  * attention does not ask for.  Entries from `keep` on are left as they are.
  * sources (device): [n_seqs][n_kv_heads][keep], the entry that each place holds now, -1 from n on.
- * weights, positions (device): `stride` elements from one KV head to the next (at least length).  weights_to, positions_to (device, nullable): weights and positions
+ * weights, positions (device): `stride` elements from one KV head to the next (at least length; length 0: may be null).  weights_to, positions_to (device, nullable): weights and positions
  *   of the places, 0 and -1 from n on, `to_stride` elements from one KV head to the next (at least keep); they may be weights and positions with the same
  *   stride, and overlap nothing else.  Rows of entries of no page are not moved.  An entry below `keep` that two table rows share holds an unspecified one of their rows.
  * keep >= 1, n_recent, n_first >= 0, n_recent + n_first <= keep; n_seqs * n_kv_heads below 2^22, n_seqs * n_kv_heads * (keep / 64 + 1) below 2^24; length up to 2^30.

@@ -556,6 +556,7 @@ class KeyBounds:
     def of(cls, cache, block, entries=None):
         """For the rows of a PagedCache, with room for `entries` of each (None: for all that its table has)."""
         pg = cache.pages
+        _need(block in (16, 32, 64, 128), "blocks of 16, 32, 64 or 128 entries")
         n = -(-(cache.entries if entries is None else entries) // block)
         return cls(cache.k_pages.new_empty((pg.n_seqs, pg.n_kv_heads, n, 2, pg.head_dim)), block)
 

@@ -178,7 +178,8 @@ int lazyev_pages_weigh(const lazyev_pages *pages, int32_t length, int32_t n_toke
   if (!weights || (known > 0 && !old) || !aligned(weights, 4) || !aligned(old, 4)) return LAZYEV_EINVAL;
   if (n_tokens > 0 && (!q || !lse || !aligned(q, elem(pages->dtype)) || !aligned(lse, 4) || !aligned(visible, 4))) return LAZYEV_EINVAL;
   if (!workspace_ok(workspace, workspace_bytes, n_tokens > 0 ? lazyev::weigh_workspace(a) : 0)) return LAZYEV_EWORKSPACE;
-  a.known = known; a.decay = decay;
+  a.known = decay == 0.f ? 0 : known;
+  a.decay = decay;
   a.scale = scale_of(scale, pages->head_dim);
   a.visible = visible; a.q = q; a.lse = lse; a.old = old; a.weights = weights; a.stride = stride;
   a.workspace = workspace;
@@ -201,7 +202,7 @@ int lazyev_pages_evict(const lazyev_pages *pages, int32_t length, const int32_t 
   const long long units = static_cast<long long>(pages->n_seqs) * pages->n_kv_heads;
   if (units >= (1 << 22) || units * (keep / 64 + 1) >= (1ll << 24)) return LAZYEV_EINVAL;
   if (stride < length || stride > (1ll << 40) || ((weights_to || positions_to) && (to_stride < keep || to_stride > (1ll << 40)))) return LAZYEV_EINVAL;
-  if (!weights || !sources) return LAZYEV_EINVAL;
+  if ((!weights && length > 0) || !sources) return LAZYEV_EINVAL;
   for (const void *x : {static_cast<const void *>(lengths), static_cast<const void *>(weights), static_cast<const void *>(positions),
                         static_cast<const void *>(sources), static_cast<const void *>(weights_to), static_cast<const void *>(positions_to)})
     if (!aligned(x, 4)) return LAZYEV_EINVAL;

@@ -381,6 +381,8 @@ def test_the_binding_refuses(lazyev_lib):
     c = Cache(lazyev_lib, "bf16", 128, 2, 4, 16, 100)
     q = c.randn(2, 3, 28, 128).bfloat16()
     x = lazyev_lib.KeyBounds.of(c.cache, 16)
+    with pytest.raises(ValueError):
+        lazyev_lib.KeyBounds.of(c.cache, 0)
     blocks = x.choose(0, q, 3)
     assert bool((blocks == -1).all())
     for bad in (dict(length=200), dict(length=-1), dict(q=q.float()), dict(q=q[:1]), dict(q=q.transpose(1, 2)), dict(n=0), dict(first=3), dict(last=0),

@@ -116,12 +116,32 @@ def test_weights_of_what_is_not_seen(lazyev_lib, dtype, d):
     assert torch.equal(got[:, :, ~none], (clean + 0.5)[:, :, ~none])
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n", [2, 40])
+def test_a_row_whose_logsumexp_is_no_number(lazyev_lib, dtype, d, n):
+    """It says nothing of the entries that it does not see."""
+    c = Cache(lazyev_lib, dtype, d, 1, 2, 16, 200, seed=16)
+    q = c.randn(1, n, 14, d).to(c.dt)
+    vis = c.randint(100, 200, 1, n).int()
+    vis[0, 1] = 33
+    lse = _lse(c, 200, q, vis)
+    clean = c.cache.weigh(200, q, lse, visible=vis)
+    for odd in (math.nan, math.inf):
+        lse[0, 1, 5] = odd
+        got = c.cache.weigh(200, q, lse, visible=vis)
+        assert torch.equal(got[0, 1], clean[0, 1]) and torch.equal(got[0, 0, 33:], clean[0, 0, 33:])
+        assert bool(torch.isnan(got[0, 0, :33]).all()) if math.isnan(odd) else bool((got[0, 0, :33] <= clean[0, 0, :33]).all())
+
+
 def test_weights_of_nothing(lazyev_lib):
     c = Cache(lazyev_lib, "bf16", 128, 2, 4, 16, 100, seed=9)
     q = c.randn(2, 3, 28, 128).bfloat16()
     lse = _lse(c, 100, q)
     old = c.randn(2, 4, 100)
     assert torch.equal(c.cache.weigh(100, q[:, :0], lse[:, :0], old=old, decay=0.5), 0.5 * old)        # no token
+    junk = torch.full_like(old, math.nan)
+    assert torch.equal(c.cache.weigh(100, q, lse, old=junk, decay=0.0, weights=junk), c.cache.weigh(100, q, lse))   # nothing of what was before
+    assert torch.equal(c.cache.weigh(100, q[:, :0], lse[:, :0], old=junk.fill_(math.inf), decay=0.0), torch.zeros_like(old))
     assert c.cache.weigh(0, q, lse).shape == (2, 4, 0)                                                 # no entry
     assert torch.equal(c.cache.weigh(100, q, torch.full_like(lse, -math.inf), old=old), old)           # nothing seen
     assert bool((c.cache.weigh(100, q, torch.full_like(lse, math.inf)) == 0).all())
@@ -211,6 +231,13 @@ def test_odd_weights(lazyev_lib):
     weights[:] = math.nan
     _evict(c, 300, weights, 100, 3, 3)
     _evict(c, 300, torch.full_like(weights, -math.inf), 100, 3, 3)
+
+
+def test_eviction_from_nothing(lazyev_lib):
+    c = Cache(lazyev_lib, "bf16", 128, 2, 4, 16, 100)
+    for weights in (torch.zeros(2, 4, 0, device="cuda"), torch.zeros(2, 4, 7, device="cuda")):
+        sources, w, p = c.cache.evict(0, weights, 5)
+        assert bool((sources == -1).all()) and bool((w == 0).all()) and bool((p == -1).all())
 
 
 def test_positions_of_all_kinds(lazyev_lib):
