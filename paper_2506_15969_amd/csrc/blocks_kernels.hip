@@ -20,8 +20,8 @@
 //   below T - 2 E is not: it is below T - E, and the k blocks from T on are not
 // and those between, a few, are summed again in binary64, where products are exact and equal blocks give equal sums.
 //
-// Measured, us for scores and choice: a token each of 16 sequences, 40 / 8 heads, 3126 blocks of 128 x bf16 (205 MB of bounds) 41 + 16.5, the first at 5.0 TB/s; 640
-// tokens of 28 / 4 heads, 512 blocks 17.4 + 19; 3 x 33 tokens of 32 / 8 heads of 64 x fp32, 313 blocks 12.5 + 13.5.  The second kernel is a chain of latencies: scores,
+// Measured, us for scores and choice: a token each of 16 sequences, 40 / 8 heads, 3126 blocks of 128 x bf16 (205 MB of bounds) 41 + 14.8, the first at 5.0 TB/s; 640
+// tokens of 28 / 4 heads, 512 blocks 17.4 + 14.9; 3 x 33 tokens of 32 / 8 heads of 64 x fp32, 313 blocks 12.5 + 10.6.  The second kernel is a chain of latencies: scores,
 // border (6 us), places (3), and the sums in binary64 that the slowest row asks for (3 - 5).  Scores that stay in LDS, one kernel for a tile of tokens: 53 us
 // in place of 36 for the 640 tokens.
 #include "kernels.h"
@@ -706,9 +706,16 @@ hipError_t launch(ChooseArgs a, hipStream_t stream) {
     const long long blocks = static_cast<long long>(a.n_seqs) * a.tokens * a.n_kv_heads;
     if (blocks > (1ll << 23)) return hipErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(blocks));
+    // (registers that hold no candidate cost as much as others: 8 a thread rather than 16, us for 16 sequences' rows of 8 heads, and for 200 tokens': 500 blocks 16.2, 17.2 ->
+    // 12.4, 14.0; 1000 15.4, 19.1 -> 11.8, 17.0; 2000 17.0, 34 -> 13.9, 24.6.  Beyond, many rows have less of eight waves that wait for one another
+    // than of four: 4000 18.0, 36 -> 16.3, 43; 8000 by eight of 16 rather than sixteen of 16 30.6, 119 -> 20.0, 85, by sixteen of 8 21.5, 132)
     if (a.scored <= 4 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 4>), grid, dim3(64), 0, stream, a);
-    else if (a.scored <= 16 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 16>), grid, dim3(64), 0, stream, a);
+    else if (a.scored <= 8 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 8>), grid, dim3(64), 0, stream, a);
+    else if (a.scored <= 8 * 128) hipLaunchKernelGGL((choose_kernel<T, D, 2, 8>), grid, dim3(128), 0, stream, a);
+    else if (a.scored <= 8 * 256) hipLaunchKernelGGL((choose_kernel<T, D, 4, 8>), grid, dim3(256), 0, stream, a);
+    else if (a.scored <= 8 * 512 && blocks <= 512) hipLaunchKernelGGL((choose_kernel<T, D, 8, 8>), grid, dim3(512), 0, stream, a);
     else if (a.scored <= 16 * 256) hipLaunchKernelGGL((choose_kernel<T, D, 4, 16>), grid, dim3(256), 0, stream, a);
+    else if (a.scored <= 16 * 512) hipLaunchKernelGGL((choose_kernel<T, D, 8, 16>), grid, dim3(512), 0, stream, a);
     else if (a.scored <= 16 * 1024) hipLaunchKernelGGL((choose_kernel<T, D, 16, 16>), grid, dim3(1024), 0, stream, a);
     else hipLaunchKernelGGL((choose_kernel<T, D, 16, 0>), grid, dim3(1024), 0, stream, a);
     const hipError_t e = hipGetLastError();

@@ -133,7 +133,7 @@ def test_choice(lazyev_lib, dtype, d, S, n, Hq, H, length, block, chosen, first,
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("n_blocks", [40, 700, 5000])
+@pytest.mark.parametrize("n_blocks", [40, 400, 700, 1500, 3000, 5000, 12000])
 def test_scores_that_nearly_tie(lazyev_lib, dtype, d, n_blocks):
     """One large sum in all blocks and a difference that sums in 32 bits lose (2^15 and multiples of 2^-12); equal blocks among them."""
     gen = torch.Generator(device="cuda").manual_seed(n_blocks)
@@ -149,7 +149,7 @@ def test_scores_that_nearly_tie(lazyev_lib, dtype, d, n_blocks):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("n_blocks", [30, 900])
+@pytest.mark.parametrize("n_blocks", [30, 400, 900, 1500, 3000, 6000, 9000])
 def test_equal_scores_go_by_their_numbers(lazyev_lib, dtype, d, n_blocks):
     gen = torch.Generator(device="cuda").manual_seed(5)
     dt = _dt(dtype)
@@ -180,6 +180,20 @@ def test_choice_of_very_many_blocks(lazyev_lib, dtype):
     size = lazyev_lib.lib.lazyev_blocks_choose_workspace(lazyev_lib.KeyBounds(bounds, 16).blocks, 16 * 4100, 300, 8, 1, 33)
     assert size < 300 * 8 * 4098 * 12              # (not for all of them at once)
     _choose(lazyev_lib, bounds, 16, 16 * 4100, q, 33)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n_blocks", [250, 500, 1000, 2000, 4000])
+def test_choice_of_many_tokens(lazyev_lib, dtype, d, n_blocks):
+    gen = torch.Generator(device="cuda").manual_seed(n_blocks)
+    dt = _dt(dtype)
+    bounds = _bounds(gen, 2, 2, n_blocks, d, dt)
+    bounds[:, :, 100:120] = bounds[:, :, 150:170]
+    q = torch.randn((2, 150, 6, d), generator=gen, device="cuda").to(dt)
+    q[:, 5] = q[:, 6, :1]
+    vis = torch.randint(0, 16 * n_blocks + 1, (2, 150), generator=gen, device="cuda").int()
+    for visible in (None, vis):
+        _choose(lazyev_lib, bounds, 16, 16 * n_blocks, q, 33, visible=visible, first=1, last=2)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
