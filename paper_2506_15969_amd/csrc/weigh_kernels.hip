@@ -15,7 +15,8 @@
 // few is bound by memory: 5 rows over 32768 entries of each of 128 units, 128 x bf16 (1.1 GB), 212 us, 5.2 TB/s, the rate of a large copy.  many is bound by the
 // products and the multiply-add, exponential and addition beside each of their results: 4096 tokens of 40 / 8 heads over their past (86 GFLOP) 110 us with
 // 5 + 5 for the kernels around it, 780 TFLOP/s, against 1220 of a bf16 product of 8192^3 on the same card; by counters the matrix cores are busy in 34 % of
-// the cycles and vector units in 56, together most of the time.  Blocks in another order than that of their work: 181 us; 16 or 32 splits in place of 8: 115, 124.
+// the cycles and vector units in 56, together most of the time.  Blocks in another order than that of their work: 181 us; 16 or 32 splits in place of 8: 115, 124;
+// three blocks to a compute unit, of waves of 32 entries: 122.
 #include "kernels.h"
 #include "lazyev.h"
 
@@ -309,19 +310,18 @@ __global__ __launch_bounds__(256, 2) void weigh_many_kernel(const WeighArgs a) {
       for (int x = 0; x < kSubs; ++x) {
         f32x16_t s;
         logits<T, D>(q, k[x], s);
-#pragma unroll
-        for (int y = 0; y < 16; ++y) s[y] = fmaf(s[y], c2, -ref[y / 4][y % 4]);
         if (mask) {                                // (what a row does not see has nothing of its lse either, a NaN for instance)
           const int entry = e0 + 32 * x + c;
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const i32x4_t limit = *reinterpret_cast<const i32x4_t *>(&row_sees[buf][half * 32 + 8 * y + 4 * h]);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) s[4 * y + z] = entry < limit[z] ? s[4 * y + z] : -INFINITY;
+            for (int z = 0; z < 4; ++z) sum[x][z & 1] += __builtin_amdgcn_exp2f(entry < limit[z] ? fmaf(s[4 * y + z], c2, -ref[y][z]) : -INFINITY);
           }
-        }
+        } else {
 #pragma unroll
-        for (int y = 0; y < 16; ++y) sum[x][y & 1] += __builtin_amdgcn_exp2f(s[y]);
+          for (int y = 0; y < 16; ++y) sum[x][y & 1] += __builtin_amdgcn_exp2f(fmaf(s[y], c2, -ref[y / 4][y % 4]));
+        }
       }
     }
   };
