@@ -398,8 +398,10 @@ template <int kChunks>
 void launch_select(const WeightEvictArgs &a, const dim3 &grid, hipStream_t stream) {
   const dim3 block(kSelectBlock);
   const int regs = (a.length + kSelectBlock - 1) / kSelectBlock;
+  // (8 units of 7000 entries 14.5 us by 8 keys a lane, 16000 21.4 by 16 and 29 by 32)
   if (regs <= 3) hipLaunchKernelGGL((select_kernel<3, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 8) hipLaunchKernelGGL((select_kernel<8, kChunks>), grid, block, 0, stream, a);
+  else if (regs <= 16) hipLaunchKernelGGL((select_kernel<16, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 32) hipLaunchKernelGGL((select_kernel<32, kChunks>), grid, block, 0, stream, a);
   else if constexpr (kChunks == 0) hipLaunchKernelGGL((select_kernel<0, 0>), grid, block, 0, stream, a);
 }
