@@ -307,6 +307,28 @@ def test_attention(lazyev_lib, dtype, d, S, n, Hq, H, page, length, block, m):
     assert all(torch.equal(x, y) for x, y in zip(c.cache.attend_blocks(length, q, blocks, block), plain))
 
 
+def _off_by_one(x):
+    """The same elements, one element behind an aligned address."""
+    flat = torch.empty(1 + x.numel(), dtype=x.dtype, device="cuda")
+    flat[1:] = x.flatten()
+    return flat[1:].view(x.shape)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n,H", [(3, 2), (40, 7)])
+def test_attention_with_rows_at_odd_addresses(lazyev_lib, dtype, d, n, H):
+    c = Cache(lazyev_lib, dtype, d, 1, H, 16, 300, seed=17)
+    q = c.randn(1, n, 3 * H, d).to(c.dt)
+    blocks = _some_blocks(c, n, 300, 16, 5)
+    joined = (c.randn(1, n, 3 * H, d).to(c.dt), c.randn(1, n, 3 * H))
+    want = c.cache.attend_blocks(300, q, blocks, 16, joined=joined)
+    odd = tuple(_off_by_one(x) for x in joined)
+    got = c.cache.attend_blocks(300, _off_by_one(q), _off_by_one(blocks), 16, joined=odd, out=_off_by_one(q), lse=_off_by_one(joined[1]))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    got = c.cache.attend_blocks(300, q, blocks, 16, joined=odd, out=odd[0], lse=odd[1])
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 # (one token's lists on their own; 40 tokens of 7 KV heads and so on: tiles of tokens)
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("n,H", [(4, 2), (40, 7)])

@@ -8,7 +8,7 @@ import torch
 
 import long64
 from plain64 import U
-from test_gpu_blocks import TYPES, Cache
+from test_gpu_blocks import TYPES, Cache, _off_by_one
 
 pytestmark = pytest.mark.gpu
 
@@ -131,6 +131,17 @@ def test_a_row_whose_logsumexp_is_no_number(lazyev_lib, dtype, d, n):
         got = c.cache.weigh(200, q, lse, visible=vis)
         assert torch.equal(got[0, 1], clean[0, 1]) and torch.equal(got[0, 0, 33:], clean[0, 0, 33:])
         assert bool(torch.isnan(got[0, 0, :33]).all()) if math.isnan(odd) else bool((got[0, 0, :33] <= clean[0, 0, :33]).all())
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n", [1, 40])
+def test_weights_with_rows_at_odd_addresses(lazyev_lib, dtype, d, n):
+    c = Cache(lazyev_lib, dtype, d, 2, 2, 16, 500, seed=18)
+    q = c.randn(2, n, 14, d).to(c.dt)
+    lse, old = _lse(c, 500, q), c.randn(2, 2, 500).exp()
+    want = c.cache.weigh(500, q, lse, old=old, decay=0.5)
+    got = c.cache.weigh(500, _off_by_one(q), _off_by_one(lse), old=_off_by_one(old), decay=0.5, weights=_off_by_one(old))
+    assert torch.equal(got, want)
 
 
 def test_weights_of_nothing(lazyev_lib):
