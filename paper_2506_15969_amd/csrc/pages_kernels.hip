@@ -1176,9 +1176,13 @@ TilePlan tile_plan_of(const AttendArgs &a) {
   const int rows = p.tokens * a.group;
   p.wr = rows <= 32 && !long_rows ? 1 : rows <= 64 ? 2 : 4;
   const long long units = static_cast<long long>(a.n_seqs / n) * p.tiles * a.n_kv_heads;
-  const long long stages = static_cast<long long>(a.length) / (p.wr == 4 || long_rows ? 64 : 128);   // of one token's list
+  // (of the joined list, at most: how much of it the tokens share is not known here.  Splits of eight stages or more, us for kernel and merge; by one token's list they
+  // were fewer: 557 tokens of 8 / 2 heads, 11 of 6240 blocks of 16, one split 172, 11 42; 300 of 40 / 8, 20 of 938 blocks of 32, two 80, five 55;
+  // every token on its own 79, 163)
+  const long long joined = static_cast<long long>(p.tokens) * a.list.n_listed;
+  const long long stages = ((joined < n_blocks ? joined : n_blocks) << a.list.block_shift) / (p.wr == 4 || long_rows ? 64 : 128);
   long long split = (p.wr == 4 ? 512 : 256) / units;
-  if (split > stages / 4) split = stages / 4;
+  if (split > stages / 8) split = stages / 8;
   p.n_split = static_cast<int>(split < 1 ? 1 : split > kSplitMax ? kSplitMax : split);
   return p;
 }
