@@ -119,11 +119,12 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
   // positions from `recent_from` on are the newest
   constexpr int kHeld = kRegs > 0 ? kRegs : 1;
   unsigned held[kHeld];
-  int place[kHeld];
+  constexpr bool kAnew = kRegs == 0 || kRegs > 32;  // positions are read twice, rather than kept
+  int place[kAnew ? 1 : kHeld];
   int newest = len - 1;
   if (positions) {
     newest = INT_MIN;
-    if constexpr (kRegs > 0) {
+    if constexpr (!kAnew) {
 #pragma unroll
       for (int x = 0; x < kRegs; ++x) place[x] = entry_of(x) < len ? positions[entry_of(x)] : INT_MIN;
 #pragma unroll
@@ -143,11 +144,28 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
     return i >= len ? 0u : p >= recent_from || p < a.n_first ? 0xFFFFFFFFu : weight_key(w);
   };
   if constexpr (kRegs > 0) {
-    float w[kHeld];
+    if constexpr (kAnew) {                         // (a few at a time: there are no registers for all of them)
 #pragma unroll
-    for (int x = 0; x < kRegs; ++x) w[x] = entry_of(x) < len ? weights[entry_of(x)] : 0.f;
+      for (int x0 = 0; x0 < kRegs; x0 += 8) {
+        float w[8];
+        int p[8];
 #pragma unroll
-    for (int x = 0; x < kRegs; ++x) held[x] = key_of(entry_of(x), positions ? place[x] : entry_of(x), w[x]);
+        for (int x = 0; x < 8; ++x) {
+          const int i = min(entry_of(x0 + x), len - 1);
+          w[x] = weights[i];
+          p[x] = positions ? positions[i] : entry_of(x0 + x);
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) held[x0 + x] = key_of(entry_of(x0 + x), p[x], w[x]);
+        __asm__ volatile("" ::: "memory");
+      }
+    } else {
+      float w[kHeld];
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) w[x] = entry_of(x) < len ? weights[entry_of(x)] : 0.f;
+#pragma unroll
+      for (int x = 0; x < kRegs; ++x) held[x] = key_of(entry_of(x), positions ? place[x] : entry_of(x), w[x]);
+    }
   }
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (kRegs > 0) {
@@ -273,8 +291,9 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
       }
     }
     __syncthreads();
-    const int word = static_cast<int>(threadIdx.x);
-    auto before_word = [&](int mine, int &total) __attribute__((always_inline)) {
+    constexpr int kWords = (32 * kRegs + kSelectBlock - 1) / kSelectBlock;   // of a thread, next to one another
+    const int word0 = static_cast<int>(threadIdx.x) * kWords;
+    auto before_words = [&](int mine, int &total) __attribute__((always_inline)) {
       int run = mine;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -283,27 +302,42 @@ __global__ __launch_bounds__(kSelectBlock) void select_kernel(const WeightEvictA
       }
       return before_wave(__builtin_amdgcn_readlane(run, 63), total) + run - mine;
     };
-    unsigned kept = word < 32 * kRegs ? beyond_bits[word] : 0u, in = word < 32 * kRegs ? in_bits[word] : 0u;
-    const int n_in = static_cast<int>(__popc(in)), room = want - before_word(n_in, all);   // (of no sign: __popc; room may be negative)
-    if (room >= n_in) {
-      kept |= in;
-    } else {
-      unsigned rest = in;
-      for (int x = 0; x < room; ++x) rest &= rest - 1;
-      kept |= in & ~rest;
+    unsigned kept[kWords], in[kWords], free[kWords], late[kWords];
+    int n_in = 0, n_moves = 0;                     // (of no sign: __popc; room may be negative)
+#pragma unroll
+    for (int y = 0; y < kWords; ++y) {
+      kept[y] = word0 + y < 32 * kRegs ? beyond_bits[word0 + y] : 0u;
+      in[y] = word0 + y < 32 * kRegs ? in_bits[word0 + y] : 0u;
+      n_in += static_cast<int>(__popc(in[y]));
     }
-    const int left = a.keep - 32 * word;           // entries of the word below `keep`
-    const unsigned low_places = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
-    unsigned free = word < 32 * kRegs ? ~kept & low_places : 0u, late = kept & ~low_places;
-    // (numbers of 16 bits: at most 32768 of each)
+    int room = want - before_words(n_in, all);
+#pragma unroll
+    for (int y = 0; y < kWords; ++y) {
+      const int n = static_cast<int>(__popc(in[y]));
+      unsigned rest = room >= n ? 0u : in[y];
+      if (room < n)
+        for (int x = 0; x < room; ++x) rest &= rest - 1;
+      kept[y] |= in[y] & ~rest;
+      room -= n;
+      const int left = a.keep - 32 * (word0 + y);  // entries of the word below `keep`
+      const unsigned low_places = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+      free[y] = word0 + y < 32 * kRegs ? ~kept[y] & low_places : 0u;
+      late[y] = kept[y] & ~low_places;
+      // (numbers of 16 bits: as many of one as of the other, of at most 65536 entries)
+      n_moves += static_cast<int>(__popc(free[y]) | __popc(late[y]) << 16);
+    }
     int both = 0;
-    const int before = before_word(static_cast<int>(__popc(free) | __popc(late) << 16), both);
+    const int before = before_words(n_moves, both);
     all = static_cast<int>(static_cast<unsigned>(both) >> 16);
-    if (word < 32 * kRegs) beyond_bits[word] = kept;
     // (numbers alone: what has to be looked up for an entry is left to a thread of its own)
     int32_t *lates = kChunks > 0 ? late_entry : list + static_cast<size_t>(a.n_seqs) * a.n_kv_heads * a.keep;
-    for (int n = before & 0xFFFF; free; free &= free - 1) list[n++] = 32 * word + __builtin_ctz(free);
-    for (int n = static_cast<int>(static_cast<unsigned>(before) >> 16); late; late &= late - 1) lates[n++] = 32 * word + __builtin_ctz(late);
+    int at_free = before & 0xFFFF, at_late = static_cast<int>(static_cast<unsigned>(before) >> 16);
+#pragma unroll
+    for (int y = 0; y < kWords; ++y) {
+      if (word0 + y < 32 * kRegs) beyond_bits[word0 + y] = kept[y];
+      for (; free[y]; free[y] &= free[y] - 1) list[at_free++] = 32 * (word0 + y) + __builtin_ctz(free[y]);
+      for (; late[y]; late[y] &= late[y] - 1) lates[at_late++] = 32 * (word0 + y) + __builtin_ctz(late[y]);
+    }
     __threadfence_block();
     __syncthreads();
     for (int i = threadIdx.x; i < a.keep; i += kSelectBlock)
@@ -398,12 +432,15 @@ template <int kChunks>
 void launch_select(const WeightEvictArgs &a, const dim3 &grid, hipStream_t stream) {
   const dim3 block(kSelectBlock);
   const int regs = (a.length + kSelectBlock - 1) / kSelectBlock;
-  // (8 units of 7000 entries 14.5 us by 8 keys a lane, 16000 21.4 by 16 and 29 by 32)
+  // (8 units of 7000 entries 14.5 us by 8 keys a lane, 16000 21.4 by 16 and 29 by 32; 33205 to 60000 50 by 64 and 120 by none)
   if (regs <= 3) hipLaunchKernelGGL((select_kernel<3, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 8) hipLaunchKernelGGL((select_kernel<8, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 16) hipLaunchKernelGGL((select_kernel<16, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 32) hipLaunchKernelGGL((select_kernel<32, kChunks>), grid, block, 0, stream, a);
-  else if constexpr (kChunks == 0) hipLaunchKernelGGL((select_kernel<0, 0>), grid, block, 0, stream, a);
+  else if constexpr (kChunks == 0) {
+    if (regs <= 64) hipLaunchKernelGGL((select_kernel<64, 0>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((select_kernel<0, 0>), grid, block, 0, stream, a);
+  }
 }
 
 }  // namespace

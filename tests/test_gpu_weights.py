@@ -223,7 +223,7 @@ def test_eviction(lazyev_lib, dtype, d, S, H, page, length, keep, recent, first)
     _evict(c, length, coarse, keep, recent, first, positions=positions, lengths=lengths, in_place=True)
 
 
-@pytest.mark.parametrize("length,keep", [(12000, 3000), (16384, 16000), (20000, 6000), (32768, 32000), (40001, 5000), (100003, 90000)])
+@pytest.mark.parametrize("length,keep", [(12000, 3000), (16384, 16000), (20000, 6000), (32768, 32000), (32769, 300), (50000, 49000), (65536, 30000), (65537, 30000), (40001, 5000), (100003, 90000)])
 def test_eviction_of_long_caches(lazyev_lib, length, keep):
     c = Cache(lazyev_lib, "bf16", 64, 1, 2, 256, length, seed=11)
     weights = torch.floor(4 * c.randn(1, 2, length).exp()) / 4
