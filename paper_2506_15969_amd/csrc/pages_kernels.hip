@@ -1171,7 +1171,8 @@ TilePlan tile_plan_of(const AttendArgs &a) {
   int most = (long_rows ? 64 : 128) / a.group;
   most = most < 32 ? most : 32;                    // (a bit each)
   p.tokens = n < most ? n : most;
-  if (p.tokens < 2) return TilePlan{0, 0, 0, 1};
+  // (entries of a joined list have 32-bit numbers, and it may be as long as all of its tokens' together: numbers twice are pairs of their own)
+  if (p.tokens < 2 || (static_cast<long long>(p.tokens) * a.list.n_listed << a.list.block_shift) > (1 << 30)) return TilePlan{0, 0, 0, 1};
   p.tiles = (n + p.tokens - 1) / p.tokens;
   const int rows = p.tokens * a.group;
   p.wr = rows <= 32 && !long_rows ? 1 : rows <= 64 ? 2 : 4;
