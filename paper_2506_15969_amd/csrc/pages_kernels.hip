@@ -1092,11 +1092,13 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
 }
 
 // The lists of a tile's tokens as one: blocks that some token reads, ascending, with a bit for each token that does.  A number that a
-// token's list has twice is a pair of its own, behind the others.  One block per unit.
+// token's list has had before is a pair of its own, behind the others: token by token (a wave each), in its list's order.  One block per unit.
+// One such number of one token in each tile, us for the whole call: 640 tokens over 32 of 512 blocks each 128 as without, 300 over 200 of 938 179 and 174 without (one
+// thread that goes over all tokens' numbers: 263, 1405).
 constexpr int kListBlocks = 8192;       // of a table row, whose bits LDS holds
 __global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
   __shared__ unsigned bits[kListBlocks];
-  __shared__ int counts[4], again;
+  __shared__ int counts[4], twice[32];             // (twice: numbers of a token that its list has had before)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int unit = static_cast<int>(blockIdx.x), tile = unit / a.n_kv_heads, kvh = unit - tile * a.n_kv_heads;
   const int table_row = tile / a.list.tiles, token0 = (tile - table_row * a.list.tiles) * a.n_tokens;
@@ -1104,23 +1106,19 @@ __global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
   const int n_blocks = (a.list.entries + (1 << a.list.block_shift) - 1) >> a.list.block_shift;
   int2 *to = a.list.pairs + static_cast<long long>(unit) * a.list.n_listed * a.n_tokens;
   for (int b = threadIdx.x; b < n_blocks; b += 256) bits[b] = 0;
-  if (threadIdx.x == 0) again = 0;
+  if (threadIdx.x < 32) twice[threadIdx.x] = 0;
   __syncthreads();
-  // number x of the tokens' lists, -1 where it is no block that its token sees
-  auto number = [&](int x, int &i) __attribute__((always_inline)) {
-    i = x / a.list.n_listed;
+  // number y of token i's list, -1 where it is no block that the token sees
+  auto number = [&](int i, int y) __attribute__((always_inline)) {
     const long long token = static_cast<long long>(table_row) * a.list.tokens + token0 + i;
-    const int b = a.list.list[(token * a.n_kv_heads + kvh) * a.list.n_listed + (x - i * a.list.n_listed)];
+    const int b = a.list.list[(token * a.n_kv_heads + kvh) * a.list.n_listed + y];
     const int reach = a.visible ? min(max(a.visible[token], 0), a.list.entries) : a.list.entries;
     return b >= 0 && b <= (reach - 1) >> a.list.block_shift ? b : -1;
   };
-  bool twice = false;
   for (int x = threadIdx.x; x < n; x += 256) {
-    int i;
-    const int b = number(x, i);
-    if (b >= 0) twice |= (atomicOr(&bits[b], 1u << i) >> i & 1u) != 0;
+    const int i = x / a.list.n_listed, b = number(i, x - i * a.list.n_listed);
+    if (b >= 0 && (atomicOr(&bits[b], 1u << i) >> i & 1u) != 0) atomicAdd(&twice[i], 1);
   }
-  if (twice) again = 1;
   __syncthreads();
   int at = 0;
   for (int b0 = 0; b0 < n_blocks; b0 += 256) {
@@ -1138,19 +1136,40 @@ __global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
     if (mine) to[before + __popcll(m & ((1ull << lane) - 1))] = make_int2(b, static_cast<int>(mine));
     __syncthreads();
   }
-  if (again) {                                     // (uniform) one after the other, in the lists' order
+  int all = at;
+  for (int i = 0; i < tokens; ++i) all += twice[i];
+  if (all > at) {                                  // (uniform)
     for (int b = threadIdx.x; b < n_blocks; b += 256) bits[b] = 0;
     __syncthreads();
-    if (threadIdx.x == 0)
-      for (int x = 0; x < n; ++x) {
-        int i;
-        const int b = number(x, i);
-        if (b < 0) continue;
-        if (bits[b] >> i & 1u) to[at++] = make_int2(b, static_cast<int>(1u << i));
-        bits[b] |= 1u << i;
+    int next = at;                                 // the place of token i's first one
+    for (int i = 0; i < tokens; next += twice[i++]) {
+      if (i % 4 != wave || twice[i] == 0) continue;            // (wave-uniform)
+      int place = next;
+      for (int y0 = 0; y0 < a.list.n_listed; y0 += 64) {
+        const int b = y0 + lane < a.list.n_listed ? number(i, y0 + lane) : -1;
+        // had before these 64 (nobody else has this token's bits); then, of equal ones among them, all but the first
+        bool had = b >= 0 && (*const_cast<volatile unsigned *>(&bits[max(b, 0)]) >> i & 1u) != 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const bool met = b >= 0 && (atomicOr(&bits[max(b, 0)], 1u << i) >> i & 1u) != 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (__ballot(met && !had) != 0) {          // (wave-uniform)
+          bool later = false;
+          for (unsigned long long rest = __ballot(b >= 0 && !had); rest != 0;) {
+            const int first = __builtin_ctzll(rest);
+            const unsigned long long same = rest & __ballot(b == __builtin_amdgcn_readlane(b, first));
+            later |= lane != first && (same >> lane & 1u) != 0;
+            rest &= ~same;
+          }
+          had |= later;
+        }
+        const unsigned long long m = __ballot(had);
+        const int to_place = place + __popcll(m & ((1ull << lane) - 1));
+        if (had && to_place < n) to[to_place] = make_int2(b, static_cast<int>(1u << i));   // (n: lists that change meanwhile, which no caller may do)
+        place += __popcll(m);
       }
+    }
   }
-  if (threadIdx.x == 0) a.list.counts[unit] = at;
+  if (threadIdx.x == 0) a.list.counts[unit] = min(all, n);
 }
 
 // Tokens that share a block's rows, by their lists as one (0: every token on its own), in tiles of a table row's; blocks of wr times 32 rows; splits of a
