@@ -436,6 +436,8 @@ size_t lazyev_blocks_choose_workspace(const lazyev_blocks *blocks /*host*/, int3
 /* lazyev_pages_attend over the entries of listed blocks alone: for every token and KV head those of the blocks chosen[s][i][kvh][..] that the token
  * sees, visible and all else as there (a token that sees nothing of its blocks gets zeros and lse = -inf; what it does not see has no influence).  A number that is
  * no block of the row's first `length` entries, -1 for instance, stands for none; a number twice counts its entries twice.
+ * Equal calls give equal bits; but lists of several tokens are gone over together, so that the order of a token's sums, and with it their roundings,
+ * may depend on what else a call lists.
  * block: 16, 32, 64 or 128; n_chosen >= 1, n_chosen * block at most 2^30; a group of up to 64 heads; n_seqs * n_tokens * n_kv_heads at most 2^22.
  * Pools of up to 2^32 - 1 rows.  Errors: those of lazyev_pages_attend. */
 int lazyev_blocks_attend(const lazyev_pages *pages /*host*/, int32_t length, int32_t block, int32_t n_chosen,

@@ -14,7 +14,8 @@
 // The reference is raised only when a lane's sum of weights relative to it in a stage (16 or, with 64 entries of a stage to a wave, 32 of
 // them) exceeds 2^12 (never rescaled otherwise): a sum is as exact relative to any reference in the range of fp32, and with weights of 2^8 on average at
 // most over 2^30 entries values of up to 2^89 stay in it.  Every decision that changes a row's arithmetic
-// is taken for that row alone: what other rows see has no influence on it.
+// is taken for that row alone: what other rows see has no influence on it.  (But for tiles of tokens with lists of their own, see kPerTile: the lists of
+// the others say which stage and split an entry of the joined list is in, and so move the roundings of a row's sums.)
 // Entries that a row does not see (or that lead to no page) are masked to weight zero, which leaves a NaN of the output where V
 // holds an infinity or NaN, as a weight's second term does.  A block that masked something, or has second terms, and ends up with such an output starts
 // over, with those taken out of V in the stages where it masks (all of them); the rows that do see one get it at the end.
