@@ -475,7 +475,10 @@ size_t lazyev_pages_weigh_workspace(const lazyev_pages *pages /*host*/, int32_t 
  * sources (device): [n_seqs][n_kv_heads][keep], the entry that each place holds now, -1 from n on.
  * weights, positions (device): `stride` elements from one KV head to the next (at least length; length 0: may be null).  weights_to, positions_to (device, nullable): weights and positions
  *   of the places, 0 and -1 from n on, `to_stride` elements from one KV head to the next (at least keep); they may be weights and positions with the same
- *   stride, and overlap nothing else.  Rows of entries of no page are not moved.  An entry below `keep` that two table rows share holds an unspecified one of their rows.
+ *   stride, and overlap nothing else.  Rows of entries of no page are not moved.
+ * Pages that are in the table more than once (a prefix that sequences share): rows are moved for all table rows and KV heads at once, in no order.  So no entry that
+ *   one of them moves, from or to, may lie in such a page, or that place's keys and values are undefined afterwards, a mixture of several entries' even.  Shared entries that
+ *   all stay where they are (the first ones, n_first of them or more) are safe; others are copied to pages of their own before.
  * keep >= 1, n_recent, n_first >= 0, n_recent + n_first <= keep; n_seqs * n_kv_heads below 2^22, n_seqs * n_kv_heads * (keep / 64 + 1) below 2^24; length up to 2^30.
  * Workspace: lazyev_pages_evict_workspace bytes, 256-byte aligned, needing no initial contents.  Errors: EINVAL, EWORKSPACE, EHIP. */
 int lazyev_pages_evict(const lazyev_pages *pages /*host*/, int32_t length, const int32_t *lengths /*device, nullable*/, int32_t keep,

@@ -460,7 +460,8 @@ class PagedCache:
         """lazyev_pages_evict: of the first `length` entries of each row and KV head (lengths int32 [S]: of each row its own number) `keep`
         stay: the `recent` newest and the `first` ones by `positions` (int32 like weights, None: the entries' numbers) and those of the largest weights
         (fp32 [S,Hkv,m], m >= length); those that stay from `keep` on move to free places below it -> (sources int32 [S,Hkv,keep],
-        weights_out, positions_out of the places: new tensors [S,Hkv,keep] where none are given; in place: weights and positions themselves)."""
+        weights_out, positions_out of the places: new tensors [S,Hkv,keep] where none are given; in place: weights and positions themselves).
+        Pages that several rows share hold no entry that moves or that another one takes the place of: copy them before, or keep them by `first`."""
         pg, device = self.pages, self.device
         _need(0 <= length <= self.entries, "entries beyond the table's row")
         _need(1 <= keep < 1 << 30 and 0 <= recent and 0 <= first and recent + first <= keep, "newest and first entries are some of those that stay")
