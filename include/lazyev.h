@@ -409,7 +409,8 @@ typedef struct {
  * block's bounds are extended, so that the same call after every append keeps all of them.  Other blocks are left alone.  (Entries that change otherwise, by
  * an eviction for instance, are counted in anew from their block's first one on.)  A NaN among a block's keys is in its bounds; entries of no page are
  * not counted: a block of nothing else has bounds of +inf and -inf.
- * Sizes agree between pages and blocks; start + n_tokens <= n_blocks * block.  Errors: EINVAL, EHIP. */
+ * Sizes agree between pages and blocks; start + n_tokens <= n_blocks * block and at most 2^30; n_seqs * n_kv_heads at most 2^22, and times the blocks that the entries lie
+ * in 2^25.  Errors: EINVAL, EHIP. */
 int lazyev_blocks_bound(const lazyev_pages *pages /*host*/, const lazyev_blocks *blocks /*host*/, int32_t start, int32_t n_tokens,
                         void *stream);
 
@@ -450,8 +451,10 @@ size_t lazyev_blocks_attend_workspace(const lazyev_pages *pages /*host*/, int32_
 
 /* The attention weight that every entry received, over the tokens that see it and the heads of its group:
  *   weights[s][kvh][e] = (e < known and decay is not 0 ? decay * old[s][kvh][e] : 0) + sum of exp(scale * q k - lse),  e < length
- * with the lse that lazyev_pages_attend (or lazyev_blocks_attend) gave these queries; one over more than the row's entries, a joined one, gives
- * the weights beside those.  Called for a prompt and then for every step, with decay 1, it keeps the sum of all weights; with decay 0 those of
+ * with the lse that lazyev_pages_attend gave these queries; one over more than the row's entries, a joined one, gives
+ * the weights beside those.  An lse over chosen blocks alone (lazyev_blocks_attend) gives the weights beside those blocks: right for the entries that the token read; any other one
+ * that it sees (but did not read) gets exp(its logit - lse) too, which nothing bounds (+inf is possible), and which a sum with decay 1 keeps.  Who evicts by weights
+ * takes the lse over all entries.  Called for a prompt and then for every step, with decay 1, it keeps the sum of all weights; with decay 0 those of
  * the call alone.  A token whose lse is -inf adds nothing, nor does any token to an entry that it does not see or that lies in no page.
  * old, weights: fp32, `stride` elements from one KV head to the next (at least length), and n_kv_heads times that from one row to the next; weights may be
  * old (known 0: old may be null).  No other argument overlaps weights.  scale as in lazyev_pages_attend, decay finite.

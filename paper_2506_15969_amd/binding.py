@@ -437,7 +437,8 @@ class PagedCache:
 
     def weigh(self, length, q, lse, weights=None, old=None, known=None, decay=1.0, visible=None, scale=0.0, workspace=None):
         """lazyev_pages_weigh: the attention weight that each of the first `length` entries received from the queries q [S,n,Hq,d] (or
-        [n,Hq,d]), whose log-sum-exps `attend` gave, over the tokens that see it and its group's heads, added to `decay` times what the first `known`
+        [n,Hq,d]), whose log-sum-exps `attend` gave (those of `attend_blocks` are over the blocks read alone: weights of other entries are then not
+        bounded by 1, and nothing to evict by), over the tokens that see it and its group's heads, added to `decay` times what the first `known`
         entries had in `old` (known None: all of them if `old` is given) -> weights fp32 [S,Hkv,m], m >= length (None: a new tensor like `old`, or of
         `length` entries; what lies behind `length` is left as it is).  weights may be `old`."""
         pg, device = self.pages, self.device
