@@ -479,6 +479,8 @@ size_t lazyev_pages_weigh_workspace(const lazyev_pages *pages /*host*/, int32_t 
  * weights, positions (device): `stride` elements from one KV head to the next (at least length; length 0: may be null).  weights_to, positions_to (device, nullable): weights and positions
  *   of the places, 0 and -1 from n on, `to_stride` elements from one KV head to the next (at least keep); they may be weights and positions with the same
  *   stride, and overlap nothing else.  Rows of entries of no page are not moved.
+ * Not for the caches of a context while it goes on with them: their statistics and positions (and its number of entries) would stay as they are, beside other entries'
+ *   keys and values.  lazyev_evict is that call.
  * Pages that are in the table more than once (a prefix that sequences share): rows are moved for all table rows and KV heads at once, in no order.  So no entry that
  *   one of them moves, from or to, may lie in such a page, or that place's keys and values are undefined afterwards, a mixture of several entries' even.  Shared entries that
  *   all stay where they are (the first ones, n_first of them or more) are safe; others are copied to pages of their own before.

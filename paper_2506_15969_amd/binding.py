@@ -333,7 +333,9 @@ class NormRope:
 class PagedCache:
     """Keys and values of one layer in pages: k_pages, v_pages [n_pages,Hkv,page_size,d] and table [S,m] int32 (entry i of row s is
     place i % page_size of page table[s, i // page_size]), all the caller's tensors.  A layer's caches of a LazyEviction are such
-    pages too: PagedCache(eng.k_cache[l], eng.v_cache[l], table) with one page per sequence, a page number = a sequence.  Results carry no gradients."""
+    pages too: PagedCache(eng.k_cache[l], eng.v_cache[l], table) with one page per sequence, a page number = a sequence
+    (but for `evict`, which moves keys and values alone: an engine's TS, MRI and positions would stay behind; eng.evict moves all of them).  Results carry
+    no gradients."""
 
     def __init__(self, k_pages, v_pages, table, n_q_heads=None):
         for x in (k_pages, v_pages):
