@@ -383,32 +383,17 @@ class PagedCache:
         lse [S,n,Hq] fp32).  visible int32 [S,n]: entries that a token sees (None: all).  joined: (out, lse) of the same queries
         over other entries, to be joined.  workspace: uint8, at least workspace_bytes(length, n) (None: allocated)."""
         pg, shape, device = self.pages, q.shape, self.device
-        _need(q.dtype is self.dtype and (len(shape) == 4 and shape[0] == pg.n_seqs or len(shape) == 3 and pg.n_seqs == 1) and
-              shape[-1] == pg.head_dim and q.is_contiguous() and q.device == device,
-              "queries are [S, n, Hq, head_dim] of the table's rows, contiguous, of the pages' type, on their GPU")
-        n, n_q_heads, rows = shape[-3], shape[-2], shape[:-1]
-        _need(self.n_q_heads in (None, n_q_heads), "another number of query heads")
-        _need(0 <= length <= self.entries, "entries beyond the table's row")
+        n, n_q_heads, rows, seen, other = self._queries(length, q, visible, joined)
         if out is None:
             out = torch.empty_like(q)
         else:
             _need(out.shape == shape and out.dtype is q.dtype and out.is_contiguous() and out.device == device, "out is like q")
         if lse is None:
             lse = q.new_empty(rows, dtype=torch.float32)
-        other = []
-        for o, l in ((None, lse),) if joined is None else ((None, lse), joined):
-            _need((o is None or o.shape == shape and o.dtype is q.dtype and o.is_contiguous() and o.device == device) and
-                  l.shape == rows and l.dtype is torch.float32 and l.is_contiguous() and l.device == device,
-                  "outputs are like q, log-sum-exps fp32, one for each row of q")
-            other = [None if o is None else o.data_ptr(), l.data_ptr()]
-        seen = None
-        if visible is not None:
-            _need(visible.dtype is torch.int32 and visible.shape == shape[:-2] and visible.is_contiguous() and visible.device == device,
-                  "visible is int32, one for each token, contiguous, on the pages' GPU")
-            seen = visible.data_ptr()
+        else:
+            _need(lse.shape == rows and lse.dtype is torch.float32 and lse.is_contiguous() and lse.device == device, "lse is fp32, one for each row of q")
         workspace, n_bytes = self._workspace(length, n, n_q_heads, workspace)
-        code = _launch(device, lib.lazyev_pages_attend, pg, length, n, n_q_heads, seen, q.data_ptr(), other[0],
-                       None if joined is None else other[1], out.data_ptr(), lse.data_ptr(), scale,
+        code = _launch(device, lib.lazyev_pages_attend, pg, length, n, n_q_heads, seen, q.data_ptr(), other[0], other[1], out.data_ptr(), lse.data_ptr(), scale,
                        None if workspace is None else workspace.data_ptr(), n_bytes)
         _check(code, "lazyev_pages_attend")
         return out, lse

@@ -27,6 +27,7 @@
 #include "kernels.h"
 #include "lanes.h"
 #include "lazyev.h"
+#include "rows.h"
 
 #include <cfloat>
 #include <climits>
@@ -149,18 +150,6 @@ __device__ __forceinline__ float squares_of(u32x4_t lo, u32x4_t hi, float sum) {
 }
 // Not below the norm whose squares sum up to this: 128 roundings and the root's, and elements too small to have a square in fp32.
 __device__ __forceinline__ float norm_of(float squares) { return sqrtf(squares) * (1.f + 0x1p-10f) + 0x1p-50f; }
-
-// Elements at any address of their own type.
-template <typename T>
-__device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
-  if (wide) return *reinterpret_cast<const u32x4_t *>(p);
-  T e[16 / sizeof(T)];
-#pragma unroll
-  for (int x = 0; x < static_cast<int>(16 / sizeof(T)); ++x) e[x] = p[x];
-  u32x4_t w;
-  __builtin_memcpy(&w, e, 16);
-  return w;
-}
 
 __device__ __forceinline__ float add(float x, float y) { return x + y; }
 
@@ -297,8 +286,10 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
   return x != x ? ~0ull : u ^ (static_cast<unsigned long long>(static_cast<long long>(u) >> 63) | 1ull << 63);
 }
 
-// What a row's waves share; kAgain: blocks between the borders whose exact scores it holds.
-template <int kWaves, int kRegs, int kAgain>
+constexpr int kAgain = 512;             // blocks between the borders whose exact scores a row holds
+
+// What a row's waves share.
+template <int kWaves, int kRegs>
 struct Room {
   int i[2][kWaves];
   unsigned u[2][kWaves];
@@ -336,8 +327,8 @@ __device__ __forceinline__ V over_waves(V x, V (&room)[2][kWaves], int &turn, F 
 // 64 (x kWaves + wave) + lane is x of a lane); 0: there are more of them, and they are read anew for every look.
 // T is not needed to its last bit: an interval of T no wider than E does, so the bits of its order are settled from the first one in which candidates
 // differ to about the fourteenth behind, by counts of the candidates from a number on.
-template <typename T, int D, int kWaves, int kRegs, int kAgain, typename F>
-__device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Room<kWaves, kRegs, kAgain> &room, F numbers) {
+template <typename T, int D, int kWaves, int kRegs>
+__device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Room<kWaves, kRegs> &room, const float *scores, const float *peaks) {
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int kBlock = 64 * kWaves, C = D * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
   constexpr int kLooks = kRegs * kWaves, kHeld = kRegs > 0 ? kRegs : 1;
@@ -355,8 +346,8 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   // candidates are the blocks first .. first + n - 1, of which `want` go
   const int n = nb - a.n_last - a.n_first, want = a.n_chosen - a.n_last - a.n_first;
   const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + kvh;
-  const auto score = [&](int i) __attribute__((always_inline)) { return numbers.score(i + a.n_first); };
-  const auto peak = [&](int i) __attribute__((always_inline)) { return numbers.peak(i + a.n_first); };
+  const auto score = [&](int i) __attribute__((always_inline)) { return scores[i + a.n_first]; };
+  const auto peak = [&](int i) __attribute__((always_inline)) { return peaks[i + a.n_first]; };
   const T *q = static_cast<const T *>(a.q) + (token * a.n_q_heads + static_cast<long long>(kvh) * a.group) * D;
   for (int i = thread; i < a.n_first; i += kBlock) to[i] = i;
   for (int i = thread; i < a.n_last; i += kBlock) to[a.n_chosen - a.n_last + i] = nb - a.n_last + i;
@@ -642,18 +633,13 @@ __device__ __forceinline__ void choose_row(const ChooseArgs &a, unsigned row, Ro
   }
 }
 
-// Scores from memory, one block for a row.
-struct ScoresFrom {
-  const float *s, *p;
-  __device__ float score(int b) const { return s[b]; }
-  __device__ float peak(int b) const { return p[b]; }
-};
+// One block for a row.
 template <typename T, int D, int kWaves, int kRegs>
 __global__ __launch_bounds__(64 * kWaves) void choose_kernel(const ChooseArgs a) {
-  __shared__ Room<kWaves, kRegs, 512> room;
+  __shared__ Room<kWaves, kRegs> room;
   const unsigned row = blockIdx.x, its = row / a.n_kv_heads, seq = its / a.tokens;
   const size_t unit = static_cast<size_t>(seq) * a.n_kv_heads + (row - its * a.n_kv_heads);
-  choose_row<T, D, kWaves, kRegs, 512>(a, row, room, ScoresFrom{a.score + static_cast<size_t>(row) * a.scored, a.peak + unit * a.scored});
+  choose_row<T, D, kWaves, kRegs>(a, row, room, a.score + static_cast<size_t>(row) * a.scored, a.peak + unit * a.scored);
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }

@@ -31,6 +31,7 @@
 // few: one token's 28 heads over 8192 entries 13.3 us, of which the second launch 5.5, the products 1.3 and the entries' arrival 1.0.
 #include "kernels.h"
 #include "lazyev.h"
+#include "rows.h"
 
 #include <cfloat>
 #include <climits>
@@ -119,13 +120,6 @@ struct RowPlace {
   int head, kvh;                    // head: within the KV head's group
   long long row;                    // token * n_q_heads + query head
 };
-// x / y for 0 <= x < 2^24, y > 0 (the rounded quotient is off by one at most).
-__device__ __forceinline__ int quotient(int x, int y) {
-  int q = static_cast<int>(static_cast<float>(x) * __builtin_amdgcn_rcpf(static_cast<float>(y)));
-  const int r = x - q * y;
-  q += r >= y ? 1 : 0;
-  return q - (r < 0 ? 1 : 0);
-}
 __device__ __forceinline__ RowPlace row_place(const AttendArgs &a, int unit, int r) {
   RowPlace p;
   const int seq = a.n_seqs == 1 ? 0 : unit / a.n_kv_heads, i = quotient(r, a.group);

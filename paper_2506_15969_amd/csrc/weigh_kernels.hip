@@ -19,6 +19,7 @@
 // three blocks to a compute unit, of waves of 32 entries: 122.
 #include "kernels.h"
 #include "lazyev.h"
+#include "rows.h"
 
 #include <climits>
 
@@ -47,24 +48,6 @@ struct Rows {
   __device__ static int slot(int r, int x) { return x ^ (kChunks == 8 ? (r >> 1) & 7 : r & 15); }
 };
 
-template <typename T>
-__device__ __forceinline__ u32x4_t load_chunk(const T *p, bool wide) {
-  if (wide) return *reinterpret_cast<const u32x4_t *>(p);
-  T e[16 / sizeof(T)];
-#pragma unroll
-  for (int x = 0; x < static_cast<int>(16 / sizeof(T)); ++x) e[x] = p[x];
-  u32x4_t w;
-  __builtin_memcpy(&w, e, 16);
-  return w;
-}
-
-// x / y for 0 <= x < 2^24, y > 0 (the rounded quotient is off by one at most).
-__device__ __forceinline__ int quotient(int x, int y) {
-  int q = static_cast<int>(static_cast<float>(x) * __builtin_amdgcn_rcpf(static_cast<float>(y)));
-  const int r = x - q * y;
-  q += r >= y ? 1 : 0;
-  return q - (r < 0 ? 1 : 0);
-}
 // The row r of a unit among all rows of q; its token.
 __device__ __forceinline__ long long row_of(const WeighArgs &a, int seq, int kvh, int r, long long &token) {
   const int i = quotient(r, a.group);
