@@ -310,7 +310,7 @@ struct ChooseArgs {
   void *workspace;
   // filled in by the launch: the tokens of each sequence that it is for; what it leaves in the workspace
   int32_t token0, tokens, wide;
-  float *peak;                      // [units][scored] largest bound of a block, in size
+  float *peak;                      // [units][scored] not below the Euclidean norm of a block's bounds, of each element the larger one in size
   float *score;                     // [n_seqs][tokens][n_kv_heads][scored]
   unsigned long long *exact;        // the same, of some blocks
 };

@@ -1,12 +1,14 @@
 // The attention weight that every entry of a cache received (lazyev_pages_weigh): w[i] = (old) + sum over the rows r that see entry i of
 // exp(scale q_r k_i - lse_r), rows being the tokens' heads of the entry's group.
 //
-// Both kernels have keys as the B operand of 32 x 32 products (32x32x16_bf16; fp32 rows: 32x32x2_f32) and rows as A: lane (c, h) = (l % 32, l / 32)
-// holds, of entry c, the logits of the rows 8 i + 4 h + j (i, j < 4), so the sum over rows is one in its register.  Rows
-// that do not see all of the entries are masked, by the number of entries that they see; those past the last, and those that saw nothing (lse of
-// -inf), see none.
-//   few   rows that fit one operand (a decode step): a wave keeps them and goes over tiles of 32 entries, one on its way while another is worked on
-//   many  the waves of a block keep 32 kSubs entries each and go over stages of 64 rows, fetched straight into LDS while the stage before
+// Both kernels have keys as the B operand and rows as A, so that a lane holds, of one entry, the logits of several rows, and the sum over rows is one in its
+// register, then over the lanes of the same entry.  Rows that do not see all of the entries are masked, by the number of entries that they see; those past the
+// last, and those that saw nothing (lse of -inf), see none.  The exponent is one multiply-add, logit scale log2 e - lse log2 e, of an lse that is
+// rounded once more in these units: half a step, 2^-24, of it, as much as the lse's own rounding is; sums are fp32, two of a lane and sub-tile at most.
+//   few   up to 32 rows (a decode step), as one or two operands of 16: 16x16x32_bf16 (fp32 rows: 16x16x4_f32), lane (c, g) = (l % 16, l / 16) holds the rows
+//         4 g + j of each 16 for entry c.  A wave keeps them and goes over tiles of 32 entries, one on its way while another is worked on
+//   many  32x32x16_bf16 (fp32 rows: 32x32x2_f32), lane (c, h) = (l % 32, l / 32) holds, of entry c, the rows 8 i + 4 h + j (i, j < 4) of each 32.
+//         The waves of a block keep 32 kSubs entries each and go over stages of 64 rows, fetched straight into LDS while the stage before
 //         is worked on.  A small kernel before it leaves, for every row, lse in units of log 2 and what it sees, and for every
 //         stage the least and the most that a row of it sees: a block goes over the stages that see some of its entries alone.
 // Few entries of many rows: the stages are also dealt out to splits in turn (where tokens see their past, late rows are seen by all entries,
@@ -382,7 +384,7 @@ Plan plan_of(const WeighArgs &a) {
   Plan p = {0, 0, 0, 1};
   const int M = a.n_tokens * a.group, units = a.n_seqs * a.n_kv_heads;
   p.many = M > 32;
-  if (!p.many) {                                   // (two blocks a compute unit, a few tiles a wave where there are so many)
+  if (!p.many) {                                   // (four blocks a compute unit, a few tiles a wave where there are so many)
     const int blocks = ((a.length + 31) / 32 + 3) / 4, most = (1024 + units - 1) / units;
     p.across = blocks < most ? blocks : most;
     return p;
