@@ -1,4 +1,5 @@
-"""Evictions of table rows that share pages, in the ways that leave every row its own entries: what is shared stays in its place, or was copied before."""
+"""Evictions of table rows that share pages, in the ways that leave every row its own entries (what is shared stays in its place, or was copied before); and those with
+the most moves that there can be."""
 import numpy as np
 import pytest
 import torch
@@ -49,3 +50,12 @@ def test_a_shared_prefix_copied_before(lazyev_lib, dtype):
             x[c.table[s, :6].long()] = x[c.table[0, :6].long()]
     before = c.rows(c.k_pages).clone(), c.rows(c.v_pages).clone()
     _check(c, before, c.randn(S, H, length).exp(), length, keep, 16, 4)
+
+
+@pytest.mark.parametrize("length,keep", [(65536, 32768), (65535, 32768), (65536, 65535), (65536, 1)])
+def test_as_many_moves_as_there_can_be(lazyev_lib, length, keep):
+    """All that stay are the last entries, so that every place (or every entry that goes) is one to move to: the largest numbers that the places' sums hold."""
+    c = Cache(lazyev_lib, "bf16", 64, 1, 2, 256, length, seed=52)
+    before = c.rows(c.k_pages).clone(), c.rows(c.v_pages).clone()
+    weights = torch.arange(length, device="cuda").float().expand(1, 2, length).contiguous()
+    _check(c, before, weights, length, keep, 0, 0)
