@@ -694,7 +694,8 @@ hipError_t launch(ChooseArgs a, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(blocks));
     // (registers that hold no candidate cost as much as others: 8 a thread rather than 16, us for 16 sequences' rows of 8 heads, and for 200 tokens': 500 blocks 16.2, 17.2 ->
     // 12.4, 14.0; 1000 15.4, 19.1 -> 11.8, 17.0; 2000 17.0, 34 -> 13.9, 24.6.  Beyond, many rows have less of eight waves that wait for one another
-    // than of four: 4000 18.0, 36 -> 16.3, 43; 8000 by eight of 16 rather than sixteen of 16 30.6, 119 -> 20.0, 85, by sixteen of 8 21.5, 132)
+    // than of four: 4000 18.0, 36 -> 16.3, 43; 8000 by eight of 16 rather than sixteen of 16 30.6, 119 -> 20.0, 85, by sixteen of 8 21.5, 132.
+    // More than 16384: read anew for every look.  Scores and choice for a token of 28 / 4 heads over 16000 and 17000 blocks 39 and 279, for 4 x 16 tokens 83 and 425)
     if (a.scored <= 4 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 4>), grid, dim3(64), 0, stream, a);
     else if (a.scored <= 8 * 64) hipLaunchKernelGGL((choose_kernel<T, D, 1, 8>), grid, dim3(64), 0, stream, a);
     else if (a.scored <= 8 * 128) hipLaunchKernelGGL((choose_kernel<T, D, 2, 8>), grid, dim3(128), 0, stream, a);

@@ -432,7 +432,7 @@ template <int kChunks>
 void launch_select(const WeightEvictArgs &a, const dim3 &grid, hipStream_t stream) {
   const dim3 block(kSelectBlock);
   const int regs = (a.length + kSelectBlock - 1) / kSelectBlock;
-  // (8 units of 7000 entries 14.5 us by 8 keys a lane, 16000 21.4 by 16 and 29 by 32; 33205 to 60000 50 by 64 and 120 by none)
+  // (keys of up to three, rather than eight, a lane: 128 units of 2112 entries 14.7 us of the whole call, 17.1; 8 of 1500 14.9, 16.7.  8 units of 7000 entries 14.5 us by 8 keys a lane, 16000 21.4 by 16 and 29 by 32; 33205 to 60000 50 by 64 and 120 by none)
   if (regs <= 3) hipLaunchKernelGGL((select_kernel<3, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 8) hipLaunchKernelGGL((select_kernel<8, kChunks>), grid, block, 0, stream, a);
   else if (regs <= 16) hipLaunchKernelGGL((select_kernel<16, kChunks>), grid, block, 0, stream, a);

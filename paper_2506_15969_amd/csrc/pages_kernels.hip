@@ -63,7 +63,9 @@ struct Rows {
   static constexpr int kTiles = D / 32;            // output tiles of 32 columns
   // Terms of a weight in the product with V.  128 x bf16 weights are rounded, as the decode step rounds them: two terms take a third longer where
   // products bind (4096 tokens of 40 / 8 heads over their past 207 -> 269 us, 80 rows over 100003 entries 81 -> 99) and lower the error against 64 bits from 0.0020 - 0.0022
-  // to the 0.0016 - 0.0017 of the output's own rounding.  64 x bf16 rows the decode step keeps exact with three terms; two are as far below that rounding
+  // to the 0.0016 - 0.0017 of the output's own rounding.  Listed entries the same: one token each of 16 sequences over 64 blocks of 32 of 8 KV heads 30.5 -> 31.5 us, 640
+  // tokens of 28 / 4 heads over 32 of 512 blocks 128 -> 154 (weights kept in fp32 until they are needed; both terms at once 157, with registers spilled), error 0.0023 -> 0.0017.
+  // 64 x bf16 rows the decode step keeps exact with three terms; two are as far below that rounding
   // here (the same calls with one / two / three terms 142 / 183 / 219 us, 52 / 56 - 61 / 71; 224 rows over 8192 entries 16.2 / 17.3 / 18.2).
   static constexpr int kTerms = kF32 || D == 128 ? 1 : 2;
   // Where chunk x of entry r of a stage lies among the entry's chunks: keys are read by 16 entries at a time, one chunk of
@@ -1090,7 +1092,7 @@ hipError_t launch(AttendArgs a, hipStream_t stream) {
 // token's list has had before is a pair of its own, behind the others: token by token (a wave each), in its list's order.  One block per unit.
 // One such number of one token in each tile, us for the whole call: 640 tokens over 32 of 512 blocks each 128 as without, 300 over 200 of 938 179 and 174 without (one
 // thread that goes over all tokens' numbers: 263, 1405).
-constexpr int kListBlocks = 8192;       // of a table row, whose bits LDS holds
+constexpr int kListBlocks = 8192;       // of a table row, whose bits LDS holds (beyond: every token on its own.  640 tokens of 28 / 4 heads over 128 blocks of 16: 320 us of 8192, 386 of 8193)
 __global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
   __shared__ unsigned bits[kListBlocks];
   __shared__ int counts[4], twice[32];             // (twice: numbers of a token that its list has had before)
@@ -1175,7 +1177,12 @@ __global__ __launch_bounds__(256) void join_lists_kernel(const AttendArgs a) {
 // the last one with 3 splits (2 167, 4 155, 5 135, 8 132: blocks come in rounds of 512), two blocks of four waves to a compute unit; with eight waves that
 // share 128 rows, a block to a compute unit, 175.  More stages on their way make no difference, so their arrival does not bind: by counters waves wait for one another
 // in 57 % of their time, at the barrier of a stage that some of them pass over, and matrix cores are busy in 16 %, vector units in 30 %.
-// Few units (at most one for each compute unit): every token on its own, as the latency of one's list is what counts.
+// The other types, us for the whole call, every token on its own -> tiles: those 640 tokens 64 x bf16 146 -> 105, 64 x fp32 598 -> 336, 128 x fp32 1742 -> 1028; 300 tokens of 40 /
+// 8 heads over 20 of 469 blocks of 64 157 -> 58 (64 x bf16 61 -> 48, 64 x fp32 219 -> 115, 128 x fp32 583 -> 246).  Lists of few entries lose: 2 x 100 tokens of 8 / 2 heads
+// over 11 of 1250 blocks of 16 21 -> 29 (64 x bf16 10 -> 26, 64 x fp32 25 -> 35, 128 x fp32 45 -> 42), by the two more launches.
+// Few units (at most one for each compute unit): every token on its own, as the latency of one's list is what counts.  Tokens of 28 / 4 heads over 32 blocks of 64, 128 x
+// bf16 (64 x fp32), own -> tiles: 64 units 19 -> 28 us (24 -> 31), 128 28 -> 30 (38 -> 41), 192 41 -> 33 (62 -> 49), 256 42 -> 36 (63 -> 58), 260 76 -> 36 (118 -> 57), 512 80 -> 48
+// (121 -> 89).  Of 2 / 1 heads: 32 15 -> 22, 128 28 -> 26, 256 42 -> 27, 260 78 -> 28: the second round of blocks is what tiles save.
 struct TilePlan { int tokens, tiles, wr, n_split; };
 TilePlan tile_plan_of(const AttendArgs &a) {
   TilePlan p = {0, 0, 0, 1};
